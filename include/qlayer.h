@@ -336,6 +336,45 @@ int ql_sample(ql_dtype dtype, int32_t n_qubits, int64_t batch, const void* psi, 
               const double* uniforms, int64_t* samples, void* zhat, void* workspace,
               size_t workspace_bytes, hipStream_t stream);
 
+/* ---- operators around a quantum layer -------------------------------------
+ *
+ * What a hybrid network needs on either side of its quantum layer: a norm that
+ * brings features to the range of angles, with its gradients. They need no
+ * circuit, allocate nothing, keep nothing between calls, run on the given
+ * stream and can be captured in a graph. Pointers are device addresses that are
+ * multiples of the element's size; outputs and the workspace overlap nothing. */
+
+/* Element types. Statistics and sums are fp64 for QL_F64 and fp32 otherwise
+ * (fp64 where sums of workgroups are joined); outputs are rounded once. */
+typedef enum { QL_F32 = 0, QL_F64 = 1, QL_BF16 = 2, QL_F16 = 3 } ql_type;
+
+/* Layer norm of rows of features:
+ *   y = (x - mean) * rstd * weight + bias,  mean = sum x / features,
+ *   rstd = 1 / sqrt(sum (x - mean)^2 / features + eps).
+ * x holds rows that start x_stride elements apart (>= 0: rows may be columns of
+ * a wider array, or one row repeated); y[rows][features] is contiguous.
+ * weight[features] and bias[features] (weight_type: type, or QL_F32 beside
+ * QL_BF16 and QL_F16 rows) may each be NULL (1 and 0). mean[rows] and
+ * rstd[rows] (QL_F64 for QL_F64, else QL_F32) are what the backward call needs
+ * and may each be NULL. A row that holds an infinity or NaN gives NaN in that
+ * row alone. rows = 0 does nothing.
+ *
+ * The backward call: with h = (x - mean) * rstd,
+ *   grad_x      = rstd * (g w - mean(g w) - h * mean(g w h)),
+ *   grad_weight = sum over rows of g h,   grad_bias = sum over rows of g,
+ * each of which may be NULL (not computed); grad_y's rows start grad_stride
+ * elements apart, grad_x[rows][features] is contiguous. The workspace is only
+ * needed with grad_weight or grad_bias. Sums over rows run in a fixed order. */
+int ql_layer_norm_forward(ql_type type, ql_type weight_type, int64_t rows, int64_t features,
+                          const void* x, int64_t x_stride, const void* weight, const void* bias,
+                          double eps, void* y, void* mean, void* rstd, hipStream_t stream);
+int ql_layer_norm_workspace_bytes(ql_type type, int64_t rows, int64_t features, size_t* out);
+int ql_layer_norm_backward(ql_type type, ql_type weight_type, int64_t rows, int64_t features,
+                           const void* grad_y, int64_t grad_stride, const void* x, int64_t x_stride,
+                           const void* mean, const void* rstd, const void* weight, void* grad_x,
+                           void* grad_weight, void* grad_bias, void* workspace,
+                           size_t workspace_bytes, hipStream_t stream);
+
 /* Message of the last failing call on this thread ("" if none). */
 const char* ql_last_error(void);
 

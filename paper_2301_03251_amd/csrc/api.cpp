@@ -19,6 +19,7 @@
 #include <string>
 #include <vector>
 
+#include "errors.hpp"
 #include "launch.hpp"
 #include "plan.hpp"
 #include "runs_launch.hpp"
@@ -33,6 +34,20 @@ int fail(int code, const std::string& msg) {
     g_err = msg;
     return code;
 }
+
+}  // namespace
+
+int qlayer::set_error(int code, const char* what, const char* detail) noexcept {
+    try {
+        g_err = what;
+        if (detail) g_err.append(": ").append(detail);
+    } catch (...) {  // no memory for the message: the code still says what happened
+        g_err.clear();
+    }
+    return code;
+}
+
+namespace {
 
 size_t align256(size_t x) { return (x + 255) & ~size_t(255); }
 

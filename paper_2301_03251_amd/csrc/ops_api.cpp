@@ -1,0 +1,96 @@
+// ops_api.cpp -- C entries of the operators around a quantum layer (qlayer.h):
+// argument checks, workspace layout, launches on the caller's stream. They hold
+// no state and allocate nothing.
+#include <hip/hip_runtime.h>
+
+#include <cmath>
+#include <cstdint>
+
+#include "errors.hpp"
+#include "norm.hpp"
+#include "qlayer.h"
+
+using namespace qlayer;
+
+namespace {
+
+int fail(int code, const char* what, const char* detail = nullptr) { return set_error(code, what, detail); }
+
+bool known_type(int t) { return t >= QL_F32 && t <= QL_F16; }
+
+// A device array's address is a multiple of its element's size (NULL is).
+bool aligned(const void* p, int type) { return (uintptr_t)p % elem_size(type) == 0; }
+
+const int64_t MOST_ELEMENTS = (int64_t)1 << 46;
+
+int check_norm(int type, int wtype, int64_t rows, int64_t features) {
+    if (!known_type(type) || !known_type(wtype)) return fail(QL_EINVAL, "unknown type");
+    if (wtype != type && !(wtype == QL_F32 && (type == QL_BF16 || type == QL_F16)))
+        return fail(QL_EUNSUPPORTED, "weight_type is neither the rows' type nor QL_F32 beside 16-bit rows");
+    if (rows < 0) return fail(QL_EINVAL, "rows must be >= 0");
+    if (features < 1 || features > INT32_MAX) return fail(QL_EINVAL, "features out of range [1, 2^31)");
+    if (rows > MOST_ELEMENTS / features) return fail(QL_EINVAL, "rows * features too large");
+    return QL_OK;
+}
+
+bool stride_ok(int64_t rows, int64_t stride) {
+    return stride >= 0 && (rows <= 1 || stride <= MOST_ELEMENTS / rows);
+}
+
+}  // namespace
+
+extern "C" {
+
+int ql_layer_norm_forward(ql_type type, ql_type weight_type, int64_t rows, int64_t features, const void* x,
+                          int64_t x_stride, const void* weight, const void* bias, double eps, void* y, void* mean,
+                          void* rstd, hipStream_t stream) {
+    if (int rc = check_norm(type, weight_type, rows, features)) return rc;
+    if (!(eps >= 0) || std::isinf(eps)) return fail(QL_EINVAL, "eps must be finite and >= 0");
+    if (!stride_ok(rows, x_stride)) return fail(QL_EINVAL, "x_stride out of range");
+    if (rows > 0 && (!x || !y)) return fail(QL_EINVAL, "x or y is NULL");
+    const int stat = type == QL_F64 ? QL_F64 : QL_F32;
+    if (!aligned(x, type) || !aligned(y, type) || !aligned(weight, weight_type) || !aligned(bias, weight_type) ||
+        !aligned(mean, stat) || !aligned(rstd, stat))
+        return fail(QL_EINVAL, "misaligned pointer");
+    NormArgs a{};
+    a.x = x, a.weight = weight, a.bias = bias, a.y = y, a.mean = mean, a.rstd = rstd;
+    a.rows = rows, a.D = features, a.x_stride = x_stride, a.eps = eps;
+    const hipError_t e = launch_norm_forward(type, weight_type, a, stream);
+    if (e != hipSuccess) return fail(QL_EHIP, "layer norm", hipGetErrorString(e));
+    return set_error(QL_OK, "");
+}
+
+int ql_layer_norm_workspace_bytes(ql_type type, int64_t rows, int64_t features, size_t* out) {
+    if (!out) return fail(QL_EINVAL, "NULL argument");
+    if (int rc = check_norm(type, type, rows, features)) return rc;
+    *out = norm_workspace(type, rows, features);
+    return set_error(QL_OK, "");
+}
+
+int ql_layer_norm_backward(ql_type type, ql_type weight_type, int64_t rows, int64_t features, const void* grad_y,
+                           int64_t grad_stride, const void* x, int64_t x_stride, const void* mean, const void* rstd,
+                           const void* weight, void* grad_x, void* grad_weight, void* grad_bias, void* ws,
+                           size_t ws_bytes, hipStream_t stream) {
+    if (int rc = check_norm(type, weight_type, rows, features)) return rc;
+    if (!stride_ok(rows, x_stride) || !stride_ok(rows, grad_stride)) return fail(QL_EINVAL, "stride out of range");
+    if (rows > 0 && (!grad_y || !x || !mean || !rstd)) return fail(QL_EINVAL, "grad_y, x, mean or rstd is NULL");
+    const int stat = type == QL_F64 ? QL_F64 : QL_F32;
+    if (!aligned(grad_y, type) || !aligned(x, type) || !aligned(grad_x, type) || !aligned(weight, weight_type) ||
+        !aligned(grad_weight, weight_type) || !aligned(grad_bias, weight_type) || !aligned(mean, stat) ||
+        !aligned(rstd, stat))
+        return fail(QL_EINVAL, "misaligned pointer");
+    if (grad_weight || grad_bias) {
+        if (!ws) return fail(QL_EINVAL, "workspace is NULL");
+        if (!aligned(ws, QL_F64)) return fail(QL_EINVAL, "misaligned workspace");
+        if (ws_bytes < norm_workspace(type, rows, features)) return fail(QL_ENOMEM, "workspace too small");
+    }
+    NormArgs a{};
+    a.grad = grad_y, a.x = x, a.mean = (void*)mean, a.rstd = (void*)rstd, a.weight = weight;
+    a.grad_x = grad_x, a.grad_weight = grad_weight, a.grad_bias = grad_bias, a.part = ws;
+    a.rows = rows, a.D = features, a.x_stride = x_stride, a.grad_stride = grad_stride;
+    const hipError_t e = launch_norm_backward(type, weight_type, a, stream);
+    if (e != hipSuccess) return fail(QL_EHIP, "layer norm backward", hipGetErrorString(e));
+    return set_error(QL_OK, "");
+}
+
+}  // extern "C"

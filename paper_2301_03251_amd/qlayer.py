@@ -59,7 +59,8 @@ EXPORTS = ("ql_circuit_create", "ql_circuit_create_ex", "ql_circuit_create_desc"
            "ql_param_shift_workspace_bytes", "ql_param_shift", "ql_state_workspace_bytes",
            "ql_state", "ql_sample_workspace_bytes", "ql_sample",
            "ql_plan_info_get", "ql_call_kernel", "ql_plan_schedule", "ql_plan_state_bytes",
-           "ql_timing_enable", "ql_timing_read")
+           "ql_timing_enable", "ql_timing_read", "ql_layer_norm_forward",
+           "ql_layer_norm_workspace_bytes", "ql_layer_norm_backward")
 
 
 def load():
@@ -89,6 +90,11 @@ def load():
     lib.ql_state.argtypes = [P, ctypes.c_int, I64, P, P, P, P, SZ, P]
     lib.ql_sample_workspace_bytes.argtypes = [I32, I64, ctypes.POINTER(SZ)]
     lib.ql_sample.argtypes = [ctypes.c_int, I32, I64, P, I64, P, P, P, P, SZ, P]
+    D = ctypes.c_double
+    lib.ql_layer_norm_forward.argtypes = [ctypes.c_int, ctypes.c_int, I64, I64, P, I64, P, P, D, P, P, P, P]
+    lib.ql_layer_norm_workspace_bytes.argtypes = [ctypes.c_int, I64, I64, ctypes.POINTER(SZ)]
+    lib.ql_layer_norm_backward.argtypes = [ctypes.c_int, ctypes.c_int, I64, I64, P, I64, P, I64, P, P, P, P, P, P,
+                                           P, SZ, P]
     lib.ql_last_error.argtypes = []
     lib.ql_last_error.restype = ctypes.c_char_p
     lib.ql_plan_info_get.argtypes = [P, ctypes.c_int, ctypes.POINTER(_PlanInfo)]
