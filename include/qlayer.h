@@ -357,18 +357,24 @@ typedef enum { QL_F32 = 0, QL_F64 = 1, QL_BF16 = 2, QL_F16 = 3 } ql_type;
  * QL_BF16 and QL_F16 rows) may each be NULL (1 and 0). mean[rows] and
  * rstd[rows] (QL_F64 for QL_F64, else QL_F32) are what the backward call needs
  * and may each be NULL. A row that holds an infinity or NaN gives NaN in that
- * row alone. rows = 0 does nothing.
+ * row alone. features in [1, 2^30]; rows = 0 does nothing.
  *
  * The backward call: with h = (x - mean) * rstd,
  *   grad_x      = rstd * (g w - mean(g w) - h * mean(g w h)),
  *   grad_weight = sum over rows of g h,   grad_bias = sum over rows of g,
  * each of which may be NULL (not computed); grad_y's rows start grad_stride
- * elements apart, grad_x[rows][features] is contiguous. The workspace is only
- * needed with grad_weight or grad_bias. Sums over rows run in a fixed order. */
+ * elements apart, grad_x[rows][features] is contiguous. Sums over rows run in a
+ * fixed order.
+ *
+ * ql_layer_norm_workspace_bytes gives the device workspace of a forward
+ * (backward = 0) or backward call; where it is 0, as for forward calls of
+ * ordinary rows, the workspace may be NULL. */
 int ql_layer_norm_forward(ql_type type, ql_type weight_type, int64_t rows, int64_t features,
                           const void* x, int64_t x_stride, const void* weight, const void* bias,
-                          double eps, void* y, void* mean, void* rstd, hipStream_t stream);
-int ql_layer_norm_workspace_bytes(ql_type type, int64_t rows, int64_t features, size_t* out);
+                          double eps, void* y, void* mean, void* rstd, void* workspace,
+                          size_t workspace_bytes, hipStream_t stream);
+int ql_layer_norm_workspace_bytes(ql_type type, int64_t rows, int64_t features, int backward,
+                                  size_t* out);
 int ql_layer_norm_backward(ql_type type, ql_type weight_type, int64_t rows, int64_t features,
                            const void* grad_y, int64_t grad_stride, const void* x, int64_t x_stride,
                            const void* mean, const void* rstd, const void* weight, void* grad_x,

@@ -44,48 +44,68 @@ template <> struct Raw16<4> { using type = raw16_at4; };
 template <> struct Raw16<8> { using type = raw16_at8; };
 
 template <typename T, int V> __device__ __forceinline__ Vec<T, V> load_vec(const T* p) {
-    using R = typename Raw16<alignof(T)>::type;
-    static_assert(sizeof(T) * V % 16 == 0, "whole loads of 16 bytes");
-    struct Q {
-        uint32_t w[sizeof(T) * V / 4];
-    } q;
+    if constexpr (V == 1) {
+        return {{*p}};
+    } else {
+        using R = typename Raw16<alignof(T)>::type;
+        static_assert(sizeof(T) * V % 16 == 0, "whole loads of 16 bytes");
+        struct Q {
+            uint32_t w[sizeof(T) * V / 4];
+        } q;
 #pragma unroll
-    for (int i = 0; i < (int)(sizeof(T) * V / 16); i++) {
-        const R r = ((const R*)p)[i];
-        q.w[4 * i] = r.x, q.w[4 * i + 1] = r.y, q.w[4 * i + 2] = r.z, q.w[4 * i + 3] = r.w;
+        for (int i = 0; i < (int)(sizeof(T) * V / 16); i++) {
+            const R r = ((const R*)p)[i];
+            q.w[4 * i] = r.x, q.w[4 * i + 1] = r.y, q.w[4 * i + 2] = r.z, q.w[4 * i + 3] = r.w;
+        }
+        return __builtin_bit_cast(Vec<T, V>, q);
     }
-    return __builtin_bit_cast(Vec<T, V>, q);
 }
 
 template <typename T, int V> __device__ __forceinline__ void store_vec(T* p, const Vec<T, V>& v) {
-    using R = typename Raw16<alignof(T)>::type;
-    struct Q {
-        uint32_t w[sizeof(T) * V / 4];
-    };
-    const Q q = __builtin_bit_cast(Q, v);
+    if constexpr (V == 1) {
+        *p = v.v[0];
+    } else {
+        using R = typename Raw16<alignof(T)>::type;
+        struct Q {
+            uint32_t w[sizeof(T) * V / 4];
+        };
+        const Q q = __builtin_bit_cast(Q, v);
 #pragma unroll
-    for (int i = 0; i < (int)(sizeof(T) * V / 16); i++) {
-        R r;
-        r.x = q.w[4 * i], r.y = q.w[4 * i + 1], r.z = q.w[4 * i + 2], r.w = q.w[4 * i + 3];
-        ((R*)p)[i] = r;
+        for (int i = 0; i < (int)(sizeof(T) * V / 16); i++) {
+            R r;
+            r.x = q.w[4 * i], r.y = q.w[4 * i + 1], r.z = q.w[4 * i + 2], r.w = q.w[4 * i + 3];
+            ((R*)p)[i] = r;
+        }
     }
 }
 
-// The first n of V elements (zeros behind them) and back.
-template <typename T, int V> __device__ __forceinline__ Vec<T, V> load_some(const T* p, int64_t n) {
-    if (n >= V) return load_vec<T, V>(p);
-    Vec<T, V> r{};
+// The same bits, which the compiler takes for new ones: keeps it from holding
+// what it has unpacked from them in registers until the next use.
+template <typename T, int V> __device__ __forceinline__ void renew(Vec<T, V>& v) {
+    if constexpr (V > 1 && sizeof(T) == 2) {
+        struct Q {
+            uint32_t w[sizeof(T) * V / 4];
+        } q = __builtin_bit_cast(Q, v);
 #pragma unroll
-    for (int e = 0; e < V; e++)
-        if (e < n) r.v[e] = p[e];
-    return r;
+        for (int i = 0; i < (int)(sizeof(T) * V / 4); i++) asm volatile("" : "+v"(q.w[i]));
+        v = __builtin_bit_cast(Vec<T, V>, q);
+    }
 }
-template <typename T, int V> __device__ __forceinline__ void store_some(T* p, const Vec<T, V>& v, int64_t n) {
-    if (n >= V) return store_vec<T, V>(p, v);
-#pragma unroll
-    for (int e = 0; e < V; e++)
-        if (e < n) p[e] = v.v[e];
-}
+
+// Where a lane's vector of a row of D >= V elements lies. One that would pass the
+// row's end is moved back to end with it: its first `skip` elements are then
+// another lane's too (V of them: the lane has none of its own). Loads and
+// stores need no branch, both lanes compute the same values for them, and only
+// sums leave them out.
+template <int V> struct Span {
+    int at, skip;
+    __device__ __forceinline__ Span(int first, int D) {
+        at = min(first, D - V);
+        skip = min(first - at, V);
+    }
+    __device__ __forceinline__ bool own(int e) const { return e >= skip; }
+    __device__ __forceinline__ bool any() const { return skip < V; }
+};
 
 template <int CTRL> __device__ __forceinline__ float dpp_move(float v) {
     return __builtin_bit_cast(float,

@@ -25,13 +25,14 @@ struct NormArgs {
     void* grad_x;        // [rows][D] or null (backward)
     void* grad_weight;   // [D] or null (backward)
     void* grad_bias;     // [D] or null (backward)
-    void* part;          // workspace: the column sums of each workgroup
+    void* part;          // workspace: the column sums of each workgroup,
+    void* sums;          // and of long rows the sums of each segment
     int64_t rows, D, x_stride, grad_stride;
     double eps;
 };
 
-// Bytes of NormArgs::part.
-size_t norm_workspace(int type, int64_t rows, int64_t D);
+// Bytes of the workspace: NormArgs::sums forward (0: none), part backward.
+size_t norm_workspace(int type, int64_t rows, int64_t D, bool backward);
 hipError_t launch_norm_forward(int type, int wtype, const NormArgs& a, hipStream_t s);
 hipError_t launch_norm_backward(int type, int wtype, const NormArgs& a, hipStream_t s);
 

@@ -28,7 +28,7 @@ int check_norm(int type, int wtype, int64_t rows, int64_t features) {
     if (wtype != type && !(wtype == QL_F32 && (type == QL_BF16 || type == QL_F16)))
         return fail(QL_EUNSUPPORTED, "weight_type is neither the rows' type nor QL_F32 beside 16-bit rows");
     if (rows < 0) return fail(QL_EINVAL, "rows must be >= 0");
-    if (features < 1 || features > INT32_MAX) return fail(QL_EINVAL, "features out of range [1, 2^31)");
+    if (features < 1 || features > 1 << 30) return fail(QL_EINVAL, "features out of range [1, 2^30]");
     if (rows > MOST_ELEMENTS / features) return fail(QL_EINVAL, "rows * features too large");
     return QL_OK;
 }
@@ -43,7 +43,7 @@ extern "C" {
 
 int ql_layer_norm_forward(ql_type type, ql_type weight_type, int64_t rows, int64_t features, const void* x,
                           int64_t x_stride, const void* weight, const void* bias, double eps, void* y, void* mean,
-                          void* rstd, hipStream_t stream) {
+                          void* rstd, void* ws, size_t ws_bytes, hipStream_t stream) {
     if (int rc = check_norm(type, weight_type, rows, features)) return rc;
     if (!(eps >= 0) || std::isinf(eps)) return fail(QL_EINVAL, "eps must be finite and >= 0");
     if (!stride_ok(rows, x_stride)) return fail(QL_EINVAL, "x_stride out of range");
@@ -52,18 +52,23 @@ int ql_layer_norm_forward(ql_type type, ql_type weight_type, int64_t rows, int64
     if (!aligned(x, type) || !aligned(y, type) || !aligned(weight, weight_type) || !aligned(bias, weight_type) ||
         !aligned(mean, stat) || !aligned(rstd, stat))
         return fail(QL_EINVAL, "misaligned pointer");
+    if (const size_t need = norm_workspace(type, rows, features, false)) {
+        if (!ws) return fail(QL_EINVAL, "workspace is NULL");
+        if (!aligned(ws, QL_F64)) return fail(QL_EINVAL, "misaligned workspace");
+        if (ws_bytes < need) return fail(QL_ENOMEM, "workspace too small");
+    }
     NormArgs a{};
-    a.x = x, a.weight = weight, a.bias = bias, a.y = y, a.mean = mean, a.rstd = rstd;
+    a.x = x, a.weight = weight, a.bias = bias, a.y = y, a.mean = mean, a.rstd = rstd, a.sums = ws;
     a.rows = rows, a.D = features, a.x_stride = x_stride, a.eps = eps;
     const hipError_t e = launch_norm_forward(type, weight_type, a, stream);
     if (e != hipSuccess) return fail(QL_EHIP, "layer norm", hipGetErrorString(e));
     return set_error(QL_OK, "");
 }
 
-int ql_layer_norm_workspace_bytes(ql_type type, int64_t rows, int64_t features, size_t* out) {
+int ql_layer_norm_workspace_bytes(ql_type type, int64_t rows, int64_t features, int backward, size_t* out) {
     if (!out) return fail(QL_EINVAL, "NULL argument");
     if (int rc = check_norm(type, type, rows, features)) return rc;
-    *out = norm_workspace(type, rows, features);
+    *out = norm_workspace(type, rows, features, backward != 0);
     return set_error(QL_OK, "");
 }
 
@@ -79,10 +84,10 @@ int ql_layer_norm_backward(ql_type type, ql_type weight_type, int64_t rows, int6
         !aligned(grad_weight, weight_type) || !aligned(grad_bias, weight_type) || !aligned(mean, stat) ||
         !aligned(rstd, stat))
         return fail(QL_EINVAL, "misaligned pointer");
-    if (grad_weight || grad_bias) {
+    if (grad_x || grad_weight || grad_bias) {
         if (!ws) return fail(QL_EINVAL, "workspace is NULL");
         if (!aligned(ws, QL_F64)) return fail(QL_EINVAL, "misaligned workspace");
-        if (ws_bytes < norm_workspace(type, rows, features)) return fail(QL_ENOMEM, "workspace too small");
+        if (ws_bytes < norm_workspace(type, rows, features, true)) return fail(QL_ENOMEM, "workspace too small");
     }
     NormArgs a{};
     a.grad = grad_y, a.x = x, a.mean = (void*)mean, a.rstd = (void*)rstd, a.weight = weight;

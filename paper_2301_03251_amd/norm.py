@@ -28,10 +28,10 @@ def type_of(t, what):
 
 
 @functools.lru_cache(maxsize=1024)
-def _workspace_bytes(type_, rows, features):
+def _workspace_bytes(type_, rows, features, backward):
     out = ctypes.c_size_t()
-    _check(load().ql_layer_norm_workspace_bytes(type_, rows, features, ctypes.byref(out)))
-    return max(out.value, 256)
+    _check(load().ql_layer_norm_workspace_bytes(type_, rows, features, backward, ctypes.byref(out)))
+    return out.value
 
 
 def _rows(t):
@@ -90,8 +90,11 @@ def layer_norm_forward(x, weight=None, bias=None, eps=1e-5, stats=True):
         mean = rstd = None
         if stats:
             mean, rstd = torch.empty((2, *x.shape[:-1]), dtype=_stats_dtype(x), device=x.device).unbind(0)
+        ws_bytes = _workspace_bytes(xt, rows, x.shape[-1], 0)
+        ws = torch.empty(ws_bytes, dtype=torch.uint8, device=x.device) if ws_bytes else None
         _check(load().ql_layer_norm_forward(xt, wt, rows, x.shape[-1], xr.data_ptr(), stride, _ptr(weight), _ptr(bias),
-                                            eps, y.data_ptr(), _ptr(mean), _ptr(rstd), _stream(x.device)))
+                                            eps, y.data_ptr(), _ptr(mean), _ptr(rstd), _ptr(ws), ws_bytes,
+                                            _stream(x.device)))
     return y, mean, rstd
 
 
@@ -120,12 +123,10 @@ def layer_norm_backward(grad_y, x, mean, rstd, weight=None, want_x=True, want_we
         gx = torch.empty(x.shape, dtype=x.dtype, device=x.device) if want_x else None
         gw = torch.empty(n, dtype=wd, device=x.device) if want_weight else None
         gb = torch.empty(n, dtype=wd, device=x.device) if want_bias else None
-        ws, ws_bytes = None, 0
-        if want_weight or want_bias:
-            ws_bytes = _workspace_bytes(xt, rows, n)
-            ws = torch.empty(ws_bytes, dtype=torch.uint8, device=x.device)
+        ws_bytes = _workspace_bytes(xt, rows, n, 1)
+        ws = torch.empty(ws_bytes, dtype=torch.uint8, device=x.device)
         _check(load().ql_layer_norm_backward(xt, wt, rows, n, gr.data_ptr(), gs, xr.data_ptr(), xs, mean.data_ptr(),
-                                             rstd.data_ptr(), _ptr(weight), _ptr(gx), _ptr(gw), _ptr(gb), _ptr(ws),
+                                             rstd.data_ptr(), _ptr(weight), _ptr(gx), _ptr(gw), _ptr(gb), ws.data_ptr(),
                                              ws_bytes, _stream(x.device)))
     return gx, gw, gb
 

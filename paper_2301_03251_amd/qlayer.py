@@ -91,8 +91,8 @@ def load():
     lib.ql_sample_workspace_bytes.argtypes = [I32, I64, ctypes.POINTER(SZ)]
     lib.ql_sample.argtypes = [ctypes.c_int, I32, I64, P, I64, P, P, P, P, SZ, P]
     D = ctypes.c_double
-    lib.ql_layer_norm_forward.argtypes = [ctypes.c_int, ctypes.c_int, I64, I64, P, I64, P, P, D, P, P, P, P]
-    lib.ql_layer_norm_workspace_bytes.argtypes = [ctypes.c_int, I64, I64, ctypes.POINTER(SZ)]
+    lib.ql_layer_norm_forward.argtypes = [ctypes.c_int, ctypes.c_int, I64, I64, P, I64, P, P, D, P, P, P, P, SZ, P]
+    lib.ql_layer_norm_workspace_bytes.argtypes = [ctypes.c_int, I64, I64, ctypes.c_int, ctypes.POINTER(SZ)]
     lib.ql_layer_norm_backward.argtypes = [ctypes.c_int, ctypes.c_int, I64, I64, P, I64, P, I64, P, P, P, P, P, P,
                                            P, SZ, P]
     lib.ql_last_error.argtypes = []

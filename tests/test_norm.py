@@ -35,17 +35,20 @@ FAKE = ctypes.c_void_p(0x1000)
 ODD = ctypes.c_void_p(0x1001)
 
 
-def _fwd(lib, type_=F32, wtype=F32, rows=2, n=4, x=FAKE, stride=4, w=FAKE, b=FAKE, eps=EPS, y=FAKE, mean=None, rstd=None):
-    return lib.ql_layer_norm_forward(type_, wtype, rows, n, x, stride, w, b, eps, y, mean, rstd, None)
+def _fwd(lib, type_=F32, wtype=F32, rows=2, n=4, x=FAKE, stride=4, w=FAKE, b=FAKE, eps=EPS, y=FAKE, mean=None, rstd=None, ws=None,
+         ws_bytes=0):
+    return lib.ql_layer_norm_forward(type_, wtype, rows, n, x, stride, w, b, eps, y, mean, rstd, ws, ws_bytes, None)
 
 
 @pytest.mark.parametrize("kw,code", [
     (dict(type_=4), -1), (dict(type_=-1), -1), (dict(wtype=9), -1),
     (dict(wtype=F64), -3), (dict(type_=F64, wtype=F32), -3), (dict(type_=BF16, wtype=F16), -3),
-    (dict(rows=-1), -1), (dict(n=0), -1), (dict(n=-3), -1), (dict(n=1 << 31), -1),
+    (dict(rows=-1), -1), (dict(n=0), -1), (dict(n=-3), -1), (dict(n=(1 << 30) + 1), -1),
     (dict(rows=1 << 40, n=1 << 20), -1), (dict(stride=-4), -1), (dict(rows=1 << 30, stride=1 << 30), -1),
     (dict(eps=-1.0), -1), (dict(eps=float("nan")), -1), (dict(eps=float("inf")), -1),
     (dict(x=None), -1), (dict(y=None), -1), (dict(x=ODD), -1), (dict(y=ODD), -1), (dict(w=ODD), -1),
+    (dict(n=70000, stride=70000), -1), (dict(n=70000, stride=70000, ws=FAKE, ws_bytes=8), -2),
+    (dict(n=70000, stride=70000, ws=ctypes.c_void_p(0x1004), ws_bytes=1 << 20), -1),
     (dict(b=ODD), -1), (dict(mean=ODD), -1), (dict(rstd=ctypes.c_void_p(0x1002)), -1),
 ])
 def test_forward_refuses(lib, kw, code):
@@ -71,12 +74,14 @@ def test_backward_refuses(lib, kw, code):
 
 def test_workspace_bytes(lib):
     out = ctypes.c_size_t()
-    assert lib.ql_layer_norm_workspace_bytes(F32, 4, 8, None) == -1
-    assert lib.ql_layer_norm_workspace_bytes(F32, 4, 0, ctypes.byref(out)) == -1
+    assert lib.ql_layer_norm_workspace_bytes(F32, 4, 8, 1, None) == -1
+    assert lib.ql_layer_norm_workspace_bytes(F32, 4, 0, 1, ctypes.byref(out)) == -1
     for t, size in ((F32, 4), (F64, 8), (BF16, 4), (F16, 4)):
         for rows, n in ((0, 5), (1, 1), (256, 10), (8192, 1024), (3, 100000)):
-            assert lib.ql_layer_norm_workspace_bytes(t, rows, n, ctypes.byref(out)) == 0
+            assert lib.ql_layer_norm_workspace_bytes(t, rows, n, 1, ctypes.byref(out)) == 0
             assert 2 * n * size <= out.value <= 4096 * 2 * n * size
+            assert lib.ql_layer_norm_workspace_bytes(t, rows, n, 0, ctypes.byref(out)) == 0
+            assert (out.value > 0) == (n == 100000)
 
 
 def test_python_refuses_cpu_and_integer_tensors():
