@@ -25,7 +25,9 @@ __device__ __forceinline__ float inv_sqrt(float v) { return 1.0f / sqrtf(v); }
 __device__ __forceinline__ double inv_sqrt(double v) { return 1.0 / sqrt(v); }
 
 // Rows in registers: a group of G lanes holds a row as K vectors of V elements
-// per lane (vector k of lane l starts at element (k G + l) V).
+// per lane (vector k of lane l starts at element (k G + l) V), and takes row,
+// row + stride, ...: weight and bias are read once, and the next row's loads
+// are under way while a row is worked on.
 template <typename T, typename W, int V, int G, int K>
 __global__ __launch_bounds__(G > 256 ? G : 256) void k_norm_fwd(NormArgs a) {
     using R = Acc<T>;
@@ -33,13 +35,28 @@ __global__ __launch_bounds__(G > 256 ? G : 256) void k_norm_fwd(NormArgs a) {
     __shared__ R lds[2][G > 64 ? G / 64 : 1];
     const int lane = threadIdx.x % G;
     const R d = (R)a.D;
-    for (int64_t row = (int64_t)blockIdx.x * ROWS + threadIdx.x / G; row < a.rows; row += (int64_t)gridDim.x * ROWS) {
-        const T* xr = (const T*)a.x + row * a.x_stride;
-        T* yr = (T*)a.y + row * a.D;
+    const int64_t stride = (int64_t)gridDim.x * ROWS;
+    int64_t row = (int64_t)blockIdx.x * ROWS + threadIdx.x / G;
+    Vec<T, V> next[K];
+    auto fetch = [&](int64_t r) {
+        const T* xr = (const T*)a.x + r * a.x_stride;
+#pragma unroll
+        for (int k = 0; k < K; k++) next[k] = load_vec<T, V>(xr + Span<V>((k * G + lane) * V, (int)a.D).at);
+    };
+    if (row < a.rows) fetch(row);
+    Vec<W, V> w[K], b[K];
+#pragma unroll
+    for (int k = 0; k < K; k++) {
+        const Span<V> sp((k * G + lane) * V, (int)a.D);
+        if (a.weight) w[k] = load_vec<W, V>((const W*)a.weight + sp.at);
+        if (a.bias) b[k] = load_vec<W, V>((const W*)a.bias + sp.at);
+    }
+    for (; row < a.rows; row += stride) {
         Vec<T, V> x[K];
         R sum = 0;
 #pragma unroll
-        for (int k = 0; k < K; k++) x[k] = load_vec<T, V>(xr + Span<V>((k * G + lane) * V, (int)a.D).at);
+        for (int k = 0; k < K; k++) x[k] = next[k];
+        fetch(row + stride < a.rows ? row + stride : row);
 #pragma unroll
         for (int k = 0; k < K; k++) {
             const Span<V> sp((k * G + lane) * V, (int)a.D);
@@ -68,18 +85,15 @@ __global__ __launch_bounds__(G > 256 ? G : 256) void k_norm_fwd(NormArgs a) {
             const Span<V> sp((k * G + lane) * V, (int)a.D);
             if (!sp.any()) continue;
             renew(x[k]);
-            Vec<W, V> w, b;
-            if (a.weight) w = load_vec<W, V>((const W*)a.weight + sp.at);
-            if (a.bias) b = load_vec<W, V>((const W*)a.bias + sp.at);
             Vec<T, V> q;
 #pragma unroll
             for (int e = 0; e < V; e++) {
                 R h = (up(x[k].v[e]) - mean) * rstd;
-                if (a.weight) h *= (R)up(w.v[e]);
-                if (a.bias) h += (R)up(b.v[e]);
+                if (a.weight) h *= (R)up(w[k].v[e]);
+                if (a.bias) h += (R)up(b[k].v[e]);
                 q.v[e] = down<T>(h);
             }
-            store_vec<T, V>(yr + sp.at, q);
+            store_vec<T, V>((T*)a.y + row * a.D + sp.at, q);
         }
     }
 }
@@ -335,6 +349,7 @@ template <typename T, typename W> __global__ __launch_bounds__(256) void k_norm_
     const int64_t col = (int64_t)blockIdx.x * 16 + c;  // of 2 D
     double t = 0;
     if (col < 2 * a.D)
+#pragma unroll 8
         for (int64_t k = g; k < chunks; k += 16) t += (double)((const R*)a.part)[k * 2 * a.D + col];
     lds[g][c] = t;
     __syncthreads();
@@ -374,10 +389,10 @@ Split split_of(int type, int64_t rows, int64_t D) {
             break;
         }
     if (p.lanes) {
-        // at least four rows for a group of lanes: its column sums cost a write
-        // and a read of two rows in fp32
-        const int64_t groups = std::max(1, 256 / p.lanes);
-        p.parts = std::max<int64_t>(1, std::min<int64_t>(512, (rows + 4 * groups - 1) / (4 * groups)));
+        // at least four rows for a group of lanes, whose column sums cost a write
+        // and a read of two rows in fp32; no more workgroups than run at once
+        const int64_t groups = std::max(1, 256 / p.lanes), most = p.lanes < 512 ? 512 : 256;
+        p.parts = std::max<int64_t>(1, std::min(most, (rows + 4 * groups - 1) / (4 * groups)));
     } else {
         p.segments = (int)((n + 255) / 256);
         const int64_t most = std::max<int64_t>(1, 2048 / p.segments);
@@ -395,7 +410,9 @@ int grid_of(int64_t groups) { return (int)std::min<int64_t>(groups, 4096); }
 
 template <typename T, typename W, int G, int K, int V = VEC<T>> hipError_t forward_rows(const NormArgs& a, hipStream_t s) {
     constexpr int threads = G > 256 ? G : 256, rows = threads / G;
-    k_norm_fwd<T, W, V, G, K><<<grid_of((a.rows + rows - 1) / rows), threads, 0, s>>>(a);
+    // as many workgroups as run at once, so that weight and bias are read once
+    const int64_t most = 256 * (1024 / threads);
+    k_norm_fwd<T, W, V, G, K><<<(unsigned)std::min<int64_t>((a.rows + rows - 1) / rows, most), threads, 0, s>>>(a);
     return hipGetLastError();
 }
 
@@ -410,9 +427,9 @@ template <typename T, typename W> hipError_t forward(int type, const NormArgs& a
     if (a.D <= 16 * V) return forward_rows<T, W, 16, 1>(a, s);
     if (a.D <= 64 * V) return forward_rows<T, W, 64, 1>(a, s);
     if (a.D <= 128 * V) return forward_rows<T, W, 64, 2>(a, s);
-    if (a.D <= 256 * V) return forward_rows<T, W, 64, 4>(a, s);
+    if (a.D <= 256 * V) return forward_rows<T, W, 256, 1>(a, s);
     if (a.D <= 512 * V) return forward_rows<T, W, 256, 2>(a, s);
-    if (a.D <= 1024 * V) return forward_rows<T, W, 256, 4>(a, s);
+    if (a.D <= 1024 * V) return forward_rows<T, W, 512, 2>(a, s);
     if (a.D <= 2048 * V) return forward_rows<T, W, 1024, 2>(a, s);
     return forward_rows<T, W, 1024, 4>(a, s);
 }
