@@ -339,7 +339,8 @@ int ql_sample(ql_dtype dtype, int32_t n_qubits, int64_t batch, const void* psi, 
 /* ---- operators around a quantum layer -------------------------------------
  *
  * What a hybrid network needs on either side of its quantum layer: a norm that
- * brings features to the range of angles, with its gradients. They need no
+ * brings features to the range of angles, with its gradients, and the
+ * optimiser's step of matrix-shaped weights. They need no
  * circuit, allocate nothing, keep nothing between calls, run on the given
  * stream and can be captured in a graph. Pointers are device addresses that are
  * multiples of the element's size; outputs and the workspace overlap nothing. */
@@ -380,6 +381,66 @@ int ql_layer_norm_backward(ql_type type, ql_type weight_type, int64_t rows, int6
                            const void* mean, const void* rstd, const void* weight, void* grad_x,
                            void* grad_weight, void* grad_bias, void* workspace,
                            size_t workspace_bytes, hipStream_t stream);
+
+/* Orthogonalised updates of matrix-shaped weights (the layers around a quantum
+ * layer, or its own angles as [layers][angles of a layer]).
+ *
+ * O = orthogonalised U: X = U / (|U|_F + eps), turned so that it has no more
+ * rows than columns, then `steps` times
+ *   A = X X^T,   X = a X + (b A + c A^2) X,
+ * which takes every singular value s of X through a s + b s^3 + c s^5 towards 1
+ * and leaves the singular vectors. A matrix of zeros gives zeros; one that holds
+ * an infinity or NaN gives NaN throughout.
+ *
+ * ql_orthogonalize: U = grad, out = O.
+ * ql_muon_step: momentum = mu * momentum + grad, U = grad + mu * momentum (with
+ * nesterov; else U = momentum), out = (1 - lr * weight_decay) * out
+ * - lr * sqrt(max(1, rows / cols)) * O, all in place.
+ *
+ * An entry is `batch` matrices of rows x cols; each array has its strides in
+ * elements between matrices, rows and columns (any order; >= 0, and out and
+ * momentum must not overlap themselves). grad and out are of `type`; momentum
+ * (unused by ql_orthogonalize) is QL_F64 for QL_F64 and QL_F32 otherwise. out may
+ * be grad's array in ql_orthogonalize where the strides are equal. All entries of
+ * a call run together: give a network's matrices in one call.
+ *
+ * Precision: QL_F64 in fp64. QL_F32 and QL_F16 products keep 22 bits of every
+ * factor (two fp16 parts each, three products) or fp32 ones for small matrices;
+ * QL_BF16 products keep 11 (one fp16 part). Sums are fp32, norms fp64.
+ *
+ * options NULL: the defaults in braces. rows, cols in [1, 65536], steps in
+ * [1, 64]; coefficients that let a singular value in [0, 1] grow past 64 before
+ * the last step are refused. The entries are read during the call only. */
+typedef struct {
+    int64_t rows, cols, batch;
+    const void* grad;
+    int64_t grad_stride[3];
+    void* momentum;
+    int64_t momentum_stride[3];
+    void* out;
+    int64_t out_stride[3];
+} ql_matrix;
+
+typedef struct {
+    double a, b, c;   /* {3.4445, -4.7750, 2.0315} */
+    double eps;       /* {1e-7} */
+    int32_t steps;    /* {5} */
+} ql_ortho_options;
+
+typedef struct {
+    double lr, momentum, weight_decay; /* {0.02, 0.95, 0} */
+    int32_t nesterov;                  /* {1} */
+} ql_muon_options;
+
+int ql_orthogonalize_workspace_bytes(ql_type type, const ql_matrix* matrices, int32_t count,
+                                     size_t* out);
+int ql_orthogonalize(ql_type type, const ql_matrix* matrices, int32_t count,
+                     const ql_ortho_options* options, void* workspace, size_t workspace_bytes,
+                     hipStream_t stream);
+/* Same workspace as ql_orthogonalize. */
+int ql_muon_step(ql_type type, const ql_matrix* matrices, int32_t count,
+                 const ql_muon_options* muon, const ql_ortho_options* options, void* workspace,
+                 size_t workspace_bytes, hipStream_t stream);
 
 /* Message of the last failing call on this thread ("" if none). */
 const char* ql_last_error(void);

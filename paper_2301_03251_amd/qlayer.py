@@ -60,7 +60,8 @@ EXPORTS = ("ql_circuit_create", "ql_circuit_create_ex", "ql_circuit_create_desc"
            "ql_state", "ql_sample_workspace_bytes", "ql_sample",
            "ql_plan_info_get", "ql_call_kernel", "ql_plan_schedule", "ql_plan_state_bytes",
            "ql_timing_enable", "ql_timing_read", "ql_layer_norm_forward",
-           "ql_layer_norm_workspace_bytes", "ql_layer_norm_backward")
+           "ql_layer_norm_workspace_bytes", "ql_layer_norm_backward", "ql_orthogonalize_workspace_bytes",
+           "ql_orthogonalize", "ql_muon_step")
 
 
 def load():
@@ -95,6 +96,9 @@ def load():
     lib.ql_layer_norm_workspace_bytes.argtypes = [ctypes.c_int, I64, I64, ctypes.c_int, ctypes.POINTER(SZ)]
     lib.ql_layer_norm_backward.argtypes = [ctypes.c_int, ctypes.c_int, I64, I64, P, I64, P, I64, P, P, P, P, P, P,
                                            P, SZ, P]
+    lib.ql_orthogonalize_workspace_bytes.argtypes = [ctypes.c_int, P, I32, ctypes.POINTER(SZ)]
+    lib.ql_orthogonalize.argtypes = [ctypes.c_int, P, I32, P, P, SZ, P]
+    lib.ql_muon_step.argtypes = [ctypes.c_int, P, I32, P, P, P, SZ, P]
     lib.ql_last_error.argtypes = []
     lib.ql_last_error.restype = ctypes.c_char_p
     lib.ql_plan_info_get.argtypes = [P, ctypes.c_int, ctypes.POINTER(_PlanInfo)]
