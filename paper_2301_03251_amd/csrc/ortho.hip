@@ -72,10 +72,21 @@ __device__ __forceinline__ Acc<T> same_update(const Source& s, const Rule& r, in
     const Acc<T> g = grad_at<T>(s, b, i, j);
     return s.momentum ? look_ahead<T>(r, g, momentum_at<T>(s, b, i, j)) : g;
 }
+template <typename T> __device__ __forceinline__ T* out_at(const Target& t, int64_t b, int64_t i, int64_t j) {
+    return (T*)t.out + b * t.ob + i * t.oi + j * t.oj;
+}
 template <typename T>
 __device__ __forceinline__ void write_out(const Target& t, const Rule& r, int64_t b, int64_t i, int64_t j, Acc<T> o) {
-    T* p = (T*)t.out + b * t.ob + i * t.oi + j * t.oj;
+    T* p = out_at<T>(t, b, i, j);
     *p = down<T>(r.muon ? (Acc<T>)r.keep * up(*p) - (Acc<T>)t.step * o : o);
+}
+
+// Four values side by side in the caller's rows.
+template <typename T> struct __attribute__((packed, aligned(sizeof(T)))) Four {
+    T v[4];
+};
+template <typename T> __device__ __forceinline__ Four<T>* four_at(const Target& t, int64_t b, int64_t i, int64_t j) {
+    return (Four<T>*)((T*)t.out + b * t.ob + i * t.oi + j);
 }
 
 // The entry of a launch's table whose blocks (first[e] ..) hold this one.
@@ -225,29 +236,11 @@ __host__ __device__ inline Layout layout_of(int mp, int np, int unit) {
     return {0, x, 3 * x, 3 * x + s, 3 * x + 2 * s};
 }
 
-template <int F> __device__ __forceinline__ void put(char* p, int64_t row, int64_t ld, int col, double v) {
+__device__ __forceinline__ void put(char* p, int64_t row, int64_t ld, int col, double v) {
     ((double*)(p + row * ld))[col] = v;
 }
-template <int F> __device__ __forceinline__ void put(char* p, int64_t row, int64_t ld, int col, float v) {
-    _Float16* r = (_Float16*)(p + row * ld);
-    const _Float16 hi = (_Float16)v;
-    if constexpr (F == ONE) {
-        r[col] = hi;
-    } else {
-        r += col / 32 * 64 + col % 32;
-        r[0] = hi;
-        r[32] = (_Float16)(v - (float)hi);
-    }
-}
-template <int F> __device__ __forceinline__ std::conditional_t<F == DOUBLE, double, float> get(const char* p, int64_t row, int64_t ld, int col) {
-    if constexpr (F == DOUBLE) {
-        return ((const double*)(p + row * ld))[col];
-    } else {
-        const _Float16* r = (const _Float16*)(p + row * ld);
-        if constexpr (F == ONE) return (float)r[col];
-        r += col / 32 * 64 + col % 32;
-        return (float)r[0] + (float)r[32];
-    }
+__device__ __forceinline__ double get(const char* p, int64_t row, int64_t ld, int col) {
+    return ((const double*)(p + row * ld))[col];
 }
 
 struct PackEntry {
@@ -263,8 +256,11 @@ struct PackArgs {
     int32_t count;
 };
 
-// The momentum's step and the sums of squares, a chunk of lines each.
+// The momentum's step and the sums of squares, a chunk of lines each: lines lie
+// along the arrays' unit stride where they have one, and are read in vectors.
 template <typename T> __global__ __launch_bounds__(256) void k_ortho_norm(PackArgs a) {
+    using R = Acc<T>;
+    constexpr int V = 16 / (int)sizeof(T);
     __shared__ double lds[4];
     const PackEntry& e = a.e[entry_of(a.e, a.count, blockIdx.x)];
     const int at = blockIdx.x - e.first, chunk = at % e.chunks;
@@ -272,10 +268,32 @@ template <typename T> __global__ __launch_bounds__(256) void k_ortho_norm(PackAr
     const bool by_row = e.s.gj == 1 || e.s.gi != 1;
     const int lines = by_row ? e.m : e.n, length = by_row ? e.n : e.m;
     const int l0 = (int)((int64_t)lines * chunk / e.chunks), l1 = (int)((int64_t)lines * (chunk + 1) / e.chunks);
+    const int64_t gl = by_row ? e.s.gi : e.s.gj, ml = by_row ? e.s.mi : e.s.mj;
+    const bool vectors = (by_row ? e.s.gj : e.s.gi) == 1 && (!e.s.momentum || (by_row ? e.s.mj : e.s.mi) == 1);
+    const int whole = vectors ? length / V : 0, rest = length - whole * V;
     double sq = 0;
-    for (int64_t k = threadIdx.x; k < (int64_t)(l1 - l0) * length; k += 256) {
-        const int l = l0 + (int)(k / length), f = (int)(k % length);
-        const Acc<T> u = first_update<T>(e.s, a.r, b, by_row ? l : f, by_row ? f : l);
+    for (unsigned k = threadIdx.x; k < (unsigned)(l1 - l0) * (unsigned)whole; k += 256) {
+        const int l = l0 + (int)(k / (unsigned)whole), f = (int)(k % (unsigned)whole) * V;
+        const Vec<T, V> g = load_vec<T, V>((const T*)e.s.grad + b * e.s.gb + l * gl + f);
+        Vec<R, V> u;
+        if (e.s.momentum) {
+            R* p = (R*)e.s.momentum + b * e.s.mb + l * ml + f;
+            u = load_vec<R, V>(p);
+#pragma unroll
+            for (int i = 0; i < V; i++) u.v[i] = (R)a.r.momentum * u.v[i] + up(g.v[i]);
+            store_vec<R, V>(p, u);
+#pragma unroll
+            for (int i = 0; i < V; i++) u.v[i] = look_ahead<T>(a.r, up(g.v[i]), u.v[i]);
+        } else {
+#pragma unroll
+            for (int i = 0; i < V; i++) u.v[i] = up(g.v[i]);
+        }
+#pragma unroll
+        for (int i = 0; i < V; i++) sq += (double)u.v[i] * (double)u.v[i];
+    }
+    for (unsigned k = threadIdx.x; k < (unsigned)(l1 - l0) * (unsigned)rest; k += 256) {
+        const int l = l0 + (int)(k / (unsigned)rest), f = whole * V + (int)(k % (unsigned)rest);
+        const R u = first_update<T>(e.s, a.r, b, by_row ? l : f, by_row ? f : l);
         sq += (double)u * (double)u;
     }
     sq = group_sum<256>(sq, lds);
@@ -296,19 +314,38 @@ template <typename T> __global__ __launch_bounds__(256) void k_ortho_pack(PackAr
     for (int k = threadIdx.x; k < e.chunks; k += 256) sq += e.part[b * e.chunks + k];
     const double inv = a.scale / (sqrt(group_sum<256>(sq, lds)) + a.r.eps);
     const bool by_row = e.s.gj == 1 || e.s.gi != 1;
-#pragma unroll 4
-    for (int k = threadIdx.x; k < 64 * 64; k += 256) {
-        const int i = by_row ? k / 64 : k % 64, j = by_row ? k % 64 : k / 64;
+#pragma unroll
+    for (int c = 0; c < 16; c++) {
+        const int k = c * 256 + threadIdx.x, i = by_row ? k / 64 : k % 64, j = by_row ? k % 64 : k / 64;
         double u = 0;
         if (i0 + i < e.m && j0 + j < e.n) u = (double)same_update<T>(e.s, a.r, b, i0 + i, j0 + j) * inv;
         tile[i][j] = (R)u;
     }
     __syncthreads();
     const Layout l = layout_of(mp, np, unit_of(F));
-    char* w = e.work + b * l.size;
-    for (int k = threadIdx.x; k < 64 * 64; k += 256) {
-        put<F>(w + l.x, i0 + k / 64, (int64_t)np * unit_of(F), j0 + k % 64, tile[k / 64][k % 64]);
-        put<F>(w + l.xt, j0 + k / 64, (int64_t)mp * unit_of(F), i0 + k % 64, tile[k % 64][k / 64]);
+    char *x = e.work + b * l.size + l.x, *xt = e.work + b * l.size + l.xt;
+    const int64_t ldx = (int64_t)np * unit_of(F), ldt = (int64_t)mp * unit_of(F);
+    if constexpr (F == DOUBLE) {
+        for (int k = threadIdx.x; k < 64 * 64; k += 256) {
+            put(x, i0 + k / 64, ldx, j0 + k % 64, tile[k / 64][k % 64]);
+            put(xt, j0 + k / 64, ldt, i0 + k % 64, tile[k % 64][k / 64]);
+        }
+    } else {  // eight values and 16 bytes of a part at a time
+#pragma unroll
+        for (int c = 0; c < 2; c++) {
+            const int k = c * 256 + threadIdx.x, r = k / 8, at = k % 8 * 8;
+            half8 hi, lo, thi, tlo;
+#pragma unroll
+            for (int v = 0; v < 8; v++) {
+                hi[v] = (_Float16)tile[r][at + v], lo[v] = (_Float16)(tile[r][at + v] - (float)hi[v]);
+                thi[v] = (_Float16)tile[at + v][r], tlo[v] = (_Float16)(tile[at + v][r] - (float)thi[v]);
+            }
+            const int in = F == ONE ? at : at / 32 * 64 + at % 32;
+            _Float16 *p = (_Float16*)(x + (i0 + r) * ldx) + j0 * (F == ONE ? 1 : 2) + in, *q = (_Float16*)(xt + (j0 + r) * ldt) + i0 * (F == ONE ? 1 : 2) + in;
+            *(half8*)p = hi;
+            *(half8*)q = thi;
+            if constexpr (F == TWO) *(half8*)(p + 32) = lo, *(half8*)(q + 32) = tlo;
+        }
     }
 }
 
@@ -330,20 +367,66 @@ struct GemmArgs {
     int32_t count, from;  // from: which X^T is read
 };
 
-template <typename T, int MODE, int BT, int WI, int WJ>
-__global__ __launch_bounds__(64 * WI * WJ) void k_ortho_gemm(GemmArgs a) {
+// 16 bytes of each lane from a buffer to LDS: lane l's lie 16 l past `to`.
+__device__ __forceinline__ void load_lds(__amdgpu_buffer_rsrc_t from, uint32_t lane_offset, uint32_t offset, char* to) {
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(from, (__attribute__((address_space(3))) void*)to, 16, lane_offset, offset, 0, 0);
+}
+
+// Consecutive workgroups go to the eight XCDs in turn: give each XCD a run of
+// consecutive tiles, whose operands its L2 then holds.
+__device__ __forceinline__ int xcd_run(int block, int blocks) {
+    const int x = block % 8, q = blocks / 8, r = blocks % 8;
+    return x * q + min(x, r) + block / 8;
+}
+
+// Four consecutive values of a row (col % 4 = 0).
+typedef _Float16 half4 __attribute__((ext_vector_type(4)));
+template <int F> __device__ __forceinline__ float4v get4(const char* p, int64_t row, int64_t ld, int col) {
+    const _Float16* r = (const _Float16*)(p + row * ld) + (F == ONE ? col : col / 32 * 64 + col % 32);
+    float4v v = __builtin_convertvector(*(const half4*)r, float4v);
+    if constexpr (F == TWO) v += __builtin_convertvector(*(const half4*)(r + 32), float4v);
+    return v;
+}
+
+// A wavefront's operands of half a step: N tiles' rows of 32 values, or of 2 x 4 in fp64.
+template <int F, int N> struct Operands {
+    std::conditional_t<F == DOUBLE, double[2], half8> v[N];
+};
+
+// The schedule of a half: READS reads of LDS from its start, a product behind each.
+template <int READS> __device__ __forceinline__ void spread() {
+#pragma unroll
+    for (int r = 0; r < READS; r++) {
+        __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+        __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+    }
+}
+
+// One step's operands in LDS, each of them an object of its own for the compiler:
+// loads on their way to one do not hold up reads of another.
+#define STAGE(name) __shared__ __attribute__((aligned(16))) char name[2 * BT * 128]
+
+// BT x BT tiles of C, WI x WJ wavefronts. The operands' next 128 bytes of every
+// row are on their way to LDS, STAGES - 1 steps ahead, while the products of a
+// step run. Chunk q (16 bytes) of a row r lies at q ^ (r % 8): the rows that a
+// wavefront reads together start in different banks.
+template <typename T, int MODE, int BT, int WI, int WJ, int STAGES>
+__global__ __launch_bounds__(64 * WI * WJ, 2) void k_ortho_gemm(GemmArgs a) {
     constexpr int F = FORMAT<T>, U = unit_of(F), THREADS = 64 * WI * WJ, TI = BT / WI / 16, TJ = BT / WJ / 16;
+    constexpr int LOADS = BT * 8 / THREADS;  // of a thread, for each operand
     using R = Acc<T>;
     using Q = typename Quad<R>::type;
-    __shared__ __attribute__((aligned(16))) char sl[BT * 128], sr[BT * 128];
-    const GemmEntry& e = a.e[entry_of(a.e, a.count, blockIdx.x)];
+    STAGE(s0);
+    STAGE(s1);
+    const int block = xcd_run(blockIdx.x, gridDim.x);
+    const GemmEntry& e = a.e[entry_of(a.e, a.count, block)];
     const int mp = (int)up64(e.m), np = (int)up64(e.n);
     const Layout l = layout_of(mp, np, U);
     const int64_t xt_from = l.xt + a.from * (l.a - l.xt) / 2, xt_to = l.xt + (1 - a.from) * (l.a - l.xt) / 2;
     const int mt = (mp + BT - 1) / BT, nt = (np + BT - 1) / BT;
     const int tiles = MODE <= POLY ? mt * (mt + 1) / 2 : mt * nt;
-    const int t = (blockIdx.x - e.first) % tiles;
-    const int64_t b = (blockIdx.x - e.first) / tiles;
+    const int t = (block - e.first) % tiles;
+    const int64_t b = (block - e.first) / tiles;
     char* w = e.work + b * l.size;
     int ti, tj;
     if (MODE <= POLY) {
@@ -351,106 +434,291 @@ __global__ __launch_bounds__(64 * WI * WJ) void k_ortho_gemm(GemmArgs a) {
         while (ti * (ti + 1) / 2 > t) ti--;
         while ((ti + 1) * (ti + 2) / 2 <= t) ti++;
         tj = t - ti * (ti + 1) / 2;
-    } else {
-        ti = t % mt, tj = t / mt;
+    } else {  // bands of eight tiles down, then across
+        const int band = t / (8 * nt), high = min(8, mt - band * 8), at = t - band * 8 * nt;
+        ti = band * 8 + at % high, tj = at / high;
     }
-    const char* left = w + (MODE == GRAM ? l.x : MODE == POLY ? l.a : l.b);
-    const char* right = w + (MODE == GRAM ? l.x : MODE == POLY ? l.a : xt_from);
     const int left_rows = mp, right_rows = MODE >= APPLY ? np : mp;
-    const int64_t ld = (int64_t)(MODE == GRAM ? np : mp) * U;  // bytes of an operand's row
+    const int ld = (MODE == GRAM ? np : mp) * U;  // bytes of an operand's row
+    const char* left = w + (MODE == GRAM ? l.x : MODE == POLY ? l.a : l.b) + (int64_t)ti * BT * ld;
+    const char* right = w + (MODE == GRAM ? l.x : MODE == POLY ? l.a : xt_from) + (int64_t)tj * BT * ld;
+    const int li = min(BT, left_rows - ti * BT), ri = min(BT, right_rows - tj * BT);
+    const auto lbuf = __builtin_amdgcn_make_buffer_rsrc((void*)left, 0, li * ld, 0x00027000);
+    const auto rbuf = __builtin_amdgcn_make_buffer_rsrc((void*)right, 0, ri * ld, 0x00027000);
 
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wi = wave / WJ, wj = wave % WJ;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wi = wave / WJ, wj = wave % WJ;
     const int row = lane % 16, part = lane / 16;
-    Q acc[TI][TJ] = {};
-    for (int64_t k = 0; k < ld; k += 128) {
-        __syncthreads();
+    uint32_t lat[LOADS], rat[LOADS];
 #pragma unroll
-        for (int c = 0; c < BT * 8 / THREADS; c++) {
-            const int id = c * THREADS + threadIdx.x, r = id / 8, q = id % 8;
-            const int li = min(ti * BT + r, left_rows - 1), ri = min(tj * BT + r, right_rows - 1);
-            // chunk q of row r lies at q ^ (r % 8): rows of a column of chunks in different banks
-            *(float4v*)(sl + r * 128 + ((q ^ (r & 7)) * 16)) = *(const float4v*)(left + li * ld + k + q * 16);
-            *(float4v*)(sr + r * 128 + ((q ^ (r & 7)) * 16)) = *(const float4v*)(right + ri * ld + k + q * 16);
-        }
-        __syncthreads();
+    for (int c = 0; c < LOADS; c++) {
+        const int r = (c * THREADS + threadIdx.x) / 8, q = threadIdx.x % 8;
+        lat[c] = (uint32_t)(min(r, li - 1) * ld + ((q ^ (r & 7)) * 16));
+        rat[c] = (uint32_t)(min(r, ri - 1) * ld + ((q ^ (r & 7)) * 16));
+    }
+    auto load = [&](char* s, int k) {
+#pragma unroll
+        for (int c = 0; c < LOADS; c++) load_lds(lbuf, lat[c], k, s + (c * THREADS + wave * 64) * 16);
+#pragma unroll
+        for (int c = 0; c < LOADS; c++) load_lds(rbuf, rat[c], k, s + BT * 128 + (c * THREADS + wave * 64) * 16);
+    };
+    Q acc[TI][TJ] = {};
+    // A step has two halves, of 64 bytes of every row. While the products of one
+    // run, the operands of the next come from LDS: the second half's at first;
+    // then, once the next step's loads have arrived everywhere and nobody reads
+    // this step's any more, its first half's, and the loads that take this
+    // step's place in LDS are sent off. Nothing waits for LDS or HBM but for what
+    // a half's products do not hide.
+    Operands<F, TI> p, p1;
+    Operands<F, TJ> q, q1;
+    const int at = F == DOUBLE ? row * 128 : row * 128 + ((part ^ (row & 7)) * 16);
+    auto read = [&](const char* s, int half, Operands<F, TI>& pp, Operands<F, TJ>& qq) {
+        const char *sl = s + wi * TI * 2048, *sr = s + BT * 128 + wj * TJ * 2048;
         if constexpr (F == DOUBLE) {
 #pragma unroll
-            for (int s = 0; s < 4; s++) {
-                double p[TI], q[TJ];
-                const int at = s * 2 + part / 2, in = part % 2 * 8;  // value 4 s + part of the row
+            for (int k = 0; k < 2; k++) {  // values 8 half + 4 k + part of the row
+                const int c = at + (((half * 4 + k * 2 + part / 2) ^ (row & 7)) * 16) + part % 2 * 8;
 #pragma unroll
-                for (int i = 0; i < TI; i++) {
-                    const int r = wi * TI * 16 + i * 16 + row;
-                    p[i] = *(const double*)(sl + r * 128 + ((at ^ (r & 7)) * 16) + in);
-                }
+                for (int i = 0; i < TI; i++) pp.v[i][k] = *(const double*)(sl + c + i * 2048);
 #pragma unroll
-                for (int j = 0; j < TJ; j++) {
-                    const int r = wj * TJ * 16 + j * 16 + row;
-                    q[j] = *(const double*)(sr + r * 128 + ((at ^ (r & 7)) * 16) + in);
-                }
-#pragma unroll
-                for (int i = 0; i < TI; i++)
-#pragma unroll
-                    for (int j = 0; j < TJ; j++) acc[i][j] = mma4(q[j], p[i], acc[i][j]);
+                for (int j = 0; j < TJ; j++) qq.v[j][k] = *(const double*)(sr + c + j * 2048);
             }
         } else {
-            half8 p[TI][2], q[TJ][2];
+            const int c = half ? at ^ 64 : at;
 #pragma unroll
-            for (int s = 0; s < 2; s++) {
-                const int at = s * 4 + part;
+            for (int i = 0; i < TI; i++) pp.v[i] = *(const half8*)(sl + c + i * 2048);
 #pragma unroll
-                for (int i = 0; i < TI; i++) {
-                    const int r = wi * TI * 16 + i * 16 + row;
-                    p[i][s] = *(const half8*)(sl + r * 128 + ((at ^ (r & 7)) * 16));
+            for (int j = 0; j < TJ; j++) qq.v[j] = *(const half8*)(sr + c + j * 2048);
+        }
+    };
+    auto product = [&](const Operands<F, TI>& pp, const Operands<F, TJ>& qq) {
+#pragma unroll
+        for (int i = 0; i < TI; i++)
+#pragma unroll
+            for (int j = 0; j < TJ; j++)
+                if constexpr (F == DOUBLE) {
+                    acc[i][j] = mma4(qq.v[j][0], pp.v[i][0], acc[i][j]);
+                    acc[i][j] = mma4(qq.v[j][1], pp.v[i][1], acc[i][j]);
+                } else {
+                    acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(qq.v[j], pp.v[i], acc[i][j], 0, 0, 0);
                 }
-#pragma unroll
-                for (int j = 0; j < TJ; j++) {
-                    const int r = wj * TJ * 16 + j * 16 + row;
-                    q[j][s] = *(const half8*)(sr + r * 128 + ((at ^ (r & 7)) * 16));
-                }
-            }
-#pragma unroll
-            for (int i = 0; i < TI; i++)
-#pragma unroll
-                for (int j = 0; j < TJ; j++) {
-                    if constexpr (F == ONE) {
-                        acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(q[j][0], p[i][0], acc[i][j], 0, 0, 0);
-                        acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(q[j][1], p[i][1], acc[i][j], 0, 0, 0);
-                    } else {
-                        acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(q[j][1], p[i][0], acc[i][j], 0, 0, 0);
-                        acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(q[j][0], p[i][1], acc[i][j], 0, 0, 0);
-                        acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(q[j][0], p[i][0], acc[i][j], 0, 0, 0);
-                    }
-                }
+    };
+    // All wavefronts' loads have arrived but for those of the later steps under
+    // way, and all their reads too. Past the last step its loads are repeated, so
+    // that the number of open loads is always the same.
+    auto arrived = [](auto open) {
+        constexpr int n = decltype(open)::value;
+        asm volatile("" ::: "memory");
+        __builtin_amdgcn_s_waitcnt((n & 15) | 7 << 4 | (n >> 4) << 14);  // vmcnt(n) lgkmcnt(0)
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+    };
+    auto step = [&](char* now, char* next, int k) {
+        read(now, 1, p1, q1);
+        product(p, q);
+        spread<TI + TJ>();
+        __builtin_amdgcn_sched_barrier(0);
+        arrived(std::integral_constant<int, 2 * LOADS*(STAGES - 2)>{});
+        load(now, min(k + 128 * STAGES, ld - 128));
+        __builtin_amdgcn_sched_barrier(0);
+        if constexpr (F == TWO) {  // hi lo, then lo hi
+            product(p, q1);
+            __builtin_amdgcn_sched_barrier(0);
+            product(p1, q);
+            read(next, 0, p, q);
+            spread<TI>();
+        } else {
+            read(next, 0, p, q);
+            product(p1, q1);
+            spread<TI + TJ>();
+        }
+        __builtin_amdgcn_sched_barrier(0);
+    };
+    load(s0, 0);
+    load(s1, min(128, ld - 128));
+    if constexpr (STAGES == 2) {
+        arrived(std::integral_constant<int, 2 * LOADS>{});
+        read(s0, 0, p, q);
+        for (int k = 0;; k += 256) {
+            step(s0, s1, k);
+            if (k + 128 >= ld) break;
+            step(s1, s0, k + 128);
+            if (k + 256 >= ld) break;
+        }
+    } else if constexpr (STAGES == 3) {
+        STAGE(s2);
+        load(s2, min(256, ld - 128));
+        arrived(std::integral_constant<int, 4 * LOADS>{});
+        read(s0, 0, p, q);
+        for (int k = 0;; k += 384) {
+            step(s0, s1, k);
+            if (k + 128 >= ld) break;
+            step(s1, s2, k + 128);
+            if (k + 256 >= ld) break;
+            step(s2, s0, k + 256);
+            if (k + 384 >= ld) break;
+        }
+    } else {
+        STAGE(s2);
+        STAGE(s3);
+        load(s2, min(256, ld - 128));
+        load(s3, min(384, ld - 128));
+        arrived(std::integral_constant<int, 6 * LOADS>{});
+        read(s0, 0, p, q);
+        for (int k = 0;; k += 512) {
+            step(s0, s1, k);
+            if (k + 128 >= ld) break;
+            step(s1, s2, k + 128);
+            if (k + 256 >= ld) break;
+            step(s2, s3, k + 256);
+            if (k + 384 >= ld) break;
+            step(s3, s0, k + 384);
+            if (k + 512 >= ld) break;
         }
     }
+    __builtin_amdgcn_s_waitcnt(0);
     const int64_t lda = (int64_t)mp * U, ldx = (int64_t)np * U;
+    const int i0 = ti * BT + wi * TI * 16 + row, j0 = tj * BT + wj * TJ * 16;
+    if constexpr (F == DOUBLE) {
 #pragma unroll
-    for (int i = 0; i < TI; i++)
+        for (int i = 0; i < TI; i++)
 #pragma unroll
-        for (int j = 0; j < TJ; j++)
+            for (int j = 0; j < TJ; j++)
 #pragma unroll
-            for (int r = 0; r < 4; r++) {
-                const int gi = ti * BT + (wi * TI + i) * 16 + row, gj = tj * BT + (wj * TJ + j) * 16 + mma_row<R>(lane, r);
-                if (gi >= left_rows || gj >= right_rows) continue;
-                R v = (R)a.f1 * acc[i][j][r];
-                if constexpr (MODE == GRAM) {
-                    put<F>(w + l.a, gi, lda, gj, v);
-                    if (ti != tj) put<F>(w + l.a, gj, lda, gi, v);
-                } else if constexpr (MODE == POLY) {
-                    v += (R)a.f0 * get<F>(w + l.a, gi, lda, gj);
-                    put<F>(w + l.b, gi, lda, gj, v);
-                    if (ti != tj) put<F>(w + l.b, gj, lda, gi, v);
-                } else {
-                    v += (R)a.f0 * get<F>(w + l.x, gi, ldx, gj);
-                    if constexpr (MODE == APPLY) {
-                        put<F>(w + l.x, gi, ldx, gj, v);
-                        put<F>(w + xt_to, gj, lda, gi, v);
+                for (int r = 0; r < 4; r++) {
+                    const int gi = i0 + i * 16, gj = j0 + j * 16 + mma_row<R>(lane, r);
+                    if (gi >= left_rows || gj >= right_rows) continue;
+                    double v = a.f1 * acc[i][j][r];
+                    if constexpr (MODE == POLY) v += a.f0 * get(w + l.a, gi, lda, gj);
+                    if constexpr (MODE >= APPLY) v += a.f0 * get(w + l.x, gi, ldx, gj);
+                    if constexpr (MODE <= POLY) {
+                        put(w + (MODE == GRAM ? l.a : l.b), gi, lda, gj, v);
+                        if (ti != tj) put(w + (MODE == GRAM ? l.a : l.b), gj, lda, gi, v);
+                    } else if constexpr (MODE == APPLY) {
+                        put(w + l.x, gi, ldx, gj, v);
+                        put(w + xt_to, gj, lda, gi, v);
                     } else if (gi < e.m && gj < e.n) {
                         write_out<T>(e.t, a.r, b, gi, gj, v);
                     }
                 }
+    } else {
+        // A wavefront's tiles from the top: what a row of them is added to is read
+        // while the row before is written, at places that are there for every lane.
+        const bool by_row = e.t.oj == 1 && e.n >= 4;  // LAST: four columns at a time to the caller
+        struct Behind {
+            float4v add[TJ];
+            Four<T> old[TJ];
+        };
+        auto fetch = [&](int i) {
+            Behind f;
+            const int gi = min(i0 + i * 16, left_rows - 1);
+#pragma unroll
+            for (int j = 0; j < TJ; j++) {
+                const int gj = min(j0 + j * 16, right_rows - 16) + 4 * part;
+                if constexpr (MODE == POLY) f.add[j] = get4<F>(w + l.a, gi, lda, gj);
+                if constexpr (MODE >= APPLY) f.add[j] = get4<F>(w + l.x, gi, ldx, gj);
+                if constexpr (MODE == LAST)
+                    if (a.r.muon) {
+                        if (by_row) {
+                            f.old[j] = *four_at<T>(e.t, b, min(gi, e.m - 1), min(gj, e.n - 4));
+                        } else {
+#pragma unroll
+                            for (int r = 0; r < 4; r++) f.old[j].v[r] = *out_at<T>(e.t, b, min(gi, e.m - 1), min(gj + r, e.n - 1));
+                        }
+                    }
             }
+            return f;
+        };
+        Behind now = fetch(0);
+        if constexpr (MODE != LAST) {
+            // the wavefront's own part of the LDS, to store whole rows of its tiles
+            asm volatile("" ::: "memory");
+            __builtin_amdgcn_s_barrier();
+            asm volatile("" ::: "memory");
+            _Float16* own = (_Float16*)(s0 + wave * (2 * BT * 128 / (WI * WJ)));
+            constexpr int PLANES = F == TWO ? 2 : 1;
+            constexpr int WIDE = TJ * 16 + 8, HIGH = TI * 16 + 8;  // pitches, off a multiple of the banks
+            static_assert(16 * HIGH * 2 <= 2 * BT * 128 / (WI * WJ) && 16 * WIDE * 2 * PLANES <= 2 * BT * 128 / (WI * WJ), "LDS");
+            char* to = w + (MODE == GRAM ? l.a : MODE == POLY ? l.b : l.x);
+            const int64_t to_ld = MODE == APPLY ? ldx : lda;
+            auto in_row = [](int64_t c, int plane) { return F == ONE ? c : c / 32 * 64 + plane * 32 + c % 32; };
+#pragma unroll
+            for (int i = 0; i < TI; i++) {
+                const Behind next = fetch(min(i + 1, TI - 1));
+#pragma unroll
+                for (int j = 0; j < TJ; j++) {
+                    float4v v = acc[i][j] * (float)a.f1;
+                    if constexpr (MODE != GRAM) v += now.add[j] * (float)a.f0;
+                    acc[i][j] = v;
+                    const half4 hi = __builtin_convertvector(v, half4);
+                    *(half4*)(own + row * WIDE + j * 16 + 4 * part) = hi;
+                    if constexpr (F == TWO)
+                        *(half4*)(own + (16 + row) * WIDE + j * 16 + 4 * part) =
+                            __builtin_convertvector(v - __builtin_convertvector(hi, float4v), half4);
+                }
+                __builtin_amdgcn_wave_barrier();
+#pragma unroll
+                for (int c = 0; c < (16 * TJ * 2 * PLANES + 63) / 64; c++) {
+                    const int id = c * 64 + lane, col = id % (TJ * 2) * 8, r = id / (TJ * 2) % 16, plane = id / (TJ * 32);
+                    const int gi = ti * BT + (wi * TI + i) * 16 + r, gj = j0 + col;
+                    if (id < 16 * TJ * 2 * PLANES && gi < left_rows && gj < right_rows)
+                        *(half8*)((_Float16*)(to + gi * to_ld) + in_row(gj, plane)) = *(const half8*)(own + (plane * 16 + r) * WIDE + col);
+                }
+                __builtin_amdgcn_wave_barrier();
+                now = next;
+            }
+            if (MODE == APPLY || ti != tj) {  // the same, transposed
+                to = w + (MODE == GRAM ? l.a : MODE == POLY ? l.b : xt_to);
+#pragma unroll
+                for (int j = 0; j < TJ; j++)
+#pragma unroll
+                    for (int plane = 0; plane < PLANES; plane++) {
+#pragma unroll
+                        for (int i = 0; i < TI; i++)
+#pragma unroll
+                            for (int r = 0; r < 4; r++) {
+                                const _Float16 hi = (_Float16)acc[i][j][r];
+                                own[(4 * part + r) * HIGH + i * 16 + row] = plane ? (_Float16)(acc[i][j][r] - (float)hi) : hi;
+                            }
+                        __builtin_amdgcn_wave_barrier();
+#pragma unroll
+                        for (int c = 0; c < (16 * TI * 2 + 63) / 64; c++) {
+                            const int id = c * 64 + lane, col = id % (TI * 2) * 8, r = id / (TI * 2);
+                            const int gj = j0 + j * 16 + r, gi = ti * BT + wi * TI * 16 + col;
+                            if (id < 16 * TI * 2 && gj < right_rows && gi < left_rows)
+                                *(half8*)((_Float16*)(to + gj * lda) + in_row(gi, plane)) = *(const half8*)(own + r * HIGH + col);
+                        }
+                        __builtin_amdgcn_wave_barrier();
+                    }
+            }
+        } else {
+            auto value = [&](float v, T was) { return down<T>(a.r.muon ? (float)a.r.keep * up(was) - (float)e.t.step * v : v); };
+#pragma unroll
+            for (int i = 0; i < TI; i++) {
+                const Behind next = fetch(min(i + 1, TI - 1));
+                const int gi = i0 + i * 16;
+#pragma unroll
+                for (int j = 0; j < TJ; j++) {
+                    const int gj = j0 + j * 16 + 4 * part;
+                    const float4v v = acc[i][j] * (float)a.f1 + now.add[j] * (float)a.f0;
+                    if (by_row && gi < e.m && gj + 4 <= e.n) {
+                        Four<T> f;
+#pragma unroll
+                        for (int r = 0; r < 4; r++) f.v[r] = value(v[r], now.old[j].v[r]);
+                        *four_at<T>(e.t, b, gi, gj) = f;
+                    } else if (gi < e.m) {
+#pragma unroll
+                        for (int r = 0; r < 4; r++)
+                            if (gj + r < e.n) {
+                                // where columns go four at a time, `old` holds others at the edge
+                                T* p = out_at<T>(e.t, b, gi, gj + r);
+                                *p = value(v[r], by_row && a.r.muon ? *p : now.old[j].v[r]);
+                            }
+                    }
+                }
+                now = next;
+            }
+        }
+    }
 }
 
 // ---------------------------------------------------------------------------
@@ -489,8 +757,9 @@ bool is_small(int type, const Shape& s) {
     return s.m <= SMALL_M && small_lds(s.m, s.n, type == E_F64 ? 8 : 4) <= SMALL_LDS;
 }
 
+// Workgroups of the norm: each takes at least 4096 elements, and whole lines.
 int chunks_of(const Shape& s) {
-    return (int)std::min<int64_t>(std::min(s.m, 256), std::max<int64_t>(1, (int64_t)s.m * s.n / 8192));
+    return (int)std::min<int64_t>(std::min(s.m, 1024), std::max<int64_t>(1, (int64_t)s.m * s.n / 4096));
 }
 
 int format_of(int type) { return type == E_BF16 ? ONE : type == E_F64 ? DOUBLE : TWO; }
@@ -548,27 +817,75 @@ template <typename T, int MODE, int BT> hipError_t gemm(GemmArgs a, const int64_
         blocks += batch[k] * (MODE <= POLY ? mt * (mt + 1) / 2 : mt * nt);
     }
     if (blocks > INT32_MAX) return hipErrorInvalidValue;
-    k_ortho_gemm<T, MODE, BT, 2, 2><<<(unsigned)blocks, 256, 0, s>>>(a);
+    constexpr int WJ = BT >= 192 ? 4 : 2, STAGES = BT == 64 ? 4 : BT == 192 ? 3 : 2;
+    k_ortho_gemm<T, MODE, BT, 2, WJ, STAGES><<<(unsigned)blocks, 128 * WJ, 0, s>>>(a);
     return hipGetLastError();
 }
 
-template <typename T, int BT>
-hipError_t run_steps(const OrthoCall& c, GemmArgs g, const int64_t* batch, double sx, double sa, double sb, hipStream_t s) {
+// What a launch with tiles of a size costs, in us, from measured kernels: a
+// main-loop step of a workgroup that has its compute unit for itself, of one
+// that shares it (two of the smaller tiles fit one), and what a tile costs
+// besides its steps. One and two parts; fp64 has one tile size.
+constexpr int TILES[] = {64, 128, 192, 256};
+struct TileCost {
+    double alone, shared, rest;
+};
+constexpr TileCost COST[2][4] = {{{0.20, 0.40, 2}, {0.42, 0.78, 8}, {0.95, 0.95, 12}, {1.1, 1.1, 20}},
+                                 {{0.25, 0.45, 2}, {0.58, 1.10, 8}, {1.00, 1.00, 12}, {1.6, 1.6, 20}}};
+constexpr int UNITS = 256;  // compute units
+
+double launch_cost(int format, int mode, int which, const GemmArgs& a, const int64_t* batch) {
+    const TileCost& c = COST[format == TWO][which];
+    const int64_t bt = TILES[which], slots = which < 2 ? 2 * UNITS : UNITS;
+    double alone = 0, shared = 0, longest = 0;  // sums over tiles, and the longest tile
+    int64_t tiles = 0;
+    for (int k = 0; k < a.count; k++) {
+        const int64_t mp = up64(a.e[k].m), np = up64(a.e[k].n), mt = (mp + bt - 1) / bt, nt = (np + bt - 1) / bt;
+        const int64_t n = batch[k] * (mode <= POLY ? mt * (mt + 1) / 2 : mt * nt);
+        const double steps = (double)(mode == GRAM ? np : mp) * unit_of(format) / 128;
+        tiles += n;
+        alone += n * (steps * c.alone + c.rest);
+        shared += n * (steps * c.shared + c.rest);
+        longest = std::max(longest, steps * c.alone + c.rest);
+    }
+    if (!tiles) return 0;
+    const int64_t rounds = tiles / slots, rest = tiles % slots;
+    return std::max(longest, rounds * shared / tiles + (rest ? (rest <= UNITS ? alone : shared) / tiles : 0));
+}
+
+template <typename T, int MODE> hipError_t gemm(const GemmArgs& a, const int64_t* batch, hipStream_t s) {
+    if constexpr (FORMAT<T> == DOUBLE) {
+        return gemm<T, MODE, 64>(a, batch, s);
+    } else {
+        int best = 0;
+        double cost[4];
+        for (int k = 0; k < 4; k++)
+            if ((cost[k] = launch_cost(FORMAT<T>, MODE, k, a, batch)) < cost[best]) best = k;
+        switch (best) {
+            case 0: return gemm<T, MODE, 64>(a, batch, s);
+            case 1: return gemm<T, MODE, 128>(a, batch, s);
+            case 2: return gemm<T, MODE, 192>(a, batch, s);
+            default: return gemm<T, MODE, 256>(a, batch, s);
+        }
+    }
+}
+
+template <typename T> hipError_t run_steps(const OrthoCall& c, GemmArgs g, const int64_t* batch, double sx, double sa, double sb, hipStream_t s) {
     hipError_t e = hipSuccess;
     for (int step = 0; step < c.steps && e == hipSuccess; step++) {
         g.from = step & 1;
         g.f0 = 0, g.f1 = sa / (sx * sx);
-        e = gemm<T, GRAM, BT>(g, batch, s);
+        e = gemm<T, GRAM>(g, batch, s);
         if (e != hipSuccess) break;
         g.f0 = c.b * sb / sa, g.f1 = c.c * sb / (sa * sa);
-        e = gemm<T, POLY, BT>(g, batch, s);
+        e = gemm<T, POLY>(g, batch, s);
         if (e != hipSuccess) break;
         if (step + 1 < c.steps) {
             g.f0 = c.a, g.f1 = 1 / sb;
-            e = gemm<T, APPLY, BT>(g, batch, s);
+            e = gemm<T, APPLY>(g, batch, s);
         } else {
             g.f0 = c.a / sx, g.f1 = 1 / (sb * sx);
-            e = gemm<T, LAST, BT>(g, batch, s);
+            e = gemm<T, LAST>(g, batch, s);
         }
     }
     return e;
@@ -587,7 +904,7 @@ template <typename T> hipError_t run_large(const OrthoCall& c, const Rule& rule,
     for (int at = 0; at < c.count;) {
         PackArgs p{};
         GemmArgs g{};
-        int64_t batch[ENTRIES], norm_blocks = 0, tiles128 = 0;
+        int64_t batch[ENTRIES], norm_blocks = 0;
         p.r = g.r = rule, p.scale = sx;
         for (; at < c.count && p.count < ENTRIES; at++) {
             const ql_matrix& q = c.mats[at];
@@ -602,7 +919,6 @@ template <typename T> hipError_t run_large(const OrthoCall& c, const Rule& rule,
             norm_blocks += q.batch * e.chunks;
             g.e[p.count] = {e.work, target_of(q, c), sh.m, sh.n, 0};
             batch[p.count++] = q.batch;
-            tiles128 += q.batch * ((sh.m + 127) / 128) * ((sh.n + 127) / 128);
         }
         if (!p.count) continue;
         g.count = p.count;
@@ -617,9 +933,7 @@ template <typename T> hipError_t run_large(const OrthoCall& c, const Rule& rule,
         if (pack_blocks > INT32_MAX) return hipErrorInvalidValue;
         k_ortho_pack<T><<<(unsigned)pack_blocks, 256, 0, s>>>(p);
         if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
-        hipError_t e;
-        if constexpr (FORMAT<T> == DOUBLE) e = run_steps<T, 64>(c, g, batch, sx, sa, sb, s);
-        else e = tiles128 >= 256 ? run_steps<T, 128>(c, g, batch, sx, sa, sb, s) : run_steps<T, 64>(c, g, batch, sx, sa, sb, s);
+        const hipError_t e = run_steps<T>(c, g, batch, sx, sa, sb, s);
         if (e != hipSuccess) return e;
     }
     return hipSuccess;
