@@ -96,9 +96,6 @@ template <typename E> __device__ __forceinline__ int entry_of(const E* e, int co
     return k;
 }
 
-__device__ __forceinline__ float4v mma4(float a, float b, float4v c) {
-    return __builtin_amdgcn_mfma_f32_16x16x4f32(a, b, c, 0, 0, 0);
-}
 __device__ __forceinline__ double4v mma4(double a, double b, double4v c) {
     return __builtin_amdgcn_mfma_f64_16x16x4f64(a, b, c, 0, 0, 0);
 }
@@ -112,7 +109,7 @@ template <typename R> __device__ __forceinline__ int mma_row(int lane, int r) {
 }
 
 // ---------------------------------------------------------------------------
-// Small matrices: one workgroup each, X, A and B in its LDS, products of 16x16x4.
+// Small matrices in fp64: one workgroup each, X, A and B in its LDS, products of 16x16x4.
 struct SmallEntry {
     Source s;
     Target t;
@@ -213,6 +210,292 @@ template <typename T> __global__ __launch_bounds__(SMALL_THREADS) void k_ortho_s
     for (int k = threadIdx.x; k < m * n; k += SMALL_THREADS) {
         const int i = out_by_row ? k / n : k % m, j = out_by_row ? k % n : k / m;
         write_out<T>(e.t, a.r, b, i, j, X[i * ldx + j]);
+    }
+}
+
+// Small matrices of the other types: as above with the fp16 products of the
+// large ones, X, its transpose and A (then B in its place) in LDS in two parts.
+// Each of the 16 wavefronts (4 for little work) takes a 16x16 tile of A and of
+// B, and 16 columns of X, which nobody else reads or writes until the step's
+// end. 16 matrices of 64x256 take 14 us, against 95 us with the fp32 products
+// above (16x16x4: an eighth of the rate even after three products).
+struct SmallScale {
+    float sx, sa, sb;
+};
+// A wavefront's 16x16 tile, K in steps of 32: rows p and q of two-part arrays,
+// whose second part lies `behind` values after the first.
+__device__ __forceinline__ float4v two_part(const _Float16* p, const _Float16* q, int behind, int depth) {
+    float4v acc = {}, cross0 = {}, cross1 = {};  // three chains of products
+    half8 ph = *(const half8*)p, pl = *(const half8*)(p + behind), qh = *(const half8*)q, ql = *(const half8*)(q + behind);
+    for (int k = 0; k < depth; k += 32) {
+        const int next = min(k + 32, depth - 32);  // read while these products run
+        const half8 nph = *(const half8*)(p + next), npl = *(const half8*)(p + behind + next);
+        const half8 nqh = *(const half8*)(q + next), nql = *(const half8*)(q + behind + next);
+        cross0 = __builtin_amdgcn_mfma_f32_16x16x32_f16(pl, qh, cross0, 0, 0, 0);
+        cross1 = __builtin_amdgcn_mfma_f32_16x16x32_f16(ph, ql, cross1, 0, 0, 0);
+        acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(ph, qh, acc, 0, 0, 0);
+        ph = nph, pl = npl, qh = nqh, ql = nql;
+    }
+    return acc + (cross0 + cross1);
+}
+typedef _Float16 half4 __attribute__((ext_vector_type(4)));
+typedef uint32_t word2 __attribute__((ext_vector_type(2)));
+__device__ __forceinline__ half4 high(float4v v) { return __builtin_convertvector(v, half4); }
+__device__ __forceinline__ half4 low(float4v v, half4 hi) {
+#pragma unroll
+    for (int r = 0; r < 4; r++) v[r] = __builtin_fmaf((float)hi[r], -1.0f, v[r]);  // exact, in one instruction
+    return __builtin_convertvector(v, half4);
+}
+
+// Lanes 4 k + i of a wavefront hold row i of 4x4 values: afterwards column i.
+__device__ __forceinline__ half4 turn4(half4 v) {
+    const word2 x = __builtin_bit_cast(word2, v);
+    const bool odd = threadIdx.x & 1, upper = threadIdx.x & 2;
+    auto swap1 = [](uint32_t w) { return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)w, 0xB1, 0xF, 0xF, false); };
+    auto swap2 = [](uint32_t w) { return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)w, 0x4E, 0xF, 0xF, false); };
+    // pairs of lanes: even (a0 b0)(a2 b2), odd (a1 b1)(a3 b3)
+    const uint32_t select = odd ? 0x03020706 : 0x05040100;
+    const uint32_t y0 = __builtin_amdgcn_perm(swap1(x.x), x.x, select), y1 = __builtin_amdgcn_perm(swap1(x.y), x.y, select);
+    const uint32_t z = swap2(upper ? y0 : y1);
+    return __builtin_bit_cast(half4, upper ? word2{z, y1} : word2{y0, z});
+}
+
+__device__ __forceinline__ float4v get_two4(const _Float16* p, int behind) {
+    return __builtin_convertvector(*(const half4*)p, float4v) + __builtin_convertvector(*(const half4*)(p + behind), float4v);
+}
+// v + f times four values in two parts.
+__device__ __forceinline__ float4v add_two4(float4v v, const _Float16* p, int behind, float f) {
+    const half4 hi = *(const half4*)p, lo = *(const half4*)(p + behind);
+#pragma unroll
+    for (int r = 0; r < 4; r++) v[r] = __builtin_fmaf((float)hi[r], f, __builtin_fmaf((float)lo[r], f, v[r]));
+    return v;
+}
+// A lane's four columns j .. of row i: to rows of pitch p, and to the transpose's rows of pitch q.
+__device__ __forceinline__ void put_two4(_Float16* p, int behind, float4v v) {
+    const half4 hi = high(v);
+    *(half4*)p = hi;
+    *(half4*)(p + behind) = low(v, hi);
+}
+__device__ __forceinline__ void put_turned(_Float16* p, int pitch, int behind, int i, int j, float4v v) {
+    const half4 hi = high(v);
+    _Float16* q = p + (j + (i & 3)) * pitch + (i & ~3);
+    *(half4*)q = turn4(hi);
+    *(half4*)(q + behind) = turn4(low(v, hi));
+}
+
+__host__ __device__ constexpr int up32(int v) { return (v + 31) / 32 * 32; }
+constexpr int PITCH = 8;  // values behind a row, so that 16 rows start in different banks
+constexpr int BATCH = 4;  // groups of four loads of a thread under way together
+// The first `count` of four elements a stride apart.
+template <typename T> __device__ __forceinline__ float4v load_four(const T* p, int64_t stride, int count) {
+    float4v v = {};
+    if (stride == 1 && count == 4) {
+        const Four<T> f = *(const Four<T>*)p;
+#pragma unroll
+        for (int r = 0; r < 4; r++) v[r] = up(f.v[r]);
+    } else {
+#pragma unroll
+        for (int r = 0; r < 4; r++)
+            if (r < count) v[r] = up(p[r * stride]);
+    }
+    return v;
+}
+template <typename T> __device__ __forceinline__ void store_four(T* p, int64_t stride, int count, float4v v) {
+    if (stride == 1 && count == 4) {
+        Four<T> f;
+#pragma unroll
+        for (int r = 0; r < 4; r++) f.v[r] = down<T>(v[r]);
+        *(Four<T>*)p = f;
+    } else {
+#pragma unroll
+        for (int r = 0; r < 4; r++)
+            if (r < count) p[r * stride] = down<T>(v[r]);
+    }
+}
+constexpr int TINY_LDS = 160 * 1024 - 1024 / 64 * 8;
+size_t tiny_lds(int m, int n) {
+    const size_t mp = up32(m), np = up32(n);
+    return 4 * (mp * (np + PITCH) + np * (mp + PITCH) + mp * (mp + PITCH));
+}
+
+template <typename T, int THREADS> __global__ __launch_bounds__(THREADS) void k_ortho_tiny(SmallArgs a, SmallScale sc) {
+    extern __shared__ double lds_tiny[];
+    __shared__ double norm_part[THREADS / 64];
+    const SmallEntry& e = a.e[entry_of(a.e, a.count, blockIdx.x)];
+    const int64_t b = blockIdx.x - e.first;
+    const int m = e.m, n = e.n, mp = up32(m), np = up32(n), px = np + PITCH, pt = mp + PITCH;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = THREADS / 64, row = lane % 16, part = lane / 16;
+    _Float16 *X = (_Float16*)lds_tiny, *XT = X + 2 * mp * px, *A = XT + 2 * np * pt;
+    const int xlow = mp * px, tlow = np * pt, alow = mp * pt;
+
+    // This thread's groups of four elements in turn, along an array's lines: rows
+    // or columns, whichever lie in the order of its addresses.
+    struct Walk {
+        int line, at, lines, step, groups;
+        __device__ __forceinline__ Walk(int groups_) : groups(groups_) {
+            line = threadIdx.x / groups, at = threadIdx.x % groups, lines = THREADS / groups, step = THREADS % groups;
+        }
+        __device__ __forceinline__ void next() {
+            line += lines, at += step;
+            if (at >= groups) at -= groups, line++;
+        }
+    };
+    const bool by_row = e.s.gj == 1 || e.s.gi != 1, out_by_row = e.t.oj == 1 || e.t.oi != 1;
+    // U waits for its norm where the second of X and X^T to be written will be
+    _Float16 *first = by_row ? X : XT, *second = by_row ? XT : X;
+    const int flow = by_row ? xlow : tlow, slow = by_row ? tlow : xlow, pf = by_row ? px : pt, ps = by_row ? pt : px;
+    const int lines = by_row ? m : n, wide = by_row ? n : m, groups = (wide + 3) / 4, total = lines * groups;
+    float4v* stage = (float4v*)second;
+    double sq = 0;
+    {
+        const T* grad = (const T*)e.s.grad + b * e.s.gb;
+        float* momentum = (float*)e.s.momentum + b * e.s.mb;
+        const int64_t gl = by_row ? e.s.gi : e.s.gj, gs = by_row ? e.s.gj : e.s.gi;
+        const int64_t ml = by_row ? e.s.mi : e.s.mj, ms = by_row ? e.s.mj : e.s.mi;
+        Walk w(groups);
+        for (int k0 = threadIdx.x; k0 < total; k0 += BATCH * THREADS) {
+            float4v u[BATCH], mom[BATCH];
+            float* at[BATCH];
+            int count[BATCH];
+#pragma unroll
+            for (int c = 0; c < BATCH; c++, w.next()) {
+                count[c] = k0 + c * THREADS < total ? min(4, wide - 4 * w.at) : 0;
+                u[c] = load_four<T>(grad + w.line * gl + 4 * w.at * gs, gs, count[c]);
+                at[c] = momentum + w.line * ml + 4 * w.at * ms;
+                if (e.s.momentum) mom[c] = load_four<float>(at[c], ms, count[c]);
+            }
+#pragma unroll
+            for (int c = 0; c < BATCH; c++)
+                if (count[c]) {
+                    if (e.s.momentum) {
+                        const float4v now = (float)a.r.momentum * mom[c] + u[c];
+                        store_four<float>(at[c], ms, count[c], now);
+                        u[c] = a.r.nesterov ? u[c] + (float)a.r.momentum * now : now;
+                    }
+                    stage[k0 + c * THREADS] = u[c];
+#pragma unroll
+                    for (int r = 0; r < 4; r++) sq += (double)u[c][r] * (double)u[c][r];
+                }
+        }
+    }
+    typedef uint32_t word4 __attribute__((ext_vector_type(4)));
+    for (int k = threadIdx.x; k < 2 * flow / 8; k += THREADS) ((word4*)first)[k] = word4{0, 0, 0, 0};
+    for (int k = threadIdx.x; k < 2 * alow / 8; k += THREADS) ((word4*)A)[k] = word4{0, 0, 0, 0};
+    const double inv = (double)sc.sx / (sqrt(group_sum<THREADS>(sq, norm_part)) + a.r.eps);
+    {
+        Walk w(groups);
+        for (int k = threadIdx.x; k < total; k += THREADS, w.next()) {
+            float4v u = stage[k];
+#pragma unroll
+            for (int r = 0; r < 4; r++) u[r] = (float)((double)u[r] * inv);
+            put_two4(first + w.line * pf + 4 * w.at, flow, u);
+        }
+    }
+    __syncthreads();
+    for (int t = wave; t < mp * np / 256; t += waves) {
+        const int ft = (by_row ? mp : np) / 16, i = t % ft * 16 + row, j = t / ft * 16 + 4 * part;
+        const _Float16* x = first + i * pf + j;
+        _Float16* q = second + (j + (i & 3)) * ps + (i & ~3);
+        *(half4*)q = turn4(*(const half4*)x);
+        *(half4*)(q + slow) = turn4(*(const half4*)(x + flow));
+    }
+    __syncthreads();
+
+    // tiles of A and B on and below the diagonal: at most 10, three for each of four wavefronts
+    constexpr int TILES_EACH = THREADS / 64 >= 10 ? 1 : 3;
+    auto tile_row = [](int t) { return (t > 0) + (t > 2) + (t > 5); };
+    const int mt = (m + 15) / 16, nt = (n + 15) / 16, lower = mt * (mt + 1) / 2;
+    for (int step = 0; step < a.steps; step++) {
+        float4v acc[TILES_EACH];
+#pragma unroll
+        for (int which = 0; which < 2; which++) {
+            const float f0 = (float)a.b * sc.sb / sc.sa;
+            const float f1 = which ? (float)a.c * sc.sb / (sc.sa * sc.sa) : sc.sa / (sc.sx * sc.sx);
+#pragma unroll
+            for (int c = 0; c < TILES_EACH; c++) {
+                const int t = wave + c * waves, ti = tile_row(t), tj = t - ti * (ti + 1) / 2;
+                if (t < lower) {
+                    const _Float16* S = which ? A : X;
+                    const int ps = which ? pt : px;
+                    const int i = ti * 16, j = tj * 16 + 4 * part;
+                    float4v v = two_part(S + (tj * 16 + row) * ps + 8 * part, S + (i + row) * ps + 8 * part, which ? alow : xlow, which ? mp : np) * f1;
+                    if (which) v = add_two4(v, A + (i + row) * pt + j, alow, f0);
+                    acc[c] = v;
+                }
+            }
+            if (which) __syncthreads();  // B takes A's place
+#pragma unroll
+            for (int c = 0; c < TILES_EACH; c++) {
+                const int t = wave + c * waves, ti = tile_row(t), tj = t - ti * (ti + 1) / 2;
+                const int i = ti * 16 + row, j = tj * 16 + 4 * part;
+                if (t < lower) {
+                    put_two4(A + i * pt + j, alow, acc[c]);
+                    if (ti != tj) put_turned(A, pt, alow, i, j, acc[c]);
+                }
+            }
+            __syncthreads();
+        }
+        const float f0 = (float)a.a, f1 = 1 / sc.sb;
+        // two columns of tiles at a time: B's rows are read half as often
+        for (int t = 2 * wave; t < nt; t += 2 * waves) {
+            const int j = t * 16 + 4 * part;
+            float4v y[SMALL_M / 16][2] = {};
+            for (int k = 0; k < mp; k += 32) {
+                half8 ph[2], pl[2];
+#pragma unroll
+                for (int c = 0; c < 2; c++) {
+                    const _Float16* p = XT + (min(t + c, nt - 1) * 16 + row) * pt + 8 * part + k;
+                    ph[c] = *(const half8*)p, pl[c] = *(const half8*)(p + tlow);
+                }
+#pragma unroll
+                for (int i = 0; i < SMALL_M / 16; i++)
+                    if (i < mt) {
+                        const _Float16* q = A + (i * 16 + row) * pt + 8 * part + k;
+                        const half8 qh = *(const half8*)q, ql = *(const half8*)(q + alow);
+#pragma unroll
+                        for (int c = 0; c < 2; c++) y[i][c] = __builtin_amdgcn_mfma_f32_16x16x32_f16(pl[c], qh, y[i][c], 0, 0, 0);
+#pragma unroll
+                        for (int c = 0; c < 2; c++) y[i][c] = __builtin_amdgcn_mfma_f32_16x16x32_f16(ph[c], ql, y[i][c], 0, 0, 0);
+#pragma unroll
+                        for (int c = 0; c < 2; c++) y[i][c] = __builtin_amdgcn_mfma_f32_16x16x32_f16(ph[c], qh, y[i][c], 0, 0, 0);
+                    }
+            }
+            __builtin_amdgcn_wave_barrier();  // all of the old X^T has been read
+#pragma unroll
+            for (int c = 0; c < 2; c++)
+#pragma unroll
+                for (int i = 0; i < SMALL_M / 16; i++)
+                    if (i < mt && t + c < nt) {
+                        _Float16* p = X + (i * 16 + row) * px + j + c * 16;
+                        const float4v v = add_two4(f1 * y[i][c], p, xlow, f0);
+                        put_two4(p, xlow, v);
+                        put_turned(XT, pt, tlow, i * 16 + row, j + c * 16, v);
+                    }
+        }
+        __syncthreads();
+    }
+    {
+        const _Float16* from = out_by_row ? X : XT;
+        const int behind = out_by_row ? xlow : tlow, pitch = out_by_row ? px : pt, wide = out_by_row ? n : m, groups = (wide + 3) / 4;
+        const int64_t ol = out_by_row ? e.t.oi : e.t.oj, os = out_by_row ? e.t.oj : e.t.oi;
+        const int total = (out_by_row ? m : n) * groups;
+        T* out = out_at<T>(e.t, b, 0, 0);
+        Walk w(groups);
+        for (int k0 = threadIdx.x; k0 < total; k0 += BATCH * THREADS) {
+            float4v v[BATCH], old[BATCH];
+            T* at[BATCH];
+            int count[BATCH];
+#pragma unroll
+            for (int c = 0; c < BATCH; c++, w.next()) {
+                count[c] = k0 + c * THREADS < total ? min(4, wide - 4 * w.at) : 0;
+                at[c] = out + w.line * ol + 4 * w.at * os;
+                if (a.r.muon) old[c] = load_four<T>(at[c], os, count[c]);
+                if (count[c]) v[c] = get_two4(from + w.line * pitch + 4 * w.at, behind) * (1 / sc.sx);
+            }
+#pragma unroll
+            for (int c = 0; c < BATCH; c++)
+                store_four<T>(at[c], os, count[c], a.r.muon ? (float)a.r.keep * old[c] - (float)e.t.step * v[c] : v[c]);
+        }
     }
 }
 
@@ -380,7 +663,6 @@ __device__ __forceinline__ int xcd_run(int block, int blocks) {
 }
 
 // Four consecutive values of a row (col % 4 = 0).
-typedef _Float16 half4 __attribute__((ext_vector_type(4)));
 template <int F> __device__ __forceinline__ float4v get4(const char* p, int64_t row, int64_t ld, int col) {
     const _Float16* r = (const _Float16*)(p + row * ld) + (F == ONE ? col : col / 32 * 64 + col % 32);
     float4v v = __builtin_convertvector(*(const half4*)r, float4v);
@@ -649,11 +931,9 @@ __global__ __launch_bounds__(64 * WI * WJ, 2) void k_ortho_gemm(GemmArgs a) {
                     float4v v = acc[i][j] * (float)a.f1;
                     if constexpr (MODE != GRAM) v += now.add[j] * (float)a.f0;
                     acc[i][j] = v;
-                    const half4 hi = __builtin_convertvector(v, half4);
+                    const half4 hi = high(v);
                     *(half4*)(own + row * WIDE + j * 16 + 4 * part) = hi;
-                    if constexpr (F == TWO)
-                        *(half4*)(own + (16 + row) * WIDE + j * 16 + 4 * part) =
-                            __builtin_convertvector(v - __builtin_convertvector(hi, float4v), half4);
+                    if constexpr (F == TWO) *(half4*)(own + (16 + row) * WIDE + j * 16 + 4 * part) = low(v, hi);
                 }
                 __builtin_amdgcn_wave_barrier();
 #pragma unroll
@@ -673,12 +953,10 @@ __global__ __launch_bounds__(64 * WI * WJ, 2) void k_ortho_gemm(GemmArgs a) {
 #pragma unroll
                     for (int plane = 0; plane < PLANES; plane++) {
 #pragma unroll
-                        for (int i = 0; i < TI; i++)
-#pragma unroll
-                            for (int r = 0; r < 4; r++) {
-                                const _Float16 hi = (_Float16)acc[i][j][r];
-                                own[(4 * part + r) * HIGH + i * 16 + row] = plane ? (_Float16)(acc[i][j][r] - (float)hi) : hi;
-                            }
+                        for (int i = 0; i < TI; i++) {
+                            const half4 hi = high(acc[i][j]);
+                            *(half4*)(own + (4 * part + (row & 3)) * HIGH + i * 16 + (row & ~3)) = turn4(plane ? low(acc[i][j], hi) : hi);
+                        }
                         __builtin_amdgcn_wave_barrier();
 #pragma unroll
                         for (int c = 0; c < (16 * TI * 2 + 63) / 64; c++) {
@@ -753,8 +1031,11 @@ Target target_of(const ql_matrix& q, const OrthoCall& c) {
     return r;
 }
 
+// Whether one workgroup's LDS holds the matrix.
 bool is_small(int type, const Shape& s) {
-    return s.m <= SMALL_M && small_lds(s.m, s.n, type == E_F64 ? 8 : 4) <= SMALL_LDS;
+    if (s.m > SMALL_M) return false;
+    if (type == E_F64) return small_lds(s.m, s.n, 8) <= SMALL_LDS;
+    return tiny_lds(s.m, s.n) <= TINY_LDS;
 }
 
 // Workgroups of the norm: each takes at least 4096 elements, and whole lines.
@@ -776,12 +1057,39 @@ bool all_small(int type, const ql_matrix* mats, int count) {
     return true;
 }
 
+struct Scales {  // powers of two that bring the largest possible values to at most 2^15
+    double sx = 1, sa = 1, sb = 1;
+};
+Scales scales_of(const OrthoCall& c) {
+    double most_x = 1, most_q = 1;
+    ortho_bounds(c.a, c.b, c.c, c.steps, most_x, most_q);
+    return {std::exp2(std::floor(std::log2(32768 / most_x))), std::exp2(std::floor(std::log2(32768 / (most_x * most_x)))),
+            std::exp2(std::floor(std::log2(32768 / std::max(most_q, 1e-3))))};
+}
+
+// Past 64 KiB the runtime wants a kernel's limit set, once on each device.
+hipError_t allow_lds(const void* kernel, std::atomic<uint64_t>& ready, int bytes) {
+    int dev = 0;
+    if (hipError_t e = hipGetDevice(&dev); e != hipSuccess) return e;
+    if (dev < 64 && (ready.load(std::memory_order_acquire) >> dev & 1)) return hipSuccess;
+    const hipError_t e = hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
+    if (e == hipSuccess && dev < 64) ready.fetch_or(1ull << dev, std::memory_order_release);
+    return e;
+}
+
+template <typename T, int THREADS> hipError_t launch_tiny(const SmallArgs& a, unsigned blocks, size_t lds, const Scales& k, hipStream_t s) {
+    static std::atomic<uint64_t> ready{0};
+    if (hipError_t e = allow_lds((const void*)k_ortho_tiny<T, THREADS>, ready, TINY_LDS); e != hipSuccess) return e;
+    k_ortho_tiny<T, THREADS><<<blocks, THREADS, lds, s>>>(a, SmallScale{(float)k.sx, (float)k.sa, (float)k.sb});
+    return hipGetLastError();
+}
+
 template <typename T> hipError_t run_small(const OrthoCall& c, const Rule& rule, hipStream_t s) {
     for (int at = 0; at < c.count;) {
         SmallArgs a{};
         a.r = rule, a.a = c.a, a.b = c.b, a.c = c.c, a.steps = c.steps;
         size_t lds = 0;
-        int64_t blocks = 0;
+        int64_t blocks = 0, most = 0;
         for (; at < c.count && a.count < ENTRIES; at++) {
             const ql_matrix& q = c.mats[at];
             if (q.batch == 0) continue;
@@ -789,20 +1097,22 @@ template <typename T> hipError_t run_small(const OrthoCall& c, const Rule& rule,
             if (blocks + q.batch > INT32_MAX) break;
             a.e[a.count++] = {source_of(q, c.muon), target_of(q, c), sh.m, sh.n, (int32_t)blocks, (int32_t)q.batch};
             blocks += q.batch;
-            lds = std::max(lds, small_lds(sh.m, sh.n, sizeof(Acc<T>)));
+            most = std::max(most, (int64_t)sh.m * sh.n);
+            lds = std::max(lds, std::is_same_v<T, double> ? small_lds(sh.m, sh.n, 8) : tiny_lds(sh.m, sh.n));
         }
         if (!blocks) continue;
-        // past 64 KiB the runtime wants the kernel's limit set, once on each device
-        static std::atomic<uint64_t> ready{0};
-        int dev = 0;
-        if (hipError_t e = hipGetDevice(&dev); e != hipSuccess) return e;
-        if (dev >= 64 || !(ready.load(std::memory_order_acquire) >> dev & 1)) {
-            const hipError_t e = hipFuncSetAttribute((const void*)k_ortho_small<T>, hipFuncAttributeMaxDynamicSharedMemorySize, SMALL_LDS);
+        hipError_t e;
+        if constexpr (std::is_same_v<T, double>) {
+            static std::atomic<uint64_t> ready{0};
+            e = allow_lds((const void*)k_ortho_small<T>, ready, SMALL_LDS);
             if (e != hipSuccess) return e;
-            if (dev < 64) ready.fetch_or(1ull << dev, std::memory_order_release);
+            k_ortho_small<T><<<(unsigned)blocks, SMALL_THREADS, lds, s>>>(a);
+            e = hipGetLastError();
+        } else {
+            const Scales k = scales_of(c);
+            e = most <= 256 * 8 ? launch_tiny<T, 256>(a, (unsigned)blocks, lds, k, s) : launch_tiny<T, 1024>(a, (unsigned)blocks, lds, k, s);
         }
-        k_ortho_small<T><<<(unsigned)blocks, SMALL_THREADS, lds, s>>>(a);
-        if (hipError_t f = hipGetLastError(); f != hipSuccess) return f;
+        if (e != hipSuccess) return e;
     }
     return hipSuccess;
 }
@@ -892,15 +1202,8 @@ template <typename T> hipError_t run_steps(const OrthoCall& c, GemmArgs g, const
 }
 
 template <typename T> hipError_t run_large(const OrthoCall& c, const Rule& rule, char* ws, hipStream_t s) {
-    // powers of two that bring the largest possible values to at most 2^15
-    double sx = 1, sa = 1, sb = 1;
-    if (FORMAT<T> != DOUBLE) {
-        double most_x = 1, most_q = 1;
-        ortho_bounds(c.a, c.b, c.c, c.steps, most_x, most_q);
-        sx = std::exp2(std::floor(std::log2(32768 / most_x)));
-        sa = std::exp2(std::floor(std::log2(32768 / (most_x * most_x))));
-        sb = std::exp2(std::floor(std::log2(32768 / std::max(most_q, 1e-3))));
-    }
+    const Scales k = FORMAT<T> == DOUBLE ? Scales{} : scales_of(c);
+    const double sx = k.sx, sa = k.sa, sb = k.sb;
     for (int at = 0; at < c.count;) {
         PackArgs p{};
         GemmArgs g{};
