@@ -13,18 +13,28 @@ import functools
 from .qlayer import _check, _ptr, _stream, _torch, load
 
 
-@functools.lru_cache(maxsize=None)
+_TYPES = {}
+
+
 def types():
     """torch dtype -> ql_type."""
-    torch = _torch()
-    return {torch.float32: 0, torch.float64: 1, torch.bfloat16: 2, torch.float16: 3}
+    if not _TYPES:
+        torch = _torch()
+        _TYPES.update({torch.float32: 0, torch.float64: 1, torch.bfloat16: 2, torch.float16: 3})
+    return _TYPES
 
 
 def type_of(t, what):
     try:
-        return types()[t.dtype]
+        return (_TYPES or types())[t.dtype]
     except KeyError:
         raise ValueError(f"{what} must be float32, float64, bfloat16 or float16, got {t.dtype}") from None
+
+
+def on_device(index):
+    """A context in which the device is current (None: it is already)."""
+    torch = _torch()
+    return None if index == torch.cuda.current_device() else torch.cuda.device(index)
 
 
 @functools.lru_cache(maxsize=1024)
@@ -34,67 +44,61 @@ def _workspace_bytes(type_, rows, features, backward):
     return out.value
 
 
-def _rows(t):
+def _rows(t, shape):
     """(tensor, rows, stride between rows) of t's rows along its last axis; a
     copy where they do not lie a fixed stride apart."""
-    if t.dim() == 2 and (t.stride(1) == 1 or t.shape[1] == 1):
-        rows, stride = t.shape[0], t.stride(0)
-        if stride >= 0:
-            return t, rows, stride
+    if len(shape) == 2:
+        stride, unit = t.stride()
+        if unit == 1 or shape[1] == 1:
+            return t, shape[0], stride
+    n = shape[-1]
     if not t.is_contiguous():
         try:
-            return _rows(t.view(-1, t.shape[-1]))
+            flat = t.view(-1, n)
+            return _rows(flat, flat.shape)
         except RuntimeError:
             t = t.contiguous()
-    n = t.shape[-1]
-    return t, t.numel() // n if n else 0, n
+    return t, t.numel() // n, n
 
 
-def _parameter(p, x, n, what):
-    if p.dim() != 1 or p.shape[0] != n or p.device != x.device or not p.is_contiguous():
-        raise ValueError(f"{what} must be a contiguous tensor [{n}] on {x.device}")
+def _parameter(p, device, n, what):
+    if p.dim() != 1 or p.shape[0] != n or p.get_device() != device or not p.is_contiguous():
+        raise ValueError(f"{what} must be a contiguous tensor [{n}] on x's device")
     return type_of(p, what)
 
 
 def _check_rows(x):
-    if not x.is_cuda or x.dim() < 1 or x.shape[-1] < 1:
+    device, shape = x.get_device(), x.shape
+    if device < 0 or not shape or shape[-1] < 1:
         raise ValueError("x must be a CUDA tensor [..., features]")
-    return type_of(x, "x")
-
-
-def _weight_type(x, xt, weight, bias):
-    wt = None
-    for p, what in ((weight, "weight"), (bias, "bias")):
-        if p is not None:
-            t = _parameter(p, x, x.shape[-1], what)
-            if wt is not None and t != wt:
-                raise ValueError("weight and bias must have the same dtype")
-            wt = t
-    return xt if wt is None else wt
-
-
-def _stats_dtype(x):
-    torch = _torch()
-    return torch.float64 if x.dtype == torch.float64 else torch.float32
+    return device, shape, type_of(x, "x")
 
 
 def layer_norm_forward(x, weight=None, bias=None, eps=1e-5, stats=True):
     """(y, mean, rstd) of the rows along x's last axis; mean and rstd (what
     ``layer_norm_backward`` takes) are None without ``stats``."""
-    torch = _torch()
-    xt = _check_rows(x)
-    wt = _weight_type(x, xt, weight, bias)
-    with torch.cuda.device_of(x):
-        xr, rows, stride = _rows(x)
-        y = torch.empty(x.shape, dtype=x.dtype, device=x.device)
-        mean = rstd = None
-        if stats:
-            mean, rstd = torch.empty((2, *x.shape[:-1]), dtype=_stats_dtype(x), device=x.device).unbind(0)
-        ws_bytes = _workspace_bytes(xt, rows, x.shape[-1], 0)
-        ws = torch.empty(ws_bytes, dtype=torch.uint8, device=x.device) if ws_bytes else None
-        _check(load().ql_layer_norm_forward(xt, wt, rows, x.shape[-1], xr.data_ptr(), stride, _ptr(weight), _ptr(bias),
-                                            eps, y.data_ptr(), _ptr(mean), _ptr(rstd), _ptr(ws), ws_bytes,
-                                            _stream(x.device)))
+    device, shape, xt = _check_rows(x)
+    n, wt = shape[-1], xt
+    if weight is not None:
+        wt = _parameter(weight, device, n, "weight")
+        if bias is not None and _parameter(bias, device, n, "bias") != wt:
+            raise ValueError("weight and bias must have the same dtype")
+    elif bias is not None:
+        wt = _parameter(bias, device, n, "bias")
+    there = on_device(device)
+    if there is not None:
+        with there:
+            return layer_norm_forward(x, weight, bias, eps, stats)
+    xr, rows, stride = _rows(x, shape)
+    y = x.new_empty(shape)
+    mean = rstd = None
+    if stats:
+        mean, rstd = x.new_empty((2, *shape[:-1]), dtype=None if xt < 2 else _torch().float32).unbind(0)
+    ws, ws_bytes = None, _workspace_bytes(xt, rows, n, 0)
+    if ws_bytes:
+        ws = x.new_empty(ws_bytes, dtype=_torch().uint8)
+    _check(load().ql_layer_norm_forward(xt, wt, rows, n, xr.data_ptr(), stride, _ptr(weight), _ptr(bias), eps,
+                                        y.data_ptr(), _ptr(mean), _ptr(rstd), _ptr(ws), ws_bytes, _stream(x.device)))
     return y, mean, rstd
 
 
@@ -103,31 +107,33 @@ def layer_norm_backward(grad_y, x, mean, rstd, weight=None, want_x=True, want_we
     """(grad_x, grad_weight, grad_bias) from the forward's x, mean and rstd;
     None for each that is not wanted. The gradients of weight and bias have
     weight's dtype (``weight_dtype``, default x's, without a weight)."""
-    torch = _torch()
-    xt = _check_rows(x)
-    n = x.shape[-1]
+    device, shape, xt = _check_rows(x)
+    n = shape[-1]
     if weight is not None:
-        wt, wd = _parameter(weight, x, n, "weight"), weight.dtype
+        wt, wd = _parameter(weight, device, n, "weight"), weight.dtype
     else:
         wd = x.dtype if weight_dtype is None else weight_dtype
         wt = types().get(wd, -1)
-    if grad_y.shape != x.shape or grad_y.dtype != x.dtype or grad_y.device != x.device:
+    if grad_y.shape != shape or grad_y.dtype != x.dtype or grad_y.get_device() != device:
         raise ValueError("grad_y must have x's shape, dtype and device")
-    sd = _stats_dtype(x)
+    sd = x.dtype if xt < 2 else _torch().float32
     for s in (mean, rstd):
-        if s.shape != x.shape[:-1] or s.dtype != sd or s.device != x.device or not s.is_contiguous():
-            raise ValueError(f"mean and rstd must be contiguous {sd} tensors {tuple(x.shape[:-1])}")
-    with torch.cuda.device_of(x):
-        xr, rows, xs = _rows(x)
-        gr, _, gs = _rows(grad_y)
-        gx = torch.empty(x.shape, dtype=x.dtype, device=x.device) if want_x else None
-        gw = torch.empty(n, dtype=wd, device=x.device) if want_weight else None
-        gb = torch.empty(n, dtype=wd, device=x.device) if want_bias else None
-        ws_bytes = _workspace_bytes(xt, rows, n, 1)
-        ws = torch.empty(ws_bytes, dtype=torch.uint8, device=x.device)
-        _check(load().ql_layer_norm_backward(xt, wt, rows, n, gr.data_ptr(), gs, xr.data_ptr(), xs, mean.data_ptr(),
-                                             rstd.data_ptr(), _ptr(weight), _ptr(gx), _ptr(gw), _ptr(gb), ws.data_ptr(),
-                                             ws_bytes, _stream(x.device)))
+        if s.shape != shape[:-1] or s.dtype != sd or s.get_device() != device or not s.is_contiguous():
+            raise ValueError(f"mean and rstd must be contiguous {sd} tensors {tuple(shape[:-1])} on x's device")
+    there = on_device(device)
+    if there is not None:
+        with there:
+            return layer_norm_backward(grad_y, x, mean, rstd, weight, want_x, want_weight, want_bias, weight_dtype)
+    xr, rows, xs = _rows(x, shape)
+    gr, _, gs = _rows(grad_y, shape)
+    gx = x.new_empty(shape) if want_x else None
+    gw = x.new_empty(n, dtype=wd) if want_weight else None
+    gb = x.new_empty(n, dtype=wd) if want_bias else None
+    ws_bytes = _workspace_bytes(xt, rows, n, 1)
+    ws = x.new_empty(ws_bytes, dtype=_torch().uint8)
+    _check(load().ql_layer_norm_backward(xt, wt, rows, n, gr.data_ptr(), gs, xr.data_ptr(), xs, mean.data_ptr(),
+                                         rstd.data_ptr(), _ptr(weight), _ptr(gx), _ptr(gw), _ptr(gb), ws.data_ptr(),
+                                         ws_bytes, _stream(x.device)))
     return gx, gw, gb
 
 
