@@ -638,6 +638,10 @@ template <typename T> __global__ __launch_bounds__(256) void k_ortho_pack(PackAr
 //   APPLY X = a X + B (X^T)^T, and its transpose
 //   LAST  the same, to the caller's matrix
 enum Mode { GRAM, POLY, APPLY, LAST };
+// A product with few tiles and a long K is split along K: PART workgroups leave
+// their sums in the workspace, and one JOIN workgroup a tile adds them in order
+// and goes on as a WHOLE one does.
+enum Split { WHOLE, PART, JOIN };
 struct GemmEntry {
     char* work;
     Target t;
@@ -648,6 +652,8 @@ struct GemmArgs {
     Rule r;
     double f0, f1;  // C is stored as f0 * (what it adds to) + f1 * (the sum)
     int32_t count, from;  // from: which X^T is read
+    int32_t splits;
+    char* part;           // [tile][split][values of a tile] fp32, as the threads hold them
 };
 
 // 16 bytes of each lane from a buffer to LDS: lane l's lie 16 l past `to`.
@@ -692,7 +698,7 @@ template <int READS> __device__ __forceinline__ void spread() {
 // row are on their way to LDS, STAGES - 1 steps ahead, while the products of a
 // step run. Chunk q (16 bytes) of a row r lies at q ^ (r % 8): the rows that a
 // wavefront reads together start in different banks.
-template <typename T, int MODE, int BT, int WI, int WJ, int STAGES>
+template <typename T, int MODE, int SPLIT, int BT, int WI, int WJ, int STAGES>
 __global__ __launch_bounds__(64 * WI * WJ, 2) void k_ortho_gemm(GemmArgs a) {
     constexpr int F = FORMAT<T>, U = unit_of(F), THREADS = 64 * WI * WJ, TI = BT / WI / 16, TJ = BT / WJ / 16;
     constexpr int LOADS = BT * 8 / THREADS;  // of a thread, for each operand
@@ -700,7 +706,8 @@ __global__ __launch_bounds__(64 * WI * WJ, 2) void k_ortho_gemm(GemmArgs a) {
     using Q = typename Quad<R>::type;
     STAGE(s0);
     STAGE(s1);
-    const int block = xcd_run(blockIdx.x, gridDim.x);
+    const int all = SPLIT == PART ? gridDim.x / a.splits : gridDim.x;
+    const int run = xcd_run(blockIdx.x, gridDim.x), block = SPLIT == PART ? run % all : run;
     const GemmEntry& e = a.e[entry_of(a.e, a.count, block)];
     const int mp = (int)up64(e.m), np = (int)up64(e.n);
     const Layout l = layout_of(mp, np, U);
@@ -730,6 +737,11 @@ __global__ __launch_bounds__(64 * WI * WJ, 2) void k_ortho_gemm(GemmArgs a) {
 
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wi = wave / WJ, wj = wave % WJ;
     const int row = lane % 16, part = lane / 16;
+    int begin = 0, end = ld;  // bytes of the rows that this workgroup multiplies
+    if constexpr (SPLIT == PART) {
+        const int each = (ld / 128 + a.splits - 1) / a.splits * 128;
+        begin = run / all * each, end = min(begin + each, ld);
+    }
     uint32_t lat[LOADS], rat[LOADS];
 #pragma unroll
     for (int c = 0; c < LOADS; c++) {
@@ -800,7 +812,7 @@ __global__ __launch_bounds__(64 * WI * WJ, 2) void k_ortho_gemm(GemmArgs a) {
         spread<TI + TJ>();
         __builtin_amdgcn_sched_barrier(0);
         arrived(std::integral_constant<int, 2 * LOADS*(STAGES - 2)>{});
-        load(now, min(k + 128 * STAGES, ld - 128));
+        load(now, min(k + 128 * STAGES, end - 128));
         __builtin_amdgcn_sched_barrier(0);
         if constexpr (F == TWO) {  // hi lo, then lo hi
             product(p, q1);
@@ -815,49 +827,74 @@ __global__ __launch_bounds__(64 * WI * WJ, 2) void k_ortho_gemm(GemmArgs a) {
         }
         __builtin_amdgcn_sched_barrier(0);
     };
-    load(s0, 0);
-    load(s1, min(128, ld - 128));
-    if constexpr (STAGES == 2) {
-        arrived(std::integral_constant<int, 2 * LOADS>{});
-        read(s0, 0, p, q);
-        for (int k = 0;; k += 256) {
-            step(s0, s1, k);
-            if (k + 128 >= ld) break;
-            step(s1, s0, k + 128);
-            if (k + 256 >= ld) break;
+    if (SPLIT != JOIN && begin < end) {
+        load(s0, begin);
+        load(s1, min(begin + 128, end - 128));
+        if constexpr (STAGES == 2) {
+            arrived(std::integral_constant<int, 2 * LOADS>{});
+            read(s0, 0, p, q);
+            for (int k = begin;; k += 256) {
+                step(s0, s1, k);
+                if (k + 128 >= end) break;
+                step(s1, s0, k + 128);
+                if (k + 256 >= end) break;
+            }
+        } else if constexpr (STAGES == 3) {
+            STAGE(s2);
+            load(s2, min(begin + 256, end - 128));
+            arrived(std::integral_constant<int, 4 * LOADS>{});
+            read(s0, 0, p, q);
+            for (int k = begin;; k += 384) {
+                step(s0, s1, k);
+                if (k + 128 >= end) break;
+                step(s1, s2, k + 128);
+                if (k + 256 >= end) break;
+                step(s2, s0, k + 256);
+                if (k + 384 >= end) break;
+            }
+        } else {
+            STAGE(s2);
+            STAGE(s3);
+            load(s2, min(begin + 256, end - 128));
+            load(s3, min(begin + 384, end - 128));
+            arrived(std::integral_constant<int, 6 * LOADS>{});
+            read(s0, 0, p, q);
+            for (int k = begin;; k += 512) {
+                step(s0, s1, k);
+                if (k + 128 >= end) break;
+                step(s1, s2, k + 128);
+                if (k + 256 >= end) break;
+                step(s2, s3, k + 256);
+                if (k + 384 >= end) break;
+                step(s3, s0, k + 384);
+                if (k + 512 >= end) break;
+            }
         }
-    } else if constexpr (STAGES == 3) {
-        STAGE(s2);
-        load(s2, min(256, ld - 128));
-        arrived(std::integral_constant<int, 4 * LOADS>{});
-        read(s0, 0, p, q);
-        for (int k = 0;; k += 384) {
-            step(s0, s1, k);
-            if (k + 128 >= ld) break;
-            step(s1, s2, k + 128);
-            if (k + 256 >= ld) break;
-            step(s2, s0, k + 256);
-            if (k + 384 >= ld) break;
+        __builtin_amdgcn_s_waitcnt(0);
+    }
+    if constexpr (SPLIT != WHOLE) {
+        Q* part = (Q*)a.part + (int64_t)block * a.splits * (TI * TJ * THREADS) + threadIdx.x;
+        if constexpr (SPLIT == PART) {
+            part += (int64_t)(run / all) * (TI * TJ * THREADS);
+#pragma unroll
+            for (int k = 0; k < TI * TJ; k++) part[k * THREADS] = acc[k / TJ][k % TJ];
+            return;
         }
-    } else {
-        STAGE(s2);
-        STAGE(s3);
-        load(s2, min(256, ld - 128));
-        load(s3, min(384, ld - 128));
-        arrived(std::integral_constant<int, 6 * LOADS>{});
-        read(s0, 0, p, q);
-        for (int k = 0;; k += 512) {
-            step(s0, s1, k);
-            if (k + 128 >= ld) break;
-            step(s1, s2, k + 128);
-            if (k + 256 >= ld) break;
-            step(s2, s3, k + 256);
-            if (k + 384 >= ld) break;
-            step(s3, s0, k + 384);
-            if (k + 512 >= ld) break;
+        // several splits' loads under way together
+        constexpr int TOGETHER = BT == 64 ? 8 : 2;
+        for (int split = 0; split < a.splits; split += TOGETHER) {
+            Q v[TOGETHER][TI * TJ];
+#pragma unroll
+            for (int c = 0; c < TOGETHER; c++)
+#pragma unroll
+                for (int k = 0; k < TI * TJ; k++) v[c][k] = part[(int64_t)(min(split + c, a.splits - 1) * TI * TJ + k) * THREADS];
+#pragma unroll
+            for (int c = 0; c < TOGETHER; c++)
+                if (split + c < a.splits)
+#pragma unroll
+                    for (int k = 0; k < TI * TJ; k++) acc[k / TJ][k % TJ] += v[c][k];
         }
     }
-    __builtin_amdgcn_s_waitcnt(0);
     const int64_t lda = (int64_t)mp * U, ldx = (int64_t)np * U;
     const int i0 = ti * BT + wi * TI * 16 + row, j0 = tj * BT + wj * TJ * 16;
     if constexpr (F == DOUBLE) {
@@ -1119,16 +1156,21 @@ template <typename T> hipError_t run_small(const OrthoCall& c, const Rule& rule,
 
 static_assert(sizeof(SmallArgs) <= 4096 && sizeof(PackArgs) <= 4096 && sizeof(GemmArgs) <= 4096, "kernel arguments");
 
-template <typename T, int MODE, int BT> hipError_t gemm(GemmArgs a, const int64_t* batch, hipStream_t s) {
+int64_t tiles_of(int mode, int64_t bt, int m, int n) {
+    const int64_t mt = (up64(m) + bt - 1) / bt, nt = (up64(n) + bt - 1) / bt;
+    return mode <= POLY ? mt * (mt + 1) / 2 : mt * nt;
+}
+
+template <typename T, int MODE, int SPLIT, int BT> hipError_t gemm(GemmArgs a, const int64_t* batch, hipStream_t s) {
     int64_t blocks = 0;
     for (int k = 0; k < a.count; k++) {
-        const int64_t mt = (up64(a.e[k].m) + BT - 1) / BT, nt = (up64(a.e[k].n) + BT - 1) / BT;
         a.e[k].first = (int32_t)blocks;
-        blocks += batch[k] * (MODE <= POLY ? mt * (mt + 1) / 2 : mt * nt);
+        blocks += batch[k] * tiles_of(MODE, BT, a.e[k].m, a.e[k].n);
     }
+    if (SPLIT == PART) blocks *= a.splits;
     if (blocks > INT32_MAX) return hipErrorInvalidValue;
     constexpr int WJ = BT >= 192 ? 4 : 2, STAGES = BT == 64 ? 4 : BT == 192 ? 3 : 2;
-    k_ortho_gemm<T, MODE, BT, 2, WJ, STAGES><<<(unsigned)blocks, 128 * WJ, 0, s>>>(a);
+    k_ortho_gemm<T, MODE, SPLIT, BT, 2, WJ, STAGES><<<(unsigned)blocks, 128 * WJ, 0, s>>>(a);
     return hipGetLastError();
 }
 
@@ -1144,100 +1186,148 @@ constexpr TileCost COST[2][4] = {{{0.20, 0.40, 2}, {0.42, 0.78, 8}, {0.95, 0.95,
                                  {{0.25, 0.45, 2}, {0.58, 1.10, 8}, {1.00, 1.00, 12}, {1.6, 1.6, 20}}};
 constexpr int UNITS = 256;  // compute units
 
-double launch_cost(int format, int mode, int which, const GemmArgs& a, const int64_t* batch) {
-    const TileCost& c = COST[format == TWO][which];
+// The entries of a table and their batches, as the costs go by them.
+struct Chunk {
+    Shape shape[ENTRIES];
+    int64_t batch[ENTRIES];
+    int count = 0;
+};
+
+double launch_cost(int format, int mode, int which, int splits, const Chunk& c) {
+    const TileCost& t = COST[format == TWO][which];
     const int64_t bt = TILES[which], slots = which < 2 ? 2 * UNITS : UNITS;
-    double alone = 0, shared = 0, longest = 0;  // sums over tiles, and the longest tile
+    double alone = 0, shared = 0, longest = 0;  // sums over workgroups, and the longest one
     int64_t tiles = 0;
-    for (int k = 0; k < a.count; k++) {
-        const int64_t mp = up64(a.e[k].m), np = up64(a.e[k].n), mt = (mp + bt - 1) / bt, nt = (np + bt - 1) / bt;
-        const int64_t n = batch[k] * (mode <= POLY ? mt * (mt + 1) / 2 : mt * nt);
-        const double steps = (double)(mode == GRAM ? np : mp) * unit_of(format) / 128;
+    for (int k = 0; k < c.count; k++) {
+        const int64_t n = c.batch[k] * tiles_of(mode, bt, c.shape[k].m, c.shape[k].n);
+        const int64_t whole = up64(mode == GRAM ? c.shape[k].n : c.shape[k].m) * unit_of(format) / 128;
+        const double steps = (double)((whole + splits - 1) / splits);
         tiles += n;
-        alone += n * (steps * c.alone + c.rest);
-        shared += n * (steps * c.shared + c.rest);
-        longest = std::max(longest, steps * c.alone + c.rest);
+        alone += (double)(n * splits) * (steps * t.alone + t.rest);
+        shared += (double)(n * splits) * (steps * t.shared + t.rest);
+        longest = std::max(longest, steps * t.alone + t.rest);
     }
     if (!tiles) return 0;
-    const int64_t rounds = tiles / slots, rest = tiles % slots;
-    return std::max(longest, rounds * shared / tiles + (rest ? (rest <= UNITS ? alone : shared) / tiles : 0));
+    const int64_t groups = tiles * splits, rounds = groups / slots, rest = groups % slots;
+    double cost = std::max(longest, rounds * shared / groups + (rest ? (rest <= UNITS ? alone : shared) / groups : 0));
+    // the second launch, and the sums' way to memory (3 TB/s) and back
+    if (splits > 1) cost += 3 + t.rest + 0.1 * splits + (double)groups * bt * bt * 8 / 3e6;
+    return cost;
 }
 
-template <typename T, int MODE> hipError_t gemm(const GemmArgs& a, const int64_t* batch, hipStream_t s) {
+// The tile size of a launch, and for GRAM with its short sides the split of K.
+struct Choice {
+    int which = 0, splits = 1;
+    int64_t bytes = 0;  // of the parts
+};
+Choice choose(int format, int mode, const Chunk& c) {
+    Choice best;
+    if (format == DOUBLE) return best;
+    double least = 0;
+    for (int which = 0; which < 4; which++) {
+        int64_t tiles = 0;
+        for (int k = 0; k < c.count; k++) tiles += c.batch[k] * tiles_of(mode, TILES[which], c.shape[k].m, c.shape[k].n);
+        for (int splits = 1; splits == 1 || (mode == GRAM && which < 2 && splits <= 64 && tiles * splits <= 2 * UNITS);
+             splits = splits < 4 ? splits + 1 : splits * 3 / 2) {
+            const double cost = launch_cost(format, mode, which, splits, c);
+            if ((which == 0 && splits == 1) || cost < least) least = cost, best.which = which, best.splits = splits;
+        }
+    }
+    if (best.splits > 1)
+        for (int k = 0; k < c.count; k++)
+            best.bytes += c.batch[k] * tiles_of(mode, TILES[best.which], c.shape[k].m, c.shape[k].n) * best.splits * TILES[best.which] * TILES[best.which] * 4;
+    return best;
+}
+
+template <typename T, int MODE> hipError_t gemm(GemmArgs a, const Chunk& c, const Choice& how, hipStream_t s) {
     if constexpr (FORMAT<T> == DOUBLE) {
-        return gemm<T, MODE, 64>(a, batch, s);
+        return gemm<T, MODE, WHOLE, 64>(a, c.batch, s);
     } else {
-        int best = 0;
-        double cost[4];
-        for (int k = 0; k < 4; k++)
-            if ((cost[k] = launch_cost(FORMAT<T>, MODE, k, a, batch)) < cost[best]) best = k;
-        switch (best) {
-            case 0: return gemm<T, MODE, 64>(a, batch, s);
-            case 1: return gemm<T, MODE, 128>(a, batch, s);
-            case 2: return gemm<T, MODE, 192>(a, batch, s);
-            default: return gemm<T, MODE, 256>(a, batch, s);
+        if constexpr (MODE == GRAM)
+            if (how.splits > 1) {
+                a.splits = how.splits;
+                hipError_t e = how.which ? gemm<T, MODE, PART, 128>(a, c.batch, s) : gemm<T, MODE, PART, 64>(a, c.batch, s);
+                if (e != hipSuccess) return e;
+                return how.which ? gemm<T, MODE, JOIN, 128>(a, c.batch, s) : gemm<T, MODE, JOIN, 64>(a, c.batch, s);
+            }
+        switch (how.which) {
+            case 0: return gemm<T, MODE, WHOLE, 64>(a, c.batch, s);
+            case 1: return gemm<T, MODE, WHOLE, 128>(a, c.batch, s);
+            case 2: return gemm<T, MODE, WHOLE, 192>(a, c.batch, s);
+            default: return gemm<T, MODE, WHOLE, 256>(a, c.batch, s);
         }
     }
 }
 
-template <typename T> hipError_t run_steps(const OrthoCall& c, GemmArgs g, const int64_t* batch, double sx, double sa, double sb, hipStream_t s) {
+// The next entries that a table holds, from `at` on; empty ones are left out.
+int next_chunk(const ql_matrix* mats, int count, int at, Chunk& c, const ql_matrix** entry) {
+    for (c.count = 0; at < count && c.count < ENTRIES; at++)
+        if (mats[at].batch > 0) {
+            c.shape[c.count] = shape_of(mats[at]);
+            c.batch[c.count] = mats[at].batch;
+            if (entry) entry[c.count] = &mats[at];
+            c.count++;
+        }
+    return at;
+}
+
+template <typename T> hipError_t run_steps(const OrthoCall& c, GemmArgs g, const Chunk& chunk, const Scales& k, hipStream_t s) {
+    const Choice gram = choose(FORMAT<T>, GRAM, chunk), poly = choose(FORMAT<T>, POLY, chunk), apply = choose(FORMAT<T>, APPLY, chunk);
     hipError_t e = hipSuccess;
     for (int step = 0; step < c.steps && e == hipSuccess; step++) {
         g.from = step & 1;
-        g.f0 = 0, g.f1 = sa / (sx * sx);
-        e = gemm<T, GRAM>(g, batch, s);
+        g.f0 = 0, g.f1 = k.sa / (k.sx * k.sx);
+        e = gemm<T, GRAM>(g, chunk, gram, s);
         if (e != hipSuccess) break;
-        g.f0 = c.b * sb / sa, g.f1 = c.c * sb / (sa * sa);
-        e = gemm<T, POLY>(g, batch, s);
+        g.f0 = c.b * k.sb / k.sa, g.f1 = c.c * k.sb / (k.sa * k.sa);
+        e = gemm<T, POLY>(g, chunk, poly, s);
         if (e != hipSuccess) break;
         if (step + 1 < c.steps) {
-            g.f0 = c.a, g.f1 = 1 / sb;
-            e = gemm<T, APPLY>(g, batch, s);
+            g.f0 = c.a, g.f1 = 1 / k.sb;
+            e = gemm<T, APPLY>(g, chunk, apply, s);
         } else {
-            g.f0 = c.a / sx, g.f1 = 1 / (sb * sx);
-            e = gemm<T, LAST>(g, batch, s);
+            g.f0 = c.a / k.sx, g.f1 = 1 / (k.sb * k.sx);
+            e = gemm<T, LAST>(g, chunk, apply, s);
         }
     }
     return e;
 }
 
 template <typename T> hipError_t run_large(const OrthoCall& c, const Rule& rule, char* ws, hipStream_t s) {
-    const Scales k = FORMAT<T> == DOUBLE ? Scales{} : scales_of(c);
-    const double sx = k.sx, sa = k.sa, sb = k.sb;
+    const Scales scales = FORMAT<T> == DOUBLE ? Scales{} : scales_of(c);
     for (int at = 0; at < c.count;) {
+        Chunk chunk;
+        const ql_matrix* entry[ENTRIES];
+        at = next_chunk(c.mats, c.count, at, chunk, entry);
+        if (!chunk.count) break;
         PackArgs p{};
         GemmArgs g{};
-        int64_t batch[ENTRIES], norm_blocks = 0;
-        p.r = g.r = rule, p.scale = sx;
-        for (; at < c.count && p.count < ENTRIES; at++) {
-            const ql_matrix& q = c.mats[at];
-            if (q.batch == 0) continue;
-            const Shape sh = shape_of(q);
-            PackEntry& e = p.e[p.count];
-            e.s = source_of(q, c.muon), e.work = ws, e.m = sh.m, e.n = sh.n, e.chunks = chunks_of(sh);
-            ws += q.batch * large_bytes(c.type, sh);
+        int64_t norm_blocks = 0, pack_blocks = 0;
+        p.r = g.r = rule, p.scale = scales.sx, p.count = g.count = chunk.count;
+        for (int k = 0; k < chunk.count; k++) {
+            const Shape& sh = chunk.shape[k];
+            PackEntry& e = p.e[k];
+            e.s = source_of(*entry[k], c.muon), e.work = ws, e.m = sh.m, e.n = sh.n, e.chunks = chunks_of(sh);
+            ws += chunk.batch[k] * large_bytes(c.type, sh);
             e.part = (double*)ws;
-            ws += q.batch * norm_bytes(sh);
+            ws += chunk.batch[k] * norm_bytes(sh);
             e.first = (int32_t)norm_blocks;
-            norm_blocks += q.batch * e.chunks;
-            g.e[p.count] = {e.work, target_of(q, c), sh.m, sh.n, 0};
-            batch[p.count++] = q.batch;
+            norm_blocks += chunk.batch[k] * e.chunks;
+            g.e[k] = {e.work, target_of(*entry[k], c), sh.m, sh.n, 0};
         }
-        if (!p.count) continue;
-        g.count = p.count;
+        g.part = ws;
+        ws += choose(FORMAT<T>, GRAM, chunk).bytes;
         if (norm_blocks > INT32_MAX) return hipErrorInvalidValue;
         k_ortho_norm<T><<<(unsigned)norm_blocks, 256, 0, s>>>(p);
         if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
-        int64_t pack_blocks = 0;
-        for (int k = 0; k < p.count; k++) {
+        for (int k = 0; k < chunk.count; k++) {
             p.e[k].first = (int32_t)pack_blocks;
-            pack_blocks += batch[k] * (up64(p.e[k].m) / 64) * (up64(p.e[k].n) / 64);
+            pack_blocks += chunk.batch[k] * (up64(p.e[k].m) / 64) * (up64(p.e[k].n) / 64);
         }
         if (pack_blocks > INT32_MAX) return hipErrorInvalidValue;
         k_ortho_pack<T><<<(unsigned)pack_blocks, 256, 0, s>>>(p);
         if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
-        const hipError_t e = run_steps<T>(c, g, batch, sx, sa, sb, s);
-        if (e != hipSuccess) return e;
+        if (hipError_t e = run_steps<T>(c, g, chunk, scales, s); e != hipSuccess) return e;
     }
     return hipSuccess;
 }
@@ -1272,9 +1362,11 @@ bool ortho_bounds(double a, double b, double c, int steps, double& most_x, doubl
 size_t ortho_workspace(int type, const ql_matrix* mats, int count) {
     if (all_small(type, mats, count)) return 0;
     int64_t bytes = 0;
-    for (int k = 0; k < count; k++) {
-        const Shape s = shape_of(mats[k]);
-        bytes += mats[k].batch * (large_bytes(type, s) + norm_bytes(s));
+    for (int at = 0; at < count;) {
+        Chunk c;
+        at = next_chunk(mats, count, at, c, nullptr);
+        for (int k = 0; k < c.count; k++) bytes += c.batch[k] * (large_bytes(type, c.shape[k]) + norm_bytes(c.shape[k]));
+        bytes += choose(format_of(type), GRAM, c).bytes;
     }
     return (size_t)bytes;
 }
