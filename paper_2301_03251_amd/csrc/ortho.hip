@@ -11,9 +11,9 @@
 //
 // Products of large matrices are fp16 ones summed in fp32. The singular values
 // of X stay below about 1.2 (ortho_bounds), so X, A and B are held in fp16 at
-// powers of two that use its range: in two parts, v = hi + lo, for float32 and
-// float16 updates (hi hi + hi lo + lo hi keeps 22 bits of every factor), and in
-// one for bfloat16 (11 bits, of which the result keeps 8). fp64 uses fp64.
+// powers of two that use its range: in two parts, v = hi + lo (hi hi + hi lo +
+// lo hi keeps 22 bits of every factor), or for much work in bfloat16 in one (11
+// bits, of which the result keeps 8). fp64 uses fp64.
 #include <algorithm>
 #include <atomic>
 #include <cmath>
@@ -231,6 +231,7 @@ __device__ __forceinline__ float4v two_part(const _Float16* p, const _Float16* q
         const int next = min(k + 32, depth - 32);  // read while these products run
         const half8 nph = *(const half8*)(p + next), npl = *(const half8*)(p + behind + next);
         const half8 nqh = *(const half8*)(q + next), nql = *(const half8*)(q + behind + next);
+        cross0 = __builtin_amdgcn_mfma_f32_16x16x32_f16(pl, ql, cross0, 0, 0, 0);  // little, but K may be short
         cross0 = __builtin_amdgcn_mfma_f32_16x16x32_f16(pl, qh, cross0, 0, 0, 0);
         cross1 = __builtin_amdgcn_mfma_f32_16x16x32_f16(ph, ql, cross1, 0, 0, 0);
         acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(ph, qh, acc, 0, 0, 0);
@@ -453,6 +454,8 @@ template <typename T, int THREADS> __global__ __launch_bounds__(THREADS) void k_
                         const _Float16* q = A + (i * 16 + row) * pt + 8 * part + k;
                         const half8 qh = *(const half8*)q, ql = *(const half8*)(q + alow);
 #pragma unroll
+                        for (int c = 0; c < 2; c++) y[i][c] = __builtin_amdgcn_mfma_f32_16x16x32_f16(pl[c], ql, y[i][c], 0, 0, 0);
+#pragma unroll
                         for (int c = 0; c < 2; c++) y[i][c] = __builtin_amdgcn_mfma_f32_16x16x32_f16(pl[c], qh, y[i][c], 0, 0, 0);
 #pragma unroll
                         for (int c = 0; c < 2; c++) y[i][c] = __builtin_amdgcn_mfma_f32_16x16x32_f16(ph[c], ql, y[i][c], 0, 0, 0);
@@ -504,7 +507,6 @@ template <typename T, int THREADS> __global__ __launch_bounds__(THREADS) void k_
 // (32 columns of hi, then the same 32 of lo), or fp64. A row of K values is
 // K * unit bytes, and 128 bytes of it are one step of a product's main loop.
 enum Format { ONE = 1, TWO = 2, DOUBLE = 3 };
-template <typename T> constexpr int FORMAT = std::is_same_v<T, bf16> ? ONE : std::is_same_v<T, double> ? DOUBLE : TWO;
 constexpr int unit_of(int format) { return format == ONE ? 2 : format == TWO ? 4 : 8; }
 
 // Padded sides: multiples of 64 hold whole main-loop steps of every format.
@@ -584,9 +586,8 @@ template <typename T> __global__ __launch_bounds__(256) void k_ortho_norm(PackAr
 }
 
 // X and X^T of a 64x64 tile.
-template <typename T> __global__ __launch_bounds__(256) void k_ortho_pack(PackArgs a) {
+template <typename T, int F> __global__ __launch_bounds__(256) void k_ortho_pack(PackArgs a) {
     using R = Acc<T>;
-    constexpr int F = FORMAT<T>;
     __shared__ R tile[64][65];
     __shared__ double lds[4];
     const PackEntry& e = a.e[entry_of(a.e, a.count, blockIdx.x)];
@@ -698,9 +699,9 @@ template <int READS> __device__ __forceinline__ void spread() {
 // row are on their way to LDS, STAGES - 1 steps ahead, while the products of a
 // step run. Chunk q (16 bytes) of a row r lies at q ^ (r % 8): the rows that a
 // wavefront reads together start in different banks.
-template <typename T, int MODE, int SPLIT, int BT, int WI, int WJ, int STAGES>
+template <typename T, int F, int MODE, int SPLIT, int BT, int WI, int WJ, int STAGES>
 __global__ __launch_bounds__(64 * WI * WJ, 2) void k_ortho_gemm(GemmArgs a) {
-    constexpr int F = FORMAT<T>, U = unit_of(F), THREADS = 64 * WI * WJ, TI = BT / WI / 16, TJ = BT / WJ / 16;
+    constexpr int U = unit_of(F), THREADS = 64 * WI * WJ, TI = BT / WI / 16, TJ = BT / WJ / 16;
     constexpr int LOADS = BT * 8 / THREADS;  // of a thread, for each operand
     using R = Acc<T>;
     using Q = typename Quad<R>::type;
@@ -814,7 +815,8 @@ __global__ __launch_bounds__(64 * WI * WJ, 2) void k_ortho_gemm(GemmArgs a) {
         arrived(std::integral_constant<int, 2 * LOADS*(STAGES - 2)>{});
         load(now, min(k + 128 * STAGES, end - 128));
         __builtin_amdgcn_sched_barrier(0);
-        if constexpr (F == TWO) {  // hi lo, then lo hi
+        if constexpr (F == TWO) {  // hi lo, then lo hi; lo lo where few values do not average it out, and it costs nothing
+            if constexpr (BT == 64) product(p1, q1);
             product(p, q1);
             __builtin_amdgcn_sched_barrier(0);
             product(p1, q);
@@ -1080,11 +1082,23 @@ int chunks_of(const Shape& s) {
     return (int)std::min<int64_t>(std::min(s.m, 1024), std::max<int64_t>(1, (int64_t)s.m * s.n / 4096));
 }
 
-int format_of(int type) { return type == E_BF16 ? ONE : type == E_F64 ? DOUBLE : TWO; }
+// One part is for bfloat16 updates whose products take the time: 5e9 operations
+// of matrices of more than 64 rows, which cost 8 us more a step in two. Below,
+// launches do, and with few rows the products' rounding does not average out:
+// 12x5992 came out at 1.7 times the error of the output's own rounding.
+int format_of(int type, const ql_matrix* mats, int count) {
+    if (type != E_BF16) return type == E_F64 ? DOUBLE : TWO;
+    double work = 0;
+    for (int k = 0; k < count; k++) {
+        const Shape s = shape_of(mats[k]);
+        if (s.m > SMALL_M) work += 5.0 * (double)mats[k].batch * s.m * s.m * (3.0 * s.n + s.m);
+    }
+    return work >= 5e9 ? ONE : TWO;
+}
 
 // Workspace of a matrix of the large route: X, A and B, then the norm's sums.
-int64_t large_bytes(int type, const Shape& s) {
-    return layout_of((int)up64(s.m), (int)up64(s.n), unit_of(format_of(type))).size;
+int64_t large_bytes(int format, const Shape& s) {
+    return layout_of((int)up64(s.m), (int)up64(s.n), unit_of(format)).size;
 }
 int64_t norm_bytes(const Shape& s) { return (chunks_of(s) * 8 + 255) / 256 * 256; }
 
@@ -1161,7 +1175,7 @@ int64_t tiles_of(int mode, int64_t bt, int m, int n) {
     return mode <= POLY ? mt * (mt + 1) / 2 : mt * nt;
 }
 
-template <typename T, int MODE, int SPLIT, int BT> hipError_t gemm(GemmArgs a, const int64_t* batch, hipStream_t s) {
+template <typename T, int F, int MODE, int SPLIT, int BT> hipError_t gemm(GemmArgs a, const int64_t* batch, hipStream_t s) {
     int64_t blocks = 0;
     for (int k = 0; k < a.count; k++) {
         a.e[k].first = (int32_t)blocks;
@@ -1170,7 +1184,9 @@ template <typename T, int MODE, int SPLIT, int BT> hipError_t gemm(GemmArgs a, c
     if (SPLIT == PART) blocks *= a.splits;
     if (blocks > INT32_MAX) return hipErrorInvalidValue;
     constexpr int WJ = BT >= 192 ? 4 : 2, STAGES = BT == 64 ? 4 : BT == 192 ? 3 : 2;
-    k_ortho_gemm<T, MODE, SPLIT, BT, 2, WJ, STAGES><<<(unsigned)blocks, 128 * WJ, 0, s>>>(a);
+    // only the last product sees the caller's type
+    using K = std::conditional_t<MODE == LAST, T, std::conditional_t<F == ONE, bf16, std::conditional_t<F == TWO, float, double>>>;
+    k_ortho_gemm<K, F, MODE, SPLIT, BT, 2, WJ, STAGES><<<(unsigned)blocks, 128 * WJ, 0, s>>>(a);
     return hipGetLastError();
 }
 
@@ -1220,11 +1236,11 @@ struct Choice {
     int which = 0, splits = 1;
     int64_t bytes = 0;  // of the parts
 };
-Choice choose(int format, int mode, const Chunk& c) {
+Choice choose(int format, int mode, const Chunk& c, int sizes) {
     Choice best;
     if (format == DOUBLE) return best;
     double least = 0;
-    for (int which = 0; which < 4; which++) {
+    for (int which = 0; which < sizes; which++) {
         int64_t tiles = 0;
         for (int k = 0; k < c.count; k++) tiles += c.batch[k] * tiles_of(mode, TILES[which], c.shape[k].m, c.shape[k].n);
         for (int splits = 1; splits == 1 || (mode == GRAM && which < 2 && splits <= 64 && tiles * splits <= 2 * UNITS);
@@ -1239,23 +1255,27 @@ Choice choose(int format, int mode, const Chunk& c) {
     return best;
 }
 
-template <typename T, int MODE> hipError_t gemm(GemmArgs a, const Chunk& c, const Choice& how, hipStream_t s) {
-    if constexpr (FORMAT<T> == DOUBLE) {
-        return gemm<T, MODE, WHOLE, 64>(a, c.batch, s);
+// Tile sizes that a type's calls come to: bfloat16 has little work in two parts.
+template <typename T, int F> constexpr int SIZES = std::is_same_v<T, bf16> && F == TWO ? 1 : 4;
+int sizes_of(int type, int format) { return type == E_BF16 && format == TWO ? 1 : 4; }
+
+template <typename T, int F, int MODE> hipError_t gemm(GemmArgs a, const Chunk& c, const Choice& how, hipStream_t s) {
+    if constexpr (F == DOUBLE) {
+        return gemm<T, F, MODE, WHOLE, 64>(a, c.batch, s);
     } else {
         if constexpr (MODE == GRAM)
             if (how.splits > 1) {
                 a.splits = how.splits;
-                hipError_t e = how.which ? gemm<T, MODE, PART, 128>(a, c.batch, s) : gemm<T, MODE, PART, 64>(a, c.batch, s);
+                hipError_t e = how.which ? gemm<T, F, MODE, PART, 128>(a, c.batch, s) : gemm<T, F, MODE, PART, 64>(a, c.batch, s);
                 if (e != hipSuccess) return e;
-                return how.which ? gemm<T, MODE, JOIN, 128>(a, c.batch, s) : gemm<T, MODE, JOIN, 64>(a, c.batch, s);
+                return how.which ? gemm<T, F, MODE, JOIN, 128>(a, c.batch, s) : gemm<T, F, MODE, JOIN, 64>(a, c.batch, s);
             }
-        switch (how.which) {
-            case 0: return gemm<T, MODE, WHOLE, 64>(a, c.batch, s);
-            case 1: return gemm<T, MODE, WHOLE, 128>(a, c.batch, s);
-            case 2: return gemm<T, MODE, WHOLE, 192>(a, c.batch, s);
-            default: return gemm<T, MODE, WHOLE, 256>(a, c.batch, s);
+        if constexpr (SIZES<T, F> == 4) {
+            if (how.which == 1) return gemm<T, F, MODE, WHOLE, 128>(a, c.batch, s);
+            if (how.which == 2) return gemm<T, F, MODE, WHOLE, 192>(a, c.batch, s);
+            if (how.which == 3) return gemm<T, F, MODE, WHOLE, 256>(a, c.batch, s);
         }
+        return gemm<T, F, MODE, WHOLE, 64>(a, c.batch, s);
     }
 }
 
@@ -1271,30 +1291,31 @@ int next_chunk(const ql_matrix* mats, int count, int at, Chunk& c, const ql_matr
     return at;
 }
 
-template <typename T> hipError_t run_steps(const OrthoCall& c, GemmArgs g, const Chunk& chunk, const Scales& k, hipStream_t s) {
-    const Choice gram = choose(FORMAT<T>, GRAM, chunk), poly = choose(FORMAT<T>, POLY, chunk), apply = choose(FORMAT<T>, APPLY, chunk);
+template <typename T, int F> hipError_t run_steps(const OrthoCall& c, GemmArgs g, const Chunk& chunk, const Scales& k, hipStream_t s) {
+    constexpr int sizes = SIZES<T, F>;
+    const Choice gram = choose(F, GRAM, chunk, sizes), poly = choose(F, POLY, chunk, sizes), apply = choose(F, APPLY, chunk, sizes);
     hipError_t e = hipSuccess;
     for (int step = 0; step < c.steps && e == hipSuccess; step++) {
         g.from = step & 1;
         g.f0 = 0, g.f1 = k.sa / (k.sx * k.sx);
-        e = gemm<T, GRAM>(g, chunk, gram, s);
+        e = gemm<T, F, GRAM>(g, chunk, gram, s);
         if (e != hipSuccess) break;
         g.f0 = c.b * k.sb / k.sa, g.f1 = c.c * k.sb / (k.sa * k.sa);
-        e = gemm<T, POLY>(g, chunk, poly, s);
+        e = gemm<T, F, POLY>(g, chunk, poly, s);
         if (e != hipSuccess) break;
         if (step + 1 < c.steps) {
             g.f0 = c.a, g.f1 = 1 / k.sb;
-            e = gemm<T, APPLY>(g, chunk, apply, s);
+            e = gemm<T, F, APPLY>(g, chunk, apply, s);
         } else {
             g.f0 = c.a / k.sx, g.f1 = 1 / (k.sb * k.sx);
-            e = gemm<T, LAST>(g, chunk, apply, s);
+            e = gemm<T, F, LAST>(g, chunk, apply, s);
         }
     }
     return e;
 }
 
-template <typename T> hipError_t run_large(const OrthoCall& c, const Rule& rule, char* ws, hipStream_t s) {
-    const Scales scales = FORMAT<T> == DOUBLE ? Scales{} : scales_of(c);
+template <typename T, int F> hipError_t run_large(const OrthoCall& c, const Rule& rule, char* ws, hipStream_t s) {
+    const Scales scales = F == DOUBLE ? Scales{} : scales_of(c);
     for (int at = 0; at < c.count;) {
         Chunk chunk;
         const ql_matrix* entry[ENTRIES];
@@ -1308,7 +1329,7 @@ template <typename T> hipError_t run_large(const OrthoCall& c, const Rule& rule,
             const Shape& sh = chunk.shape[k];
             PackEntry& e = p.e[k];
             e.s = source_of(*entry[k], c.muon), e.work = ws, e.m = sh.m, e.n = sh.n, e.chunks = chunks_of(sh);
-            ws += chunk.batch[k] * large_bytes(c.type, sh);
+            ws += chunk.batch[k] * large_bytes(F, sh);
             e.part = (double*)ws;
             ws += chunk.batch[k] * norm_bytes(sh);
             e.first = (int32_t)norm_blocks;
@@ -1316,7 +1337,7 @@ template <typename T> hipError_t run_large(const OrthoCall& c, const Rule& rule,
             g.e[k] = {e.work, target_of(*entry[k], c), sh.m, sh.n, 0};
         }
         g.part = ws;
-        ws += choose(FORMAT<T>, GRAM, chunk).bytes;
+        ws += choose(F, GRAM, chunk, SIZES<T, F>).bytes;
         if (norm_blocks > INT32_MAX) return hipErrorInvalidValue;
         k_ortho_norm<T><<<(unsigned)norm_blocks, 256, 0, s>>>(p);
         if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
@@ -1325,9 +1346,9 @@ template <typename T> hipError_t run_large(const OrthoCall& c, const Rule& rule,
             pack_blocks += chunk.batch[k] * (up64(p.e[k].m) / 64) * (up64(p.e[k].n) / 64);
         }
         if (pack_blocks > INT32_MAX) return hipErrorInvalidValue;
-        k_ortho_pack<T><<<(unsigned)pack_blocks, 256, 0, s>>>(p);
+        k_ortho_pack<T, F><<<(unsigned)pack_blocks, 256, 0, s>>>(p);
         if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
-        if (hipError_t e = run_steps<T>(c, g, chunk, scales, s); e != hipSuccess) return e;
+        if (hipError_t e = run_steps<T, F>(c, g, chunk, scales, s); e != hipSuccess) return e;
     }
     return hipSuccess;
 }
@@ -1335,7 +1356,14 @@ template <typename T> hipError_t run_large(const OrthoCall& c, const Rule& rule,
 template <typename T> hipError_t run(const OrthoCall& c, void* ws, hipStream_t s) {
     Rule r{};
     r.momentum = c.momentum, r.keep = c.keep, r.eps = c.eps, r.muon = c.muon, r.nesterov = c.nesterov;
-    return all_small(c.type, c.mats, c.count) ? run_small<T>(c, r, s) : run_large<T>(c, r, (char*)ws, s);
+    if (all_small(c.type, c.mats, c.count)) return run_small<T>(c, r, s);
+    if constexpr (std::is_same_v<T, double>) {
+        return run_large<T, DOUBLE>(c, r, (char*)ws, s);
+    } else {
+        if constexpr (std::is_same_v<T, bf16>)
+            if (format_of(c.type, c.mats, c.count) == ONE) return run_large<T, ONE>(c, r, (char*)ws, s);
+        return run_large<T, TWO>(c, r, (char*)ws, s);
+    }
 }
 
 }  // namespace
@@ -1361,12 +1389,13 @@ bool ortho_bounds(double a, double b, double c, int steps, double& most_x, doubl
 
 size_t ortho_workspace(int type, const ql_matrix* mats, int count) {
     if (all_small(type, mats, count)) return 0;
+    const int format = format_of(type, mats, count);
     int64_t bytes = 0;
     for (int at = 0; at < count;) {
         Chunk c;
         at = next_chunk(mats, count, at, c, nullptr);
-        for (int k = 0; k < c.count; k++) bytes += c.batch[k] * (large_bytes(type, c.shape[k]) + norm_bytes(c.shape[k]));
-        bytes += choose(format_of(type), GRAM, c).bytes;
+        for (int k = 0; k < c.count; k++) bytes += c.batch[k] * (large_bytes(format, c.shape[k]) + norm_bytes(c.shape[k]));
+        bytes += choose(format, GRAM, c, sizes_of(type, format)).bytes;
     }
     return (size_t)bytes;
 }
