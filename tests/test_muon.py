@@ -230,6 +230,51 @@ def test_large(need_gpu, name, rows, cols):
     near(_f64(Q.orthogonalize(g)), _f64(g), name, f"{rows}x{cols}")
 
 
+def _fp16_parts_torch(parts):
+    def hold(v, size):
+        s = 2.0 ** 14 / size
+        hi = (v * s).half().double()
+        if parts == 2:
+            hi = hi + (v * s - hi).half().double()
+        return hi / s
+    return hold
+
+
+def steps_on_gpu(u, hold=lambda v, size: v):
+    """steps_of with the default options, in torch's float64."""
+    a, b, c = COEF
+    turned = u.shape[0] > u.shape[1]
+    u = u.T.contiguous() if turned else u
+    x = hold(u / (u.square().sum().sqrt() + EPS), 1.0)
+    for _ in range(5):
+        g = hold(x @ x.T.contiguous(), 1.0)
+        x = hold(a * x + hold(b * g + c * (g @ g), 4.0) @ x, 1.0)
+    return x.T if turned else x
+
+
+# each tile size, a long K that is split, and matrices beside smaller ones
+@gpu
+@pytest.mark.parametrize("name,rows,cols", [("bf16", 4096, 4096), ("bf16", 2900, 3500), ("f32", 2048, 8192), ("f32", 3500, 2900),
+                                            ("f16", 1500, 4100), ("f32", 64, 9000), ("bf16", 20, 6000), ("f32", 300, 8200),
+                                            ("f64", 70, 5000)])
+def test_tile_sizes_and_splits(need_gpu, name, rows, cols):
+    """The model's bounds as above, both computed on the GPU in torch's float64."""
+    g = gradient((rows, cols), TYPES[name], seed=rows + cols)
+    u = g.double()
+    want = steps_on_gpu(u)
+    unit, out = (2.0 ** -53 if name == "f64" else 2.0 ** -24) * math.sqrt(cols) * 4 * 16, 1.01 * OUT_U[name]
+    off = steps_on_gpu(u, _fp16_parts_torch(1 if name == "bf16" else 2)) - want if name != "f64" else 0 * want
+    norm = 3 * off.norm().item() + (out + unit) * want.norm().item() + 3e-8 * math.sqrt(want.numel()) * (name == "f16")
+    each = 3 * off.abs().max().item() + (out + unit) * want.abs().max().item() + 3e-8 * (name == "f16")
+    for v in (g, g.t().contiguous().t()):
+        got = Q.orthogonalize(v).double() - want
+        assert got.norm().item() <= norm and got.abs().max().item() <= each
+    p, m = torch.zeros_like(g), torch.zeros_like(g, dtype=torch.float64 if name == "f64" else torch.float32)
+    Q.muon_step([p], [g], [m], lr=1.0, momentum=0.0)
+    got = p.double() + max(1.0, rows / cols) ** 0.5 * want
+    assert got.norm().item() <= max(1.0, rows / cols) ** 0.5 * norm and got.abs().max().item() <= max(1.0, rows / cols) ** 0.5 * each
+
+
 @gpu
 @pytest.mark.parametrize("name", ["f32", "bf16"])
 @pytest.mark.parametrize("shape", [(3, 10, 20), (2, 3, 40, 30), (5, 100, 140), (40, 70, 66)])
