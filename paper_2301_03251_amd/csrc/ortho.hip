@@ -4,16 +4,20 @@
 //   X = a X + B X.
 //
 // m^2 n + m^3 + 2 m^2 n operations a step (A and A^2 are symmetric: half of
-// each is computed) on m n values: matrix products, bound by the matrix cores
-// for all but small matrices. Those (m <= 64, and X, A and B in one workgroup's
-// LDS) take one launch in fp32; all others of a call run together, tile by
-// tile, in three launches a step.
+// each is computed) on m n values: matrix products. If all matrices of a call
+// are small (m <= 64, and X, A and B fit one workgroup's LDS), they take one
+// launch, bound by its steps' latency; else all run together, tile by tile, in
+// three launches a step: bound by the launches up to some 1000 rows and columns,
+// by the matrix cores beyond.
 //
-// Products of large matrices are fp16 ones summed in fp32. The singular values
-// of X stay below about 1.2 (ortho_bounds), so X, A and B are held in fp16 at
-// powers of two that use its range: in two parts, v = hi + lo (hi hi + hi lo +
-// lo hi keeps 22 bits of every factor), or for much work in bfloat16 in one (11
-// bits, of which the result keeps 8). fp64 uses fp64.
+// Products are fp16 ones summed in fp32. The singular values of X stay below
+// about 1.2 (ortho_bounds), so X, A and B are held in fp16 at powers of two that
+// use its range: in two parts, v = hi + lo (hi hi + hi lo + lo hi keeps 22 bits
+// of every factor, at a third of fp16's rate, five times fp32's), or for much
+// work in bfloat16 in one (11 bits, of which the result keeps 8). What they are
+// held in costs the result less than its own rounding does, and in float32 less
+// than fp32 sums do (2048x8192: 1.9e-6 off, 3.3e-6 with fp32 products). fp64
+// uses fp64.
 #include <algorithm>
 #include <atomic>
 #include <cmath>
@@ -217,8 +221,10 @@ template <typename T> __global__ __launch_bounds__(SMALL_THREADS) void k_ortho_s
 // large ones, X, its transpose and A (then B in its place) in LDS in two parts.
 // Each of the 16 wavefronts (4 for little work) takes a 16x16 tile of A and of
 // B, and 16 columns of X, which nobody else reads or writes until the step's
-// end. 16 matrices of 64x256 take 14 us, against 95 us with the fp32 products
-// above (16x16x4: an eighth of the rate even after three products).
+// end. 16 matrices of 64x256 take 36 us, one of 20x72 17 us: 11 and 7 us of them
+// for reading, the norm and writing, 5 and 2 us a step, which is the way from
+// barrier to barrier of four phases. With the fp32 products above (16x16x4, a
+// sixteenth of the rate) it was 95 and 19 us.
 struct SmallScale {
     float sx, sa, sb;
 };
@@ -598,12 +604,28 @@ template <typename T, int F> __global__ __launch_bounds__(256) void k_ortho_pack
     for (int k = threadIdx.x; k < e.chunks; k += 256) sq += e.part[b * e.chunks + k];
     const double inv = a.scale / (sqrt(group_sum<256>(sq, lds)) + a.r.eps);
     const bool by_row = e.s.gj == 1 || e.s.gi != 1;
+    if constexpr (F == DOUBLE) {
+        for (int k = threadIdx.x; k < 64 * 64; k += 256) {
+            const int i = by_row ? k / 64 : k % 64, j = by_row ? k % 64 : k / 64;
+            tile[i][j] = 0;
+            if (i0 + i < e.m && j0 + j < e.n) tile[i][j] = same_update<T>(e.s, a.r, b, i0 + i, j0 + j) * inv;
+        }
+    } else {  // four elements of a line at a time
+        const int l0 = by_row ? i0 : j0, f0 = by_row ? j0 : i0, lines = by_row ? e.m : e.n, wide = by_row ? e.n : e.m;
+        const int64_t gl = by_row ? e.s.gi : e.s.gj, gs = by_row ? e.s.gj : e.s.gi;
+        const int64_t ml = by_row ? e.s.mi : e.s.mj, ms = by_row ? e.s.mj : e.s.mi;
 #pragma unroll
-    for (int c = 0; c < 16; c++) {
-        const int k = c * 256 + threadIdx.x, i = by_row ? k / 64 : k % 64, j = by_row ? k % 64 : k / 64;
-        double u = 0;
-        if (i0 + i < e.m && j0 + j < e.n) u = (double)same_update<T>(e.s, a.r, b, i0 + i, j0 + j) * inv;
-        tile[i][j] = (R)u;
+        for (int c = 0; c < 4; c++) {
+            const int k = c * 256 + threadIdx.x, l = k / 16, f = k % 16 * 4;
+            const int count = l0 + l < lines ? max(0, min(4, wide - f0 - f)) : 0;
+            float4v u = load_four<T>((const T*)e.s.grad + b * e.s.gb + (l0 + l) * gl + (f0 + f) * gs, gs, count);
+            if (e.s.momentum) {
+                const float4v m = load_four<float>((const float*)e.s.momentum + b * e.s.mb + (l0 + l) * ml + (f0 + f) * ms, ms, count);
+                u = a.r.nesterov ? u + (float)a.r.momentum * m : m;
+            }
+#pragma unroll
+            for (int r = 0; r < 4; r++) (by_row ? tile[l][f + r] : tile[f + r][l]) = (float)((double)u[r] * inv);
+        }
     }
     __syncthreads();
     const Layout l = layout_of(mp, np, unit_of(F));
@@ -696,9 +718,17 @@ template <int READS> __device__ __forceinline__ void spread() {
 #define STAGE(name) __shared__ __attribute__((aligned(16))) char name[2 * BT * 128]
 
 // BT x BT tiles of C, WI x WJ wavefronts. The operands' next 128 bytes of every
-// row are on their way to LDS, STAGES - 1 steps ahead, while the products of a
-// step run. Chunk q (16 bytes) of a row r lies at q ^ (r % 8): the rows that a
-// wavefront reads together start in different banks.
+// row are on their way to LDS, STAGES steps ahead, while the products of a step
+// run. Chunk q (16 bytes) of a row r lies at q ^ (r % 8): the rows that a
+// wavefront reads together start in different banks (no conflicts counted).
+// 256 is the tile whose products (2048 clocks of a unit a step in one part)
+// take as long as its LDS traffic; smaller ones fill the chip where there are
+// fewer tiles than units. Measured: X of 4096x4096 in one part 117 us (1.17
+// PFLOP/s; the clock falls to 2 GHz under it, and lower with inputs of wider
+// spread: 145 us), in two parts of 2048x8192 170 us (0.40 PFLOP/s, 1.2 of fp16
+// products); a step takes 1.49 us of 1.28 for its products alone. What is left is
+// the end: X read, X and X^T written at once by all units. Four wavefronts
+// instead of eight a tile, with fewer LDS reads, took 1.1 to 1.3 times as long.
 template <typename T, int F, int MODE, int SPLIT, int BT, int WI, int WJ, int STAGES>
 __global__ __launch_bounds__(64 * WI * WJ, 2) void k_ortho_gemm(GemmArgs a) {
     constexpr int U = unit_of(F), THREADS = 64 * WI * WJ, TI = BT / WI / 16, TJ = BT / WJ / 16;
