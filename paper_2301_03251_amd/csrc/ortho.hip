@@ -219,10 +219,10 @@ template <typename T> __global__ __launch_bounds__(SMALL_THREADS) void k_ortho_s
 
 // Small matrices of the other types: as above with the fp16 products of the
 // large ones, X, its transpose and A (then B in its place) in LDS in two parts.
-// Each of the 16 wavefronts (4 for little work) takes a 16x16 tile of A and of
-// B, and 16 columns of X, which nobody else reads or writes until the step's
-// end. 16 matrices of 64x256 take 36 us, one of 20x72 17 us: 11 and 7 us of them
-// for reading, the norm and writing, 5 and 2 us a step, which is the way from
+// Each of the 16 wavefronts (8 for little work) takes a 16x16 tile of A and of
+// B, and 16 or 32 columns of X, which nobody else reads or writes until the step's
+// end. 16 matrices of 64x256 take 36 us, one of 20x72 15 us: 11 and 6 us of them
+// for reading, the norm and writing, 5 and 1.8 us a step, which is the way from
 // barrier to barrier of four phases. With the fp32 products above (16x16x4, a
 // sixteenth of the rate) it was 95 and 19 us.
 struct SmallScale {
@@ -408,8 +408,8 @@ template <typename T, int THREADS> __global__ __launch_bounds__(THREADS) void k_
     }
     __syncthreads();
 
-    // tiles of A and B on and below the diagonal: at most 10, three for each of four wavefronts
-    constexpr int TILES_EACH = THREADS / 64 >= 10 ? 1 : 3;
+    // tiles of A and B on and below the diagonal: at most 10
+    constexpr int TILES_EACH = (10 + THREADS / 64 - 1) / (THREADS / 64);
     auto tile_row = [](int t) { return (t > 0) + (t > 2) + (t > 5); };
     const int mt = (m + 15) / 16, nt = (n + 15) / 16, lower = mt * (mt + 1) / 2;
     for (int step = 0; step < a.steps; step++) {
@@ -443,14 +443,15 @@ template <typename T, int THREADS> __global__ __launch_bounds__(THREADS) void k_
             __syncthreads();
         }
         const float f0 = (float)a.a, f1 = 1 / sc.sb;
-        // two columns of tiles at a time: B's rows are read half as often
-        for (int t = 2 * wave; t < nt; t += 2 * waves) {
+        // two columns of tiles at a time where there are many: B's rows are read half as often
+        constexpr int WIDE = THREADS == 1024 ? 2 : 1;
+        for (int t = WIDE * wave; t < nt; t += WIDE * waves) {
             const int j = t * 16 + 4 * part;
-            float4v y[SMALL_M / 16][2] = {};
+            float4v y[SMALL_M / 16][WIDE] = {};
             for (int k = 0; k < mp; k += 32) {
-                half8 ph[2], pl[2];
+                half8 ph[WIDE], pl[WIDE];
 #pragma unroll
-                for (int c = 0; c < 2; c++) {
+                for (int c = 0; c < WIDE; c++) {
                     const _Float16* p = XT + (min(t + c, nt - 1) * 16 + row) * pt + 8 * part + k;
                     ph[c] = *(const half8*)p, pl[c] = *(const half8*)(p + tlow);
                 }
@@ -460,18 +461,18 @@ template <typename T, int THREADS> __global__ __launch_bounds__(THREADS) void k_
                         const _Float16* q = A + (i * 16 + row) * pt + 8 * part + k;
                         const half8 qh = *(const half8*)q, ql = *(const half8*)(q + alow);
 #pragma unroll
-                        for (int c = 0; c < 2; c++) y[i][c] = __builtin_amdgcn_mfma_f32_16x16x32_f16(pl[c], ql, y[i][c], 0, 0, 0);
+                        for (int c = 0; c < WIDE; c++) y[i][c] = __builtin_amdgcn_mfma_f32_16x16x32_f16(pl[c], ql, y[i][c], 0, 0, 0);
 #pragma unroll
-                        for (int c = 0; c < 2; c++) y[i][c] = __builtin_amdgcn_mfma_f32_16x16x32_f16(pl[c], qh, y[i][c], 0, 0, 0);
+                        for (int c = 0; c < WIDE; c++) y[i][c] = __builtin_amdgcn_mfma_f32_16x16x32_f16(pl[c], qh, y[i][c], 0, 0, 0);
 #pragma unroll
-                        for (int c = 0; c < 2; c++) y[i][c] = __builtin_amdgcn_mfma_f32_16x16x32_f16(ph[c], ql, y[i][c], 0, 0, 0);
+                        for (int c = 0; c < WIDE; c++) y[i][c] = __builtin_amdgcn_mfma_f32_16x16x32_f16(ph[c], ql, y[i][c], 0, 0, 0);
 #pragma unroll
-                        for (int c = 0; c < 2; c++) y[i][c] = __builtin_amdgcn_mfma_f32_16x16x32_f16(ph[c], qh, y[i][c], 0, 0, 0);
+                        for (int c = 0; c < WIDE; c++) y[i][c] = __builtin_amdgcn_mfma_f32_16x16x32_f16(ph[c], qh, y[i][c], 0, 0, 0);
                     }
             }
             __builtin_amdgcn_wave_barrier();  // all of the old X^T has been read
 #pragma unroll
-            for (int c = 0; c < 2; c++)
+            for (int c = 0; c < WIDE; c++)
 #pragma unroll
                 for (int i = 0; i < SMALL_M / 16; i++)
                     if (i < mt && t + c < nt) {
@@ -1191,7 +1192,7 @@ template <typename T> hipError_t run_small(const OrthoCall& c, const Rule& rule,
             e = hipGetLastError();
         } else {
             const Scales k = scales_of(c);
-            e = most <= 256 * 8 ? launch_tiny<T, 256>(a, (unsigned)blocks, lds, k, s) : launch_tiny<T, 1024>(a, (unsigned)blocks, lds, k, s);
+            e = most <= 2048 ? launch_tiny<T, 512>(a, (unsigned)blocks, lds, k, s) : launch_tiny<T, 1024>(a, (unsigned)blocks, lds, k, s);
         }
         if (e != hipSuccess) return e;
     }
