@@ -1401,17 +1401,30 @@ template <typename T> hipError_t run(const OrthoCall& c, void* ws, hipStream_t s
 
 bool ortho_bounds(double a, double b, double c, int steps, double& most_x, double& most_q) {
     most_x = 1, most_q = 0;
+    if (!std::isfinite(a) || !std::isfinite(b) || !std::isfinite(c)) return false;
+    // over t = x^2: where p' = a + 3 b t + 5 c t^2 and q' = b + 2 c t vanish
+    double inner[3];
+    int n = 0;
+    const double disc = 9 * b * b - 20 * a * c;
+    if (c != 0) {
+        inner[n++] = -b / (2 * c);
+        if (disc >= 0) inner[n++] = (-3 * b + std::sqrt(disc)) / (10 * c), inner[n++] = (-3 * b - std::sqrt(disc)) / (10 * c);
+    } else if (b != 0) {
+        inner[n++] = -a / (3 * b);
+    }
     double reach = 1;  // singular values lie in [0, reach]
     for (int s = 0; s < steps; s++) {
         double next = 0;
-        for (int k = 0; k <= 1024; k++) {  // a margin of 1/256 covers what lies between two values
-            const double x = reach * k / 1024, q = x * x * (b + c * x * x), v = std::fabs(x * (a + q));
+        for (int k = 0; k <= n; k++) {
+            const double t = k < n ? inner[k] : reach * reach;
+            if (!(t >= 0 && t <= reach * reach)) continue;
+            const double q = t * (b + c * t), v = std::fabs(std::sqrt(t) * (a + q));
             if (!(v <= 1e6) || !(std::fabs(q) <= 1e5)) return false;
             next = std::max(next, v);
             most_q = std::max(most_q, std::fabs(q));
         }
         if (s + 1 == steps) break;  // what the last step gives is not held
-        reach = next * (1 + 1.0 / 256);
+        reach = next * (1 + 1.0 / 256);  // and a margin for the products' rounding
         most_x = std::max(most_x, reach);
         if (reach > 64) return false;
     }
