@@ -404,9 +404,11 @@ int ql_layer_norm_backward(ql_type type, ql_type weight_type, int64_t rows, int6
  * be grad's array in ql_orthogonalize where the strides are equal. All entries of
  * a call run together: give a network's matrices in one call.
  *
- * Precision: QL_F64 in fp64. QL_F32 and QL_F16 products keep 22 bits of every
- * factor (two fp16 parts each, three products) or fp32 ones for small matrices;
- * QL_BF16 products keep 11 (one fp16 part). Sums are fp32, norms fp64.
+ * Precision: QL_F64 in fp64. Other products are fp16 ones that keep 22 bits of
+ * every factor (in two parts), or 11 for calls of QL_BF16 with 5e9 operations or
+ * more in matrices of more than 64 rows. Sums are fp32, norms fp64. A matrix's
+ * last bits can depend on what else the call holds (the tiles follow from all of
+ * it), and nothing else: the same call gives the same bits.
  *
  * options NULL: the defaults in braces. rows, cols in [1, 65536], steps in
  * [1, 64]; coefficients that let a singular value in [0, 1] grow past 64 before

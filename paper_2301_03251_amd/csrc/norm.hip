@@ -173,7 +173,8 @@ template <typename T, typename W> __global__ __launch_bounds__(256) void k_norm_
 // every lane sums its columns' g h and g over the rows that its group takes
 // (row, row + stride, ...). The next row's loads are under way while a row is
 // worked on. part[workgroup][2][D] gets the workgroup's sums, joined over its
-// groups in LDS; a null part leaves them out.
+// groups in LDS; a null part leaves them out. 16384x8192 bf16: 150 us, 5.4 TB/s,
+// a copy's rate (one kernel for dx and one for the columns: 310 us).
 template <typename T, typename W, int V, int G, int K>
 __global__ __launch_bounds__(G > 256 ? G : 256) void k_norm_bwd(NormArgs a) {
     using R = Acc<T>;
@@ -341,7 +342,9 @@ __global__ __launch_bounds__(256) void k_norm_bwd_segment(NormArgs a, int segmen
     store_vec<R, V>(out + a.D, q);
 }
 
-// Sum of the chunks' column sums, in fp64: 16 columns and 16 threads for each.
+// Sum of the workgroups' column sums, in fp64: 16 columns and 16 threads for
+// each, eight loads of a thread under way (4 us for 512 parts of 2x1024 columns,
+// 11 us one by one).
 template <typename T, typename W> __global__ __launch_bounds__(256) void k_norm_reduce(NormArgs a, int64_t chunks) {
     using R = Acc<T>;
     __shared__ double lds[16][17];

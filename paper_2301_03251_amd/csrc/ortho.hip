@@ -774,6 +774,8 @@ __global__ __launch_bounds__(64 * WI * WJ, 2) void k_ortho_gemm(GemmArgs a) {
         const int each = (ld / 128 + a.splits - 1) / a.splits * 128;
         begin = run / all * each, end = min(begin + each, ld);
     }
+    // sums of up to 128 products do not average out what lo lo would add
+    [[maybe_unused]] const bool few = ld <= 512;
     uint32_t lat[LOADS], rat[LOADS];
 #pragma unroll
     for (int c = 0; c < LOADS; c++) {
@@ -846,8 +848,9 @@ __global__ __launch_bounds__(64 * WI * WJ, 2) void k_ortho_gemm(GemmArgs a) {
         arrived(std::integral_constant<int, 2 * LOADS*(STAGES - 2)>{});
         load(now, min(k + 128 * STAGES, end - 128));
         __builtin_amdgcn_sched_barrier(0);
-        if constexpr (F == TWO) {  // hi lo, then lo hi; lo lo where few values do not average it out, and it costs nothing
-            if constexpr (BT == 64) product(p1, q1);
+        if constexpr (F == TWO) {  // hi lo, then lo hi
+            if constexpr (BT == 64)
+                if (few) product(p1, q1);
             product(p, q1);
             __builtin_amdgcn_sched_barrier(0);
             product(p1, q);

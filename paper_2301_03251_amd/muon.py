@@ -127,7 +127,20 @@ def muon_step(params, grads, momenta, lr=0.02, momentum=0.95, nesterov=True, wei
 def _class():
     torch = _torch()
 
+    def wide(p):
+        return torch.float64 if p.dtype == torch.float64 else torch.float32
+
     class MuonOptimizer(torch.optim.Optimizer):
+        def load_state_dict(self, state_dict):
+            """As the base class, which gives state its parameter's dtype; a momentum keeps its own."""
+            super().load_state_dict(state_dict)
+            saved = [i for g in state_dict["param_groups"] for i in g["params"]]
+            held = [p for g in self.param_groups for p in g["params"]]
+            for i, p in zip(saved, held):
+                if "momentum" in state_dict["state"].get(i, {}):
+                    m = state_dict["state"][i]["momentum"]
+                    self.state[p]["momentum"] = m.detach().to(device=p.device, dtype=wide(p), copy=True)
+
         @torch.no_grad()
         def step(self, closure=None):
             loss = None
@@ -141,8 +154,7 @@ def _class():
                         continue
                     state = self.state[p]
                     if not state:
-                        wide = torch.float64 if p.dtype == torch.float64 else torch.float32
-                        state["momentum"] = torch.zeros_like(p, dtype=wide)
+                        state["momentum"] = torch.zeros_like(p, dtype=wide(p))
                     kinds.setdefault((p.device, p.dtype), []).append((p, p.grad, state["momentum"]))
                 for matrices in kinds.values():
                     lists = [[t if group["matrix"] is None else t.view(group["matrix"]) for t in ts]

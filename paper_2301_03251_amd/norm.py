@@ -47,17 +47,18 @@ def _workspace_bytes(type_, rows, features, backward):
 def _rows(t, shape):
     """(tensor, rows, stride between rows) of t's rows along its last axis; a
     copy where they do not lie a fixed stride apart."""
+    n = shape[-1]
     if len(shape) == 2:
         stride, unit = t.stride()
-        if unit == 1 or shape[1] == 1:
+        if unit == 1 or n == 1:
             return t, shape[0], stride
-    n = shape[-1]
-    if not t.is_contiguous():
+    elif not t.is_contiguous() and (n == 1 or t.stride(-1) == 1):
         try:
-            flat = t.view(-1, n)
-            return _rows(flat, flat.shape)
+            t = t.view(-1, n)
+            return t, t.shape[0], t.stride(0)
         except RuntimeError:
-            t = t.contiguous()
+            pass
+    t = t.contiguous()
     return t, t.numel() // n, n
 
 

@@ -420,6 +420,25 @@ def test_optimizer(need_gpu):
 
 
 @gpu
+def test_optimizer_state_is_saved_whole(need_gpu):
+    """A bfloat16 weight's momentum is float32 after saving and loading too."""
+    w = [torch.nn.Parameter(torch.randn(12, 20, device="cuda").bfloat16()) for _ in range(2)]
+    w[1].data.copy_(w[0].data)
+    a, b = Q.Muon([w[0]], lr=0.1), Q.Muon([w[1]], lr=0.1)
+    for turn in range(3):
+        g = torch.randn(12, 20, device="cuda").bfloat16()
+        w[0].grad = g
+        if turn == 2:
+            b.load_state_dict(a.state_dict())
+            w[1].data.copy_(w[0].data)
+            w[1].grad = g.clone()
+            b.step()
+        a.step()
+    assert b.state[w[1]]["momentum"].dtype == torch.float32
+    assert torch.equal(w[0], w[1]) and torch.equal(a.state[w[0]]["momentum"], b.state[w[1]]["momentum"])
+
+
+@gpu
 def test_python_refuses(need_gpu):
     g = torch.randn(8, 12, device="cuda")
     m = torch.zeros_like(g)

@@ -237,6 +237,14 @@ def test_orders_of_axes(need_gpu):
     one = x[:1].expand(24, 40)
     assert torch.equal(Q.layer_norm(one, w, b), want[:1].expand(24, 40))
     assert torch.equal(Q.layer_norm(x[0], w, b), want[0])
+    wide = torch.full((24, 80), float("nan"), device="cuda")
+    wide[:, ::2] = x
+    assert torch.equal(Q.layer_norm(wide[:, ::2], w, b), want) and torch.equal(Q.layer_norm(wide[3, ::2], w, b), want[3])
+    cube = torch.full((2, 12, 41), float("nan"), device="cuda")
+    cube[..., :40] = x.view(2, 12, 40)
+    assert torch.equal(Q.layer_norm(cube[..., :40], w, b).view(24, 40), want)
+    column = x[:, :1]
+    assert torch.equal(Q.layer_norm(column, w[:1], b[:1]), Q.layer_norm(column.contiguous(), w[:1], b[:1]))
     y, mean, rstd = Q.layer_norm_forward(x, w, b)
     a = Q.layer_norm_backward(g[:1].expand(24, 40), x, mean, rstd, w)
     c = Q.layer_norm_backward(g[:1].repeat(24, 1), x, mean, rstd, w)
