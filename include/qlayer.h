@@ -357,8 +357,8 @@ typedef enum { QL_F32 = 0, QL_F64 = 1, QL_BF16 = 2, QL_F16 = 3 } ql_type;
  * weight[features] and bias[features] (weight_type: type, or QL_F32 beside
  * QL_BF16 and QL_F16 rows) may each be NULL (1 and 0). mean[rows] and
  * rstd[rows] (QL_F64 for QL_F64, else QL_F32) are what the backward call needs
- * and may each be NULL. A row that holds an infinity or NaN gives NaN in that
- * row alone. features in [1, 2^30]; rows = 0 does nothing.
+ * and may each be NULL. A row that holds an infinity or NaN, or with
+ * eps = 0 no variance, gives NaN in that row alone. features in [1, 2^30]; rows = 0 does nothing.
  *
  * The backward call: with h = (x - mean) * rstd,
  *   grad_x      = rstd * (g w - mean(g w) - h * mean(g w h)),
@@ -389,8 +389,8 @@ int ql_layer_norm_backward(ql_type type, ql_type weight_type, int64_t rows, int6
  * rows than columns, then `steps` times
  *   A = X X^T,   X = a X + (b A + c A^2) X,
  * which takes every singular value s of X through a s + b s^3 + c s^5 towards 1
- * and leaves the singular vectors. A matrix of zeros gives zeros; one that holds
- * an infinity or NaN gives NaN throughout.
+ * and leaves the singular vectors. A matrix of zeros gives zeros (NaN with eps
+ * = 0); one that holds an infinity or NaN gives NaN throughout.
  *
  * ql_orthogonalize: U = grad, out = O.
  * ql_muon_step: momentum = mu * momentum + grad, U = grad + mu * momentum (with
