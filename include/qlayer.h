@@ -357,8 +357,9 @@ typedef enum { QL_F32 = 0, QL_F64 = 1, QL_BF16 = 2, QL_F16 = 3 } ql_type;
  * weight[features] and bias[features] (weight_type: type, or QL_F32 beside
  * QL_BF16 and QL_F16 rows) may each be NULL (1 and 0). mean[rows] and
  * rstd[rows] (QL_F64 for QL_F64, else QL_F32) are what the backward call needs
- * and may each be NULL. A row that holds an infinity or NaN, or with
- * eps = 0 no variance, gives NaN in that row alone. features in [1, 2^30]; rows = 0 does nothing.
+ * and may each be NULL. A row that holds an infinity or NaN, or with eps = 0 no
+ * variance, gives NaN in that row alone. features in [1, 2^30]; rows = 0 does
+ * nothing.
  *
  * The backward call: with h = (x - mean) * rstd,
  *   grad_x      = rstd * (g w - mean(g w) - h * mean(g w h)),
