@@ -94,6 +94,7 @@ def muon_step(params, grads, momenta, lr=0.02, momentum=0.95, nesterov=True, wei
     t, device, dtype = type_of(first, "params"), first.device, first.dtype
     state = torch.float64 if dtype == torch.float64 else torch.float32
     words, shapes = [], []
+    held = []  # copies of gradients, whose memory is theirs until the launch
     for p, g, m in zip(params, grads, momenta):
         if not p.is_cuda or p.dim() < 2 or p.dtype != dtype or p.device != device:
             raise ValueError("params must be CUDA tensors [..., rows, cols] of one dtype on one device")
@@ -109,7 +110,9 @@ def muon_step(params, grads, momenta, lr=0.02, momentum=0.95, nesterov=True, wei
             words += (rows, cols, 1, g.data_ptr(), 0, *g.stride(), m.data_ptr(), 0, *m.stride(), p.data_ptr(), 0,
                       *p.stride())
         else:
-            g = g.reshape(-1, *g.shape[-2:]) if g.dim() > 3 else g
+            if g.dim() > 3:
+                g = g.reshape(-1, *g.shape[-2:])
+                held.append(g)
             m, p = _batched(m), _batched(p)
             batch, rows, cols = p.shape
             shapes.append((rows, cols, batch))
