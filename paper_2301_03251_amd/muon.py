@@ -38,9 +38,30 @@ def _workspace_bytes(type_, shapes):
     return out.value
 
 
-def _batched(t):
-    """t as [batch, rows, cols], without a copy."""
-    return t.unsqueeze(0) if t.dim() == 2 else t if t.dim() == 3 else t.view(-1, *t.shape[-2:])
+def _viewed(t):
+    """t as [batch, rows, cols] without a copy; None where its leading axes do not collapse."""
+    if t.dim() < 4:
+        return t if t.dim() == 3 else t.unsqueeze(0)
+    try:
+        return t.view(-1, *t.shape[-2:])
+    except RuntimeError:
+        return None
+
+
+def _readable(t):
+    """t, or a copy of it whose leading axes collapse."""
+    return t.contiguous() if _viewed(t) is None else t
+
+
+def _batches(*tensors):
+    """The tensors' matrices as views [batch, rows, cols] in step: one of all of
+    them, or one for each index of the first axis where they do not collapse."""
+    views = [_viewed(t) for t in tensors]
+    if all(v is not None for v in views):
+        yield views
+    else:
+        for parts in zip(*tensors):
+            yield from _batches(*parts)
 
 
 def _run(call, type_, words, shapes, device, *options):
@@ -67,11 +88,12 @@ def orthogonalize(g, steps=5, coefficients=COEFFICIENTS, eps=1e-7, out=None):
     if g.numel() == 0:
         return out
     with torch.cuda.device_of(g):
-        q = g.reshape(-1, *g.shape[-2:]) if g.dim() > 3 else _batched(g)
-        o = _batched(out)
-        batch, rows, cols = q.shape
-        words = array.array("q", (rows, cols, batch, q.data_ptr(), *q.stride(), 0, 0, 0, 0, o.data_ptr(), *o.stride()))
-        _run(load().ql_orthogonalize, t, words, ((rows, cols, batch),), g.device,
+        g, words, shapes = _readable(g), array.array("q"), []
+        for q, o in _batches(g, out):
+            batch, rows, cols = q.shape
+            shapes.append((rows, cols, batch))
+            words.extend((rows, cols, batch, q.data_ptr(), *q.stride(), 0, 0, 0, 0, o.data_ptr(), *o.stride()))
+        _run(load().ql_orthogonalize, t, words, shapes, g.device,
              _options(int(steps), tuple(coefficients), float(eps)))
     return out
 
@@ -110,14 +132,12 @@ def muon_step(params, grads, momenta, lr=0.02, momentum=0.95, nesterov=True, wei
             words += (rows, cols, 1, g.data_ptr(), 0, *g.stride(), m.data_ptr(), 0, *m.stride(), p.data_ptr(), 0,
                       *p.stride())
         else:
-            if g.dim() > 3:
-                g = g.reshape(-1, *g.shape[-2:])
-                held.append(g)
-            m, p = _batched(m), _batched(p)
-            batch, rows, cols = p.shape
-            shapes.append((rows, cols, batch))
-            words += (rows, cols, batch, g.data_ptr(), *g.stride(), m.data_ptr(), *m.stride(), p.data_ptr(),
-                      *p.stride())
+            held.append(_readable(g))
+            for gb, mb, pb in _batches(held[-1], m, p):
+                batch, rows, cols = pb.shape
+                shapes.append((rows, cols, batch))
+                words += (rows, cols, batch, gb.data_ptr(), *gb.stride(), mb.data_ptr(), *mb.stride(), pb.data_ptr(),
+                          *pb.stride())
     if not shapes:
         return
     with torch.cuda.device_of(first):

@@ -87,6 +87,21 @@ def test_every_gradient_is_there_when_the_step_is_launched(arrays, order):
         assert np.array_equal(e["grad"], want.as_subclass(torch.Tensor).reshape(-1, 3, 3).numpy())
 
 
+@pytest.mark.parametrize("order", ["channels_last", "permuted"])
+def test_leading_axes_that_do_not_collapse(arrays, order):
+    """Weights, momenta and outputs are written where they lie, each matrix once."""
+    torch.manual_seed(0)
+    shape = (6, 5, 3, 4)
+    p, g, m, o = (orders(order, shape) for _ in range(4))
+    muon.muon_step([posing(p)], [posing(g)], [posing(m)])
+    for name, t in (("grad", g), ("momentum", m), ("out", p)):
+        assert np.array_equal(np.concatenate([e[name] for e in arrays.entries]), t.reshape(-1, 3, 4).numpy())
+    arrays.entries.clear()
+    assert muon.orthogonalize(posing(g), out=posing(o)).data_ptr() == o.data_ptr()
+    for name, t in (("grad", g), ("out", o)):
+        assert np.array_equal(np.concatenate([e[name] for e in arrays.entries]), t.reshape(-1, 3, 4).numpy())
+
+
 # ---------------------------------------------------------------------------
 # results
 
@@ -114,3 +129,26 @@ def test_gradients_of_any_order(need_gpu, order, beside):
     Q.muon_step(p, g, m)
     Q.muon_step(q, [t.contiguous() for t in g], n)
     assert all(torch.equal(a, b) for a, b in zip(p + m, q + n))
+
+
+@gpu
+@pytest.mark.parametrize("order", ["channels_last", "permuted"])
+def test_weights_of_any_order(need_gpu, order):
+    torch.manual_seed(2)
+    shape = (6, 5, 3, 4)
+    p, g, m = ([orders(order, shape, "cuda") for _ in range(2)] for _ in range(3))
+    q, h, n = ([t.contiguous() for t in ts] for ts in (p, g, m))
+    Q.muon_step(p, g, m)
+    Q.muon_step(q, h, n)
+    assert all(torch.equal(a, b) for a, b in zip(p + m, q + n))
+    out = orders(order, shape, "cuda")
+    assert Q.orthogonalize(g[0], out=out) is out
+    assert torch.equal(out, Q.orthogonalize(h[0]))
+    assert torch.equal(Q.orthogonalize(g[0], out=g[0]), out)
+    w = torch.nn.Parameter(orders(order, shape, "cuda"))
+    w.grad = orders("expanded", shape, "cuda")
+    opt = Q.Muon([w], lr=0.1)
+    want, state = w.detach().contiguous(), torch.zeros(shape, device="cuda")
+    opt.step()
+    Q.muon_step([want], [w.grad.contiguous()], [state], lr=0.1)
+    assert torch.equal(w, want)
