@@ -37,6 +37,12 @@ def on_device(index):
     return None if index == torch.cuda.current_device() else torch.cuda.device(index)
 
 
+def has_tangent(*tensors):
+    """Whether forward mode carries a derivative of one of them (None: no)."""
+    fwd = _torch().autograd.forward_ad
+    return fwd._current_level >= 0 and any(t is not None and fwd.unpack_dual(t).tangent is not None for t in tensors)
+
+
 @functools.lru_cache(maxsize=1024)
 def _workspace_bytes(type_, rows, features, backward):
     out = ctypes.c_size_t()
@@ -77,7 +83,8 @@ def _check_rows(x):
 
 def layer_norm_forward(x, weight=None, bias=None, eps=1e-5, stats=True):
     """(y, mean, rstd) of the rows along x's last axis; mean and rstd (what
-    ``layer_norm_backward`` takes) are None without ``stats``."""
+    ``layer_norm_backward`` takes) are None without ``stats``. Autograd does not
+    see the call: ``layer_norm`` is the differentiable one."""
     device, shape, xt = _check_rows(x)
     n, wt = shape[-1], xt
     if weight is not None:
@@ -107,7 +114,8 @@ def layer_norm_backward(grad_y, x, mean, rstd, weight=None, want_x=True, want_we
                         weight_dtype=None):
     """(grad_x, grad_weight, grad_bias) from the forward's x, mean and rstd;
     None for each that is not wanted. The gradients of weight and bias have
-    weight's dtype (``weight_dtype``, default x's, without a weight)."""
+    weight's dtype (``weight_dtype``, default x's, without a weight). Autograd
+    does not see the call."""
     device, shape, xt = _check_rows(x)
     n = shape[-1]
     if weight is not None:
@@ -163,11 +171,12 @@ def _function():
 
 def layer_norm(x, weight=None, bias=None, eps=1e-5):
     """Layer norm over x's last axis (CUDA tensor [..., features] of float32,
-    float64, bfloat16 or float16), differentiable in x, weight and bias.
-    weight and bias have x's dtype, or are float32 beside 16-bit rows."""
+    float64, bfloat16 or float16), differentiable once in x, weight and bias, in
+    reverse mode (forward mode raises). weight and bias have x's dtype, or are
+    float32 beside 16-bit rows."""
     torch = _torch()
-    if torch.is_grad_enabled() and (x.requires_grad or (weight is not None and weight.requires_grad)
-                                    or (bias is not None and bias.requires_grad)):
+    if (torch.is_grad_enabled() and (x.requires_grad or (weight is not None and weight.requires_grad)
+                                     or (bias is not None and bias.requires_grad))) or has_tangent(x, weight, bias):
         return _function().apply(x, weight, bias, eps)
     return layer_norm_forward(x, weight, bias, eps, stats=False)[0]
 

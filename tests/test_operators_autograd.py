@@ -1,0 +1,64 @@
+"""What autograd sees of the operators around a quantum layer: tangents of
+forward mode, vmap, and writes to tensors that a graph has saved. The dispatch
+is checked on the CPU with the kernels' part replaced, the rest needs an MI355X."""
+
+from __future__ import annotations
+
+import pytest
+
+torch = pytest.importorskip("torch")
+import torch.autograd.forward_ad as fwd  # noqa: E402
+
+import paper_2301_03251_amd as Q  # noqa: E402
+from paper_2301_03251_amd import norm  # noqa: E402
+
+gpu = pytest.mark.gpu
+
+
+@pytest.fixture
+def need_gpu():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    Q.load()
+
+
+@pytest.fixture
+def plain_forward(monkeypatch):
+    def forward(x, weight=None, bias=None, eps=1e-5, stats=True):
+        return x.detach().clone(), x.detach()[..., 0], x.detach()[..., 0]
+    monkeypatch.setattr(norm, "layer_norm_forward", forward)
+
+
+def lost_tangent(device, which, grad):
+    """layer_norm of a dual tensor has no tangent to give: it says so."""
+    ts = [torch.randn(3, 4, device=device), torch.randn(4, device=device), torch.randn(4, device=device)]
+    with torch.set_grad_enabled(grad), fwd.dual_level():
+        ts[which] = fwd.make_dual(ts[which], torch.ones_like(ts[which]))
+        with pytest.raises(RuntimeError, match="forward mode AD"):
+            Q.layer_norm(*ts)
+        ts[which] = fwd.unpack_dual(ts[which]).primal
+        Q.layer_norm(*ts)  # no tangent, no error
+
+
+@pytest.mark.parametrize("which", [0, 1, 2])
+@pytest.mark.parametrize("grad", [True, False])
+def test_a_tangent_is_not_dropped(plain_forward, which, grad):
+    lost_tangent("cpu", which, grad)
+
+
+@gpu
+@pytest.mark.parametrize("which", [0, 1, 2])
+@pytest.mark.parametrize("grad", [True, False])
+def test_a_tangent_is_not_dropped_on_the_gpu(need_gpu, which, grad):
+    lost_tangent("cuda", which, grad)
+
+
+@gpu
+def test_transforms_are_refused(need_gpu):
+    x = torch.randn(3, 4, 5, device="cuda")
+    with pytest.raises(RuntimeError):
+        torch.func.vmap(Q.layer_norm)(x)
+    with pytest.raises(RuntimeError):
+        torch.func.jvp(Q.layer_norm, (x,), (x,))
+    with pytest.raises(RuntimeError):
+        torch.func.grad(lambda t: Q.layer_norm(t).sum())(x)
