@@ -64,6 +64,11 @@ def _batches(*tensors):
             yield from _batches(*parts)
 
 
+def _written(tensors):
+    """Tells autograd of writes to the tensors, as torch's own in-place operations do."""
+    _torch().autograd.graph.increment_version([t for t in tensors if not t.is_inference()])
+
+
 def _run(call, type_, words, shapes, device, *options):
     torch = _torch()
     need = _workspace_bytes(type_, tuple(shapes))
@@ -78,7 +83,7 @@ def orthogonalize(g, steps=5, coefficients=COEFFICIENTS, eps=1e-7, out=None):
     singular values taken towards 1 by ``steps`` Newton-Schulz steps. ``out``
     may be g."""
     torch = _torch()
-    t = type_of(g, "g")
+    t, given = type_of(g, "g"), out
     if not g.is_cuda or g.dim() < 2:
         raise ValueError("g must be a CUDA tensor [..., rows, cols]")
     if out is None:
@@ -95,6 +100,8 @@ def orthogonalize(g, steps=5, coefficients=COEFFICIENTS, eps=1e-7, out=None):
             words.extend((rows, cols, batch, q.data_ptr(), *q.stride(), 0, 0, 0, 0, o.data_ptr(), *o.stride()))
         _run(load().ql_orthogonalize, t, words, shapes, g.device,
              _options(int(steps), tuple(coefficients), float(eps)))
+    if given is not None:
+        _written((given,))
     return out
 
 
@@ -143,7 +150,7 @@ def muon_step(params, grads, momenta, lr=0.02, momentum=0.95, nesterov=True, wei
     with torch.cuda.device_of(first):
         _run(load().ql_muon_step, t, array.array("q", words), shapes, device,
              _Muon(lr, momentum, weight_decay, bool(nesterov)), _options(int(steps), tuple(coefficients), float(eps)))
-    torch.autograd.graph.increment_version(tuple(params) + tuple(momenta))
+    _written((*params, *momenta))
 
 
 @functools.lru_cache(maxsize=None)

@@ -10,7 +10,7 @@ torch = pytest.importorskip("torch")
 import torch.autograd.forward_ad as fwd  # noqa: E402
 
 import paper_2301_03251_amd as Q  # noqa: E402
-from paper_2301_03251_amd import norm  # noqa: E402
+from paper_2301_03251_amd import muon, norm  # noqa: E402
 
 gpu = pytest.mark.gpu
 
@@ -62,3 +62,56 @@ def test_transforms_are_refused(need_gpu):
         torch.func.jvp(Q.layer_norm, (x,), (x,))
     with pytest.raises(RuntimeError):
         torch.func.grad(lambda t: Q.layer_norm(t).sum())(x)
+
+
+class Posing(torch.Tensor):
+    """A CPU tensor that passes the binding's checks for a GPU's."""
+
+    is_cuda = True
+
+
+class Idle:
+    """In the library's place: entries that do nothing."""
+
+    def ql_orthogonalize(self, *_):
+        return 0
+
+    ql_muon_step = ql_orthogonalize
+
+
+@pytest.fixture
+def idle(monkeypatch):
+    monkeypatch.setattr(muon, "load", Idle)
+    monkeypatch.setattr(muon, "_stream", lambda device: None)
+    monkeypatch.setattr(muon, "_workspace_bytes", lambda type_, shapes: 0)
+
+
+def saved_out_is_seen(make):
+    """out= is a write like any in place: a graph that has saved the array says so."""
+    w = make(6, 4)
+    for out_is_input in (False, True):
+        y = (torch.ones(6, 4, device=w.device, requires_grad=True) * w).sum()
+        version = w._version
+        Q.orthogonalize(w if out_is_input else make(6, 4), out=w)
+        assert w._version > version
+        with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+            y.backward()
+
+
+def inference_tensors(make):
+    """They have no version to count."""
+    with torch.inference_mode():
+        p, g, m = make(6, 4), make(6, 4), make(6, 4)
+        Q.muon_step([p], [g], [m])
+        assert Q.orthogonalize(g, out=p) is p
+
+
+def test_orthogonalize_is_seen_by_autograd(idle):
+    saved_out_is_seen(lambda *s: torch.randn(s).as_subclass(Posing))
+    inference_tensors(lambda *s: torch.randn(s).as_subclass(Posing))
+
+
+@gpu
+def test_orthogonalize_is_seen_by_autograd_on_the_gpu(need_gpu):
+    saved_out_is_seen(lambda *s: torch.randn(s, device="cuda"))
+    inference_tensors(lambda *s: torch.randn(s, device="cuda"))
