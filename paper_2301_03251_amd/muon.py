@@ -9,7 +9,7 @@ import array
 import ctypes
 import functools
 
-from .norm import type_of
+from .norm import has_tangent, type_of
 from .qlayer import _check, _stream, _torch, load
 
 COEFFICIENTS = (3.4445, -4.7750, 2.0315)
@@ -81,11 +81,13 @@ def orthogonalize(g, steps=5, coefficients=COEFFICIENTS, eps=1e-7, out=None):
     """The orthogonalised update of g [..., rows, cols] (CUDA tensor of float32,
     float64, bfloat16 or float16, any strides): g / (|g|_F + eps) with its
     singular values taken towards 1 by ``steps`` Newton-Schulz steps. ``out``
-    may be g."""
+    may be g. Not differentiable: refused where autograd would follow it."""
     torch = _torch()
     t, given = type_of(g, "g"), out
     if not g.is_cuda or g.dim() < 2:
         raise ValueError("g must be a CUDA tensor [..., rows, cols]")
+    if (torch.is_grad_enabled() and (g.requires_grad or (out is not None and out.requires_grad))) or has_tangent(g, out):
+        raise ValueError("orthogonalize is not differentiable: detach its tensors or call it under torch.no_grad()")
     if out is None:
         out = torch.empty(g.shape, dtype=g.dtype, device=g.device)
     elif out.shape != g.shape or out.dtype != g.dtype or out.device != g.device:
@@ -113,7 +115,8 @@ def muon_step(params, grads, momenta, lr=0.02, momentum=0.95, nesterov=True, wei
         m = momentum * m + g,  u = g + momentum * m (nesterov; else m)
         p = (1 - lr * weight_decay) * p - lr * sqrt(max(1, rows / cols)) * orthogonalize(u)
 
-    ``momenta`` are float32 (float64 for float64 weights)."""
+    ``momenta`` are float32 (float64 for float64 weights). Autograd does not
+    follow the step."""
     torch = _torch()
     if not len(params) == len(grads) == len(momenta):
         raise ValueError("params, grads and momenta must be lists of the same length")

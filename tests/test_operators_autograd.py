@@ -106,12 +106,34 @@ def inference_tensors(make):
         assert Q.orthogonalize(g, out=p) is p
 
 
+def graph_is_not_dropped(make):
+    """What autograd would have to follow is refused; under no_grad and detached it runs."""
+    g = make(6, 4).requires_grad_()
+    for call in (lambda: Q.orthogonalize(g), lambda: Q.orthogonalize(g * 2), lambda: Q.orthogonalize(make(6, 4), out=g)):
+        with pytest.raises(ValueError, match="not differentiable"):
+            call()
+    with fwd.dual_level(), pytest.raises(ValueError, match="not differentiable"):
+        Q.orthogonalize(fwd.make_dual(make(6, 4), make(6, 4)))
+    assert not Q.orthogonalize(g.detach()).requires_grad
+    with torch.no_grad():
+        assert not Q.orthogonalize(g).requires_grad
+
+
 def test_orthogonalize_is_seen_by_autograd(idle):
     saved_out_is_seen(lambda *s: torch.randn(s).as_subclass(Posing))
     inference_tensors(lambda *s: torch.randn(s).as_subclass(Posing))
+
+
+def test_orthogonalize_does_not_drop_a_graph(idle):
+    graph_is_not_dropped(lambda *s: torch.randn(s).as_subclass(Posing))
 
 
 @gpu
 def test_orthogonalize_is_seen_by_autograd_on_the_gpu(need_gpu):
     saved_out_is_seen(lambda *s: torch.randn(s, device="cuda"))
     inference_tensors(lambda *s: torch.randn(s, device="cuda"))
+
+
+@gpu
+def test_orthogonalize_does_not_drop_a_graph_on_the_gpu(need_gpu):
+    graph_is_not_dropped(lambda *s: torch.randn(s, device="cuda"))
