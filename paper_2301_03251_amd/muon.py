@@ -49,8 +49,14 @@ def _viewed(t):
 
 
 def _readable(t):
-    """t, or a copy of it whose leading axes collapse."""
-    return t.contiguous() if _viewed(t) is None else t
+    """t, or a copy of it whose leading axes collapse and whose memory holds its values."""
+    t = t.resolve_neg()
+    return t.contiguous() if t.dim() > 3 and _viewed(t) is None else t
+
+
+def _writable(t, what):
+    if t.is_neg():
+        raise ValueError(f"{what} must not be a view of negatives")
 
 
 def _batches(*tensors):
@@ -92,6 +98,8 @@ def orthogonalize(g, steps=5, coefficients=COEFFICIENTS, eps=1e-7, out=None):
         out = torch.empty(g.shape, dtype=g.dtype, device=g.device)
     elif out.shape != g.shape or out.dtype != g.dtype or out.device != g.device:
         raise ValueError("out must have g's shape, dtype and device")
+    else:
+        _writable(out, "out")
     if g.numel() == 0:
         return out
     with torch.cuda.device_of(g):
@@ -134,16 +142,19 @@ def muon_step(params, grads, momenta, lr=0.02, momentum=0.95, nesterov=True, wei
             raise ValueError("a gradient must have its parameter's shape, dtype and device")
         if m.shape != p.shape or m.dtype != state or m.device != device:
             raise ValueError(f"a momentum must be {state}, of its parameter's shape and device")
+        _writable(p, "a parameter")
+        _writable(m, "a momentum")
         if p.numel() == 0:
             continue
+        g = _readable(g)
+        held.append(g)
         if p.dim() == 2:
             rows, cols = p.shape
             shapes.append((rows, cols, 1))
             words += (rows, cols, 1, g.data_ptr(), 0, *g.stride(), m.data_ptr(), 0, *m.stride(), p.data_ptr(), 0,
                       *p.stride())
         else:
-            held.append(_readable(g))
-            for gb, mb, pb in _batches(held[-1], m, p):
+            for gb, mb, pb in _batches(g, m, p):
                 batch, rows, cols = pb.shape
                 shapes.append((rows, cols, batch))
                 words += (rows, cols, batch, gb.data_ptr(), *gb.stride(), mb.data_ptr(), *mb.stride(), pb.data_ptr(),

@@ -54,6 +54,8 @@ def _rows(t, shape):
     """(tensor, rows, stride between rows) of t's rows along its last axis; a
     copy where they do not lie a fixed stride apart."""
     n = shape[-1]
+    if n == 1:  # with more features a view of negatives has no unit stride and is copied
+        t = t.resolve_neg()
     if len(shape) == 2:
         stride, unit = t.stride()
         if unit == 1 or n == 1:
@@ -69,7 +71,7 @@ def _rows(t, shape):
 
 
 def _parameter(p, device, n, what):
-    if p.dim() != 1 or p.shape[0] != n or p.get_device() != device or not p.is_contiguous():
+    if p.dim() != 1 or p.shape[0] != n or p.get_device() != device or not p.is_contiguous() or p.is_neg():
         raise ValueError(f"{what} must be a contiguous tensor [{n}] on x's device")
     return type_of(p, what)
 
