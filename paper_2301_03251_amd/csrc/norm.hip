@@ -344,24 +344,30 @@ __global__ __launch_bounds__(256) void k_norm_bwd_segment(NormArgs a, int segmen
 
 // Sum of the workgroups' column sums, in fp64: 16 columns and 16 threads for
 // each, eight loads of a thread under way (4 us for 512 parts of 2x1024 columns,
-// 11 us one by one).
+// 11 us one by one). A launch's threads number less than 2^32: columns past the
+// grid's go around.
+constexpr int64_t REDUCE_BLOCKS = 65536;
+
 template <typename T, typename W> __global__ __launch_bounds__(256) void k_norm_reduce(NormArgs a, int64_t chunks) {
     using R = Acc<T>;
     __shared__ double lds[16][17];
     const int c = threadIdx.x % 16, g = threadIdx.x / 16;
-    const int64_t col = (int64_t)blockIdx.x * 16 + c;  // of 2 D
-    double t = 0;
-    if (col < 2 * a.D)
+    for (int64_t first = (int64_t)blockIdx.x * 16; first < 2 * a.D; first += (int64_t)gridDim.x * 16) {
+        const int64_t col = first + c;  // of 2 D
+        double t = 0;
+        if (col < 2 * a.D)
 #pragma unroll 8
-        for (int64_t k = g; k < chunks; k += 16) t += (double)((const R*)a.part)[k * 2 * a.D + col];
-    lds[g][c] = t;
-    __syncthreads();
-    if (g == 0 && col < 2 * a.D) {
-        t = 0;
+            for (int64_t k = g; k < chunks; k += 16) t += (double)((const R*)a.part)[k * 2 * a.D + col];
+        __syncthreads();
+        lds[g][c] = t;
+        __syncthreads();
+        if (g == 0 && col < 2 * a.D) {
+            t = 0;
 #pragma unroll
-        for (int i = 0; i < 16; i++) t += lds[i][c];
-        W* out = (W*)(col < a.D ? a.grad_weight : a.grad_bias);
-        if (out) out[col < a.D ? col : col - a.D] = down<W>((Acc<W>)t);
+            for (int i = 0; i < 16; i++) t += lds[i][c];
+            W* out = (W*)(col < a.D ? a.grad_weight : a.grad_bias);
+            if (out) out[col < a.D ? col : col - a.D] = down<W>((Acc<W>)t);
+        }
     }
 }
 
@@ -468,7 +474,7 @@ template <typename T, typename W> hipError_t backward(int type, NormArgs a, hipS
             e = hipGetLastError();
     }
     if (e != hipSuccess || !columns) return e;
-    k_norm_reduce<T, W><<<(unsigned)((2 * a.D + 15) / 16), 256, 0, s>>>(a, p.parts);
+    k_norm_reduce<T, W><<<(unsigned)std::min((2 * a.D + 15) / 16, REDUCE_BLOCKS), 256, 0, s>>>(a, p.parts);
     return hipGetLastError();
 }
 
