@@ -1409,11 +1409,11 @@ bool ortho_bounds(double a, double b, double c, int steps, double& most_x, doubl
     double inner[3];
     int n = 0;
     const double disc = 9 * b * b - 20 * a * c;
-    if (c != 0) {
-        inner[n++] = -b / (2 * c);
-        if (disc >= 0) inner[n++] = (-3 * b + std::sqrt(disc)) / (10 * c), inner[n++] = (-3 * b - std::sqrt(disc)) / (10 * c);
-    } else if (b != 0) {
-        inner[n++] = -a / (3 * b);
+    if (c != 0) inner[n++] = -b / (2 * c);
+    if (disc >= 0) {  // both roots without a difference of nearly equal numbers
+        const double h = -(3 * b + std::copysign(std::sqrt(disc), b)) / 2;
+        if (c != 0) inner[n++] = h / (5 * c);
+        if (h != 0) inner[n++] = a / h;
     }
     double reach = 1;  // singular values lie in [0, reach]
     for (int s = 0; s < steps; s++) {

@@ -65,3 +65,31 @@ def test_norm_of_very_long_rows(need_gpu, n):
         size[1] += gr.abs()
     within(gw, sums[0], slack + 8 * u * size[0], "grad_weight")
     within(gb, sums[1], 8 * u * size[1], "grad_bias")
+
+
+class Ortho(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_double) for n in ("a", "b", "c", "eps")] + [("steps", ctypes.c_int32)]
+
+
+class Step(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_double) for n in ("lr", "momentum", "weight_decay")] + [("nesterov", ctypes.c_int32)]
+
+
+FAKE = 0x1000
+
+
+def orthogonalize(entries, type_=F32, ortho=None, ws=None, ws_bytes=0):
+    words = array.array("q", [v for r, c, b in entries for v in (r, c, b, FAKE, r * c, c, 1, 0, 0, 0, 0, FAKE, r * c, c, 1)])
+    return Q.load().ql_orthogonalize(type_, words.buffer_info()[0], len(entries),
+                                     ctypes.byref(ortho) if ortho is not None else None, ws, ws_bytes, None)
+
+
+@pytest.mark.parametrize("a,b,c", [(-200.0, 200.0, 1e-16), (30.0, -30.0, 1e-17), (-30.0, 30.0, -1e-17), (200.0, -200.0, 0.0)])
+def test_growth_between_zero_and_one_is_seen(a, b, c):
+    """a x + b x^3 is 0 at both ends of [0, 1], and past 64 or a few steps from it
+    between them: the two roots of its slope may differ by 16 orders of magnitude."""
+    reach = 1.0
+    for _ in range(3):
+        reach = max(abs(x * (a + x * x * (b + c * x * x))) for x in (reach * i / 1000 for i in range(1001)))
+    assert reach > 64
+    assert orthogonalize([(200, 300, 1)], ortho=Ortho(a, b, c, 1e-7, 4), ws=FAKE, ws_bytes=1 << 40) == -1
