@@ -21,7 +21,7 @@ ROOT = os.path.dirname(PKG)
 CSRC = os.path.join(PKG, "csrc")
 BUILD = os.path.join(ROOT, "_build")
 LIB = os.path.join(PKG, "libqlayer.so")
-SOURCES = ["tile.hip", "kernels.hip", "runs.hip", "norm.hip", "ortho.hip", "api.cpp", "ops_api.cpp", "plan.cpp", "runs.cpp"]
+SOURCES = ["tile.hip", "kernels.hip", "runs.hip", "norm.hip", "ortho.hip", "api.cpp", "ops_api.cpp", "plan.cpp", "runs.cpp", "ortho_plan.cpp"]
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 ARCH = "gfx950"
@@ -43,7 +43,7 @@ def _compile(src: str) -> str:
     cmd = [HIPCC, *COMMON, "-c", os.path.join(CSRC, src), "-o", obj]
     if src.endswith(".hip"):
         cmd[1:1] = ["-x", "hip", *DEVICE, *SOURCE_FLAGS.get(src, [])]
-    elif src in ("api.cpp", "ops_api.cpp"):
+    elif src in ("api.cpp", "ops_api.cpp", "ortho_plan.cpp"):
         cmd[1:1] = ["-x", "hip", *DEVICE]
     else:
         cmd[1:1] = ["-x", "c++"]

@@ -25,7 +25,7 @@
 
 #include "elem.hpp"
 #include "norm.hpp"
-#include "ortho.hpp"
+#include "ortho_plan.hpp"
 
 namespace qlayer {
 namespace {
@@ -33,8 +33,6 @@ namespace {
 typedef _Float16 half8 __attribute__((ext_vector_type(8)));
 typedef float float4v __attribute__((ext_vector_type(4)));
 typedef double double4v __attribute__((ext_vector_type(4)));
-
-constexpr int ENTRIES = 24;  // of a launch's table, which is a kernel argument (4 KiB at most)
 
 // ---------------------------------------------------------------------------
 // The update U of one matrix, oriented so that rows i are the shorter side.
@@ -125,16 +123,6 @@ struct SmallArgs {
     double a, b, c;
     int32_t count, steps;
 };
-
-constexpr int SMALL_M = 64, SMALL_THREADS = 512;
-
-__host__ __device__ constexpr int up16(int v) { return (v + 15) / 16 * 16; }
-// Leading dimensions: four words past a multiple of 16, so that the 16 rows of
-// an operand start in different banks.
-size_t small_lds(int m, int n, size_t size) {
-    return size * ((size_t)up16(m) * (up16(n) + 4) + 2 * (size_t)up16(m) * (up16(m) + 4));
-}
-constexpr int SMALL_LDS = 160 * 1024 - SMALL_THREADS / 64 * 8;  // with the norm's sums
 
 template <typename T> __global__ __launch_bounds__(SMALL_THREADS) void k_ortho_small(SmallArgs a) {
     using R = Acc<T>;
@@ -290,8 +278,6 @@ __device__ __forceinline__ void put_turned(_Float16* p, int pitch, int behind, i
     *(half4*)(q + behind) = turn4(low(v, hi));
 }
 
-__host__ __device__ constexpr int up32(int v) { return (v + 31) / 32 * 32; }
-constexpr int PITCH = 8;  // values behind a row, so that 16 rows start in different banks
 constexpr int BATCH = 4;  // groups of four loads of a thread under way together
 // The first `count` of four elements a stride apart.
 template <typename T> __device__ __forceinline__ float4v load_four(const T* p, int64_t stride, int count) {
@@ -319,12 +305,6 @@ template <typename T> __device__ __forceinline__ void store_four(T* p, int64_t s
             if (r < count) p[r * stride] = down<T>(v[r]);
     }
 }
-constexpr int TINY_LDS = 160 * 1024 - 1024 / 64 * 8;
-size_t tiny_lds(int m, int n) {
-    const size_t mp = up32(m), np = up32(n);
-    return 4 * (mp * (np + PITCH) + np * (mp + PITCH) + mp * (mp + PITCH));
-}
-
 template <typename T, int THREADS> __global__ __launch_bounds__(THREADS) void k_ortho_tiny(SmallArgs a, SmallScale sc) {
     extern __shared__ double lds_tiny[];
     __shared__ double norm_part[THREADS / 64];
@@ -510,24 +490,6 @@ template <typename T, int THREADS> __global__ __launch_bounds__(THREADS) void k_
 }
 
 // ---------------------------------------------------------------------------
-// Large matrices in the workspace. Formats of X, A and B: one fp16 part, two
-// (32 columns of hi, then the same 32 of lo), or fp64. A row of K values is
-// K * unit bytes, and 128 bytes of it are one step of a product's main loop.
-enum Format { ONE = 1, TWO = 2, DOUBLE = 3 };
-constexpr int unit_of(int format) { return format == ONE ? 2 : format == TWO ? 4 : 8; }
-
-// Padded sides: multiples of 64 hold whole main-loop steps of every format.
-// Padding is zero: zero rows and columns of X stay zero.
-constexpr int64_t up64(int64_t v) { return (v + 63) / 64 * 64; }
-
-struct Layout {  // of one matrix's part of the workspace
-    int64_t x, xt, a, b, size;  // two X^T: one is read while the other is written
-};
-__host__ __device__ inline Layout layout_of(int mp, int np, int unit) {
-    const int64_t x = (int64_t)mp * np * unit, s = (int64_t)mp * mp * unit;
-    return {0, x, 3 * x, 3 * x + s, 3 * x + 2 * s};
-}
-
 __device__ __forceinline__ void put(char* p, int64_t row, int64_t ld, int col, double v) {
     ((double*)(p + row * ld))[col] = v;
 }
@@ -656,12 +618,6 @@ template <typename T, int F> __global__ __launch_bounds__(256) void k_ortho_pack
     }
 }
 
-// The products: C = L R^T of rows of K values, both with K along the row.
-//   GRAM  A = X X^T            (tiles on and below the diagonal, written twice)
-//   POLY  B = b A + c A A      (the same)
-//   APPLY X = a X + B (X^T)^T, and its transpose
-//   LAST  the same, to the caller's matrix
-enum Mode { GRAM, POLY, APPLY, LAST };
 // A product with few tiles and a long K is split along K: PART workgroups leave
 // their sums in the workspace, and one JOIN workgroup a tile adds them in order
 // and goes on as a WHOLE one does.
@@ -1075,15 +1031,6 @@ __global__ __launch_bounds__(64 * WI * WJ, 2) void k_ortho_gemm(GemmArgs a) {
 // ---------------------------------------------------------------------------
 // Host side.
 
-struct Shape {
-    int m, n;
-    bool turned;
-};
-Shape shape_of(const ql_matrix& q) {
-    const bool turned = q.rows > q.cols;
-    return {(int)(turned ? q.cols : q.rows), (int)(turned ? q.rows : q.cols), turned};
-}
-
 Source source_of(const ql_matrix& q, bool muon) {
     const bool t = shape_of(q).turned;
     Source s{};
@@ -1102,54 +1049,6 @@ Target target_of(const ql_matrix& q, const OrthoCall& c) {
     r.ob = q.out_stride[0], r.oi = q.out_stride[t ? 2 : 1], r.oj = q.out_stride[t ? 1 : 2];
     r.step = c.step * std::sqrt(std::max(1.0, (double)q.rows / (double)q.cols));
     return r;
-}
-
-// Whether one workgroup's LDS holds the matrix.
-bool is_small(int type, const Shape& s) {
-    if (s.m > SMALL_M) return false;
-    if (type == E_F64) return small_lds(s.m, s.n, 8) <= SMALL_LDS;
-    return tiny_lds(s.m, s.n) <= TINY_LDS;
-}
-
-// Workgroups of the norm: each takes at least 4096 elements, and whole lines.
-int chunks_of(const Shape& s) {
-    return (int)std::min<int64_t>(std::min(s.m, 1024), std::max<int64_t>(1, (int64_t)s.m * s.n / 4096));
-}
-
-// One part is for bfloat16 updates whose products take the time: 5e9 operations
-// of matrices of more than 64 rows, which cost 8 us more a step in two. Below,
-// launches do, and with few rows the products' rounding does not average out:
-// 12x5992 came out at 1.7 times the error of the output's own rounding.
-int format_of(int type, const ql_matrix* mats, int count) {
-    if (type != E_BF16) return type == E_F64 ? DOUBLE : TWO;
-    double work = 0;
-    for (int k = 0; k < count; k++) {
-        const Shape s = shape_of(mats[k]);
-        if (s.m > SMALL_M) work += 5.0 * (double)mats[k].batch * s.m * s.m * (3.0 * s.n + s.m);
-    }
-    return work >= 5e9 ? ONE : TWO;
-}
-
-// Workspace of a matrix of the large route: X, A and B, then the norm's sums.
-int64_t large_bytes(int format, const Shape& s) {
-    return layout_of((int)up64(s.m), (int)up64(s.n), unit_of(format)).size;
-}
-int64_t norm_bytes(const Shape& s) { return (chunks_of(s) * 8 + 255) / 256 * 256; }
-
-bool all_small(int type, const ql_matrix* mats, int count) {
-    for (int k = 0; k < count; k++)
-        if (mats[k].batch > 0 && !is_small(type, shape_of(mats[k]))) return false;
-    return true;
-}
-
-struct Scales {  // powers of two that bring the largest possible values to at most 2^15
-    double sx = 1, sa = 1, sb = 1;
-};
-Scales scales_of(const OrthoCall& c) {
-    double most_x = 1, most_q = 1;
-    ortho_bounds(c.a, c.b, c.c, c.steps, most_x, most_q);
-    return {std::exp2(std::floor(std::log2(32768 / most_x))), std::exp2(std::floor(std::log2(32768 / (most_x * most_x)))),
-            std::exp2(std::floor(std::log2(32768 / std::max(most_q, 1e-3))))};
 }
 
 // Past 64 KiB the runtime wants a kernel's limit set, once on each device.
@@ -1204,11 +1103,6 @@ template <typename T> hipError_t run_small(const OrthoCall& c, const Rule& rule,
 
 static_assert(sizeof(SmallArgs) <= 4096 && sizeof(PackArgs) <= 4096 && sizeof(GemmArgs) <= 4096, "kernel arguments");
 
-int64_t tiles_of(int mode, int64_t bt, int m, int n) {
-    const int64_t mt = (up64(m) + bt - 1) / bt, nt = (up64(n) + bt - 1) / bt;
-    return mode <= POLY ? mt * (mt + 1) / 2 : mt * nt;
-}
-
 template <typename T, int F, int MODE, int SPLIT, int BT> hipError_t gemm(GemmArgs a, const int64_t* batch, hipStream_t s) {
     int64_t blocks = 0;
     for (int k = 0; k < a.count; k++) {
@@ -1224,74 +1118,8 @@ template <typename T, int F, int MODE, int SPLIT, int BT> hipError_t gemm(GemmAr
     return hipGetLastError();
 }
 
-// What a launch with tiles of a size costs, in us, from measured kernels: a
-// main-loop step of a workgroup that has its compute unit for itself, of one
-// that shares it (two of the smaller tiles fit one), and what a tile costs
-// besides its steps. One and two parts; fp64 has one tile size.
-constexpr int TILES[] = {64, 128, 192, 256};
-struct TileCost {
-    double alone, shared, rest;
-};
-constexpr TileCost COST[2][4] = {{{0.20, 0.40, 2}, {0.42, 0.78, 8}, {0.95, 0.95, 12}, {1.1, 1.1, 20}},
-                                 {{0.25, 0.45, 2}, {0.58, 1.10, 8}, {1.00, 1.00, 12}, {1.6, 1.6, 20}}};
-constexpr int UNITS = 256;  // compute units
-
-// The entries of a table and their batches, as the costs go by them.
-struct Chunk {
-    Shape shape[ENTRIES];
-    int64_t batch[ENTRIES];
-    int count = 0;
-};
-
-double launch_cost(int format, int mode, int which, int splits, const Chunk& c) {
-    const TileCost& t = COST[format == TWO][which];
-    const int64_t bt = TILES[which], slots = which < 2 ? 2 * UNITS : UNITS;
-    double alone = 0, shared = 0, longest = 0;  // sums over workgroups, and the longest one
-    int64_t tiles = 0;
-    for (int k = 0; k < c.count; k++) {
-        const int64_t n = c.batch[k] * tiles_of(mode, bt, c.shape[k].m, c.shape[k].n);
-        const int64_t whole = up64(mode == GRAM ? c.shape[k].n : c.shape[k].m) * unit_of(format) / 128;
-        const double steps = (double)((whole + splits - 1) / splits);
-        tiles += n;
-        alone += (double)(n * splits) * (steps * t.alone + t.rest);
-        shared += (double)(n * splits) * (steps * t.shared + t.rest);
-        longest = std::max(longest, steps * t.alone + t.rest);
-    }
-    if (!tiles) return 0;
-    const int64_t groups = tiles * splits, rounds = groups / slots, rest = groups % slots;
-    double cost = std::max(longest, rounds * shared / groups + (rest ? (rest <= UNITS ? alone : shared) / groups : 0));
-    // the second launch, and the sums' way to memory (3 TB/s) and back
-    if (splits > 1) cost += 3 + t.rest + 0.1 * splits + (double)groups * bt * bt * 8 / 3e6;
-    return cost;
-}
-
-// The tile size of a launch, and for GRAM with its short sides the split of K.
-struct Choice {
-    int which = 0, splits = 1;
-    int64_t bytes = 0;  // of the parts
-};
-Choice choose(int format, int mode, const Chunk& c, int sizes) {
-    Choice best;
-    if (format == DOUBLE) return best;
-    double least = 0;
-    for (int which = 0; which < sizes; which++) {
-        int64_t tiles = 0;
-        for (int k = 0; k < c.count; k++) tiles += c.batch[k] * tiles_of(mode, TILES[which], c.shape[k].m, c.shape[k].n);
-        for (int splits = 1; splits == 1 || (mode == GRAM && which < 2 && splits <= 64 && tiles * splits <= 2 * UNITS);
-             splits = splits < 4 ? splits + 1 : splits * 3 / 2) {
-            const double cost = launch_cost(format, mode, which, splits, c);
-            if ((which == 0 && splits == 1) || cost < least) least = cost, best.which = which, best.splits = splits;
-        }
-    }
-    if (best.splits > 1)
-        for (int k = 0; k < c.count; k++)
-            best.bytes += c.batch[k] * tiles_of(mode, TILES[best.which], c.shape[k].m, c.shape[k].n) * best.splits * TILES[best.which] * TILES[best.which] * 4;
-    return best;
-}
-
-// Tile sizes that a type's calls come to: bfloat16 has little work in two parts.
+// Tile sizes that a type's calls come to (ortho_plan.cpp chooses among these).
 template <typename T, int F> constexpr int SIZES = std::is_same_v<T, bf16> && F == TWO ? 1 : 4;
-int sizes_of(int type, int format) { return type == E_BF16 && format == TWO ? 1 : 4; }
 
 template <typename T, int F, int MODE> hipError_t gemm(GemmArgs a, const Chunk& c, const Choice& how, hipStream_t s) {
     if constexpr (F == DOUBLE) {
@@ -1311,18 +1139,6 @@ template <typename T, int F, int MODE> hipError_t gemm(GemmArgs a, const Chunk& 
         }
         return gemm<T, F, MODE, WHOLE, 64>(a, c.batch, s);
     }
-}
-
-// The next entries that a table holds, from `at` on; empty ones are left out.
-int next_chunk(const ql_matrix* mats, int count, int at, Chunk& c, const ql_matrix** entry) {
-    for (c.count = 0; at < count && c.count < ENTRIES; at++)
-        if (mats[at].batch > 0) {
-            c.shape[c.count] = shape_of(mats[at]);
-            c.batch[c.count] = mats[at].batch;
-            if (entry) entry[c.count] = &mats[at];
-            c.count++;
-        }
-    return at;
 }
 
 template <typename T, int F> hipError_t run_steps(const OrthoCall& c, GemmArgs g, const Chunk& chunk, const Scales& k, hipStream_t s) {
@@ -1401,51 +1217,6 @@ template <typename T> hipError_t run(const OrthoCall& c, void* ws, hipStream_t s
 }
 
 }  // namespace
-
-bool ortho_bounds(double a, double b, double c, int steps, double& most_x, double& most_q) {
-    most_x = 1, most_q = 0;
-    if (!std::isfinite(a) || !std::isfinite(b) || !std::isfinite(c)) return false;
-    // over t = x^2: where p' = a + 3 b t + 5 c t^2 and q' = b + 2 c t vanish
-    double inner[3];
-    int n = 0;
-    const double disc = 9 * b * b - 20 * a * c;
-    if (c != 0) inner[n++] = -b / (2 * c);
-    if (disc >= 0) {  // both roots without a difference of nearly equal numbers
-        const double h = -(3 * b + std::copysign(std::sqrt(disc), b)) / 2;
-        if (c != 0) inner[n++] = h / (5 * c);
-        if (h != 0) inner[n++] = a / h;
-    }
-    double reach = 1;  // singular values lie in [0, reach]
-    for (int s = 0; s < steps; s++) {
-        double next = 0;
-        for (int k = 0; k <= n; k++) {
-            const double t = k < n ? inner[k] : reach * reach;
-            if (!(t >= 0 && t <= reach * reach)) continue;
-            const double q = t * (b + c * t), v = std::fabs(std::sqrt(t) * (a + q));
-            if (!(v <= 1e6) || !(std::fabs(q) <= 1e5)) return false;
-            next = std::max(next, v);
-            most_q = std::max(most_q, std::fabs(q));
-        }
-        if (s + 1 == steps) break;  // what the last step gives is not held
-        reach = next * (1 + 1.0 / 256);  // and a margin for the products' rounding
-        most_x = std::max(most_x, reach);
-        if (reach > 64) return false;
-    }
-    return true;
-}
-
-size_t ortho_workspace(int type, const ql_matrix* mats, int count) {
-    if (all_small(type, mats, count)) return 0;
-    const int format = format_of(type, mats, count);
-    int64_t bytes = 0;
-    for (int at = 0; at < count;) {
-        Chunk c;
-        at = next_chunk(mats, count, at, c, nullptr);
-        for (int k = 0; k < c.count; k++) bytes += c.batch[k] * (large_bytes(format, c.shape[k]) + norm_bytes(c.shape[k]));
-        bytes += choose(format, GRAM, c, sizes_of(type, format)).bytes;
-    }
-    return (size_t)bytes;
-}
 
 hipError_t launch_ortho(const OrthoCall& c, void* ws, hipStream_t s) {
     switch (c.type) {
