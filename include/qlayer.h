@@ -406,10 +406,9 @@ int ql_layer_norm_backward(ql_type type, ql_type weight_type, int64_t rows, int6
  * a call run together: give a network's matrices in one call.
  *
  * Precision: QL_F64 in fp64. Other products are fp16 ones that keep 22 bits of
- * every factor (in two parts), or 11 for calls of QL_BF16 with 5e9 operations or
- * more in matrices of more than 64 rows. Sums are fp32, norms fp64. A matrix's
- * last bits can depend on what else the call holds (the tiles follow from all of
- * it), and nothing else: the same call gives the same bits.
+ * every factor (in two parts); sums are fp32, norms fp64. A matrix's last bits
+ * can depend on what else the call holds (the tiles follow from all of it), and
+ * nothing else: the same call gives the same bits.
  *
  * options NULL: the defaults in braces. rows, cols in [1, 65536], steps in
  * [1, 64]; coefficients that let a singular value in [0, 1] grow past 64 before

@@ -12,12 +12,10 @@
 //
 // Products are fp16 ones summed in fp32. The singular values of X stay below
 // about 1.2 (ortho_bounds), so X, A and B are held in fp16 at powers of two that
-// use its range: in two parts, v = hi + lo (hi hi + hi lo + lo hi keeps 22 bits
-// of every factor, at a third of fp16's rate, five times fp32's), or for much
-// work in bfloat16 in one (11 bits, of which the result keeps 8). What they are
-// held in costs the result less than its own rounding does, and in float32 less
-// than fp32 sums do (2048x8192: 1.9e-6 off, 3.3e-6 with fp32 products). fp64
-// uses fp64.
+// use its range, in two parts, v = hi + lo (hi hi + hi lo + lo hi keeps 22 bits
+// of every factor, at a third of fp16's rate, five times fp32's). In float32
+// they cost the result less than fp32 sums do (2048x8192: 1.8e-6 off, 3.2e-6
+// with fp32 products). fp64 uses fp64.
 #include <algorithm>
 #include <atomic>
 #include <cmath>
@@ -609,11 +607,10 @@ template <typename T, int F> __global__ __launch_bounds__(256) void k_ortho_pack
                 hi[v] = (_Float16)tile[r][at + v], lo[v] = (_Float16)(tile[r][at + v] - (float)hi[v]);
                 thi[v] = (_Float16)tile[at + v][r], tlo[v] = (_Float16)(tile[at + v][r] - (float)thi[v]);
             }
-            const int in = F == ONE ? at : at / 32 * 64 + at % 32;
-            _Float16 *p = (_Float16*)(x + (i0 + r) * ldx) + j0 * (F == ONE ? 1 : 2) + in, *q = (_Float16*)(xt + (j0 + r) * ldt) + i0 * (F == ONE ? 1 : 2) + in;
-            *(half8*)p = hi;
-            *(half8*)q = thi;
-            if constexpr (F == TWO) *(half8*)(p + 32) = lo, *(half8*)(q + 32) = tlo;
+            const int in = at / 32 * 64 + at % 32;
+            _Float16 *p = (_Float16*)(x + (i0 + r) * ldx) + j0 * 2 + in, *q = (_Float16*)(xt + (j0 + r) * ldt) + i0 * 2 + in;
+            *(half8*)p = hi, *(half8*)(p + 32) = lo;
+            *(half8*)q = thi, *(half8*)(q + 32) = tlo;
         }
     }
 }
@@ -648,12 +645,9 @@ __device__ __forceinline__ int xcd_run(int block, int blocks) {
     return x * q + min(x, r) + block / 8;
 }
 
-// Four consecutive values of a row (col % 4 = 0).
-template <int F> __device__ __forceinline__ float4v get4(const char* p, int64_t row, int64_t ld, int col) {
-    const _Float16* r = (const _Float16*)(p + row * ld) + (F == ONE ? col : col / 32 * 64 + col % 32);
-    float4v v = __builtin_convertvector(*(const half4*)r, float4v);
-    if constexpr (F == TWO) v += __builtin_convertvector(*(const half4*)(r + 32), float4v);
-    return v;
+// Four consecutive values of a row in two parts (col % 4 = 0).
+__device__ __forceinline__ float4v get4(const char* p, int64_t row, int64_t ld, int col) {
+    return get_two4((const _Float16*)(p + row * ld) + col / 32 * 64 + col % 32, 32);
 }
 
 // A wavefront's operands of half a step: N tiles' rows of 32 values, or of 2 x 4 in fp64.
@@ -925,8 +919,8 @@ __global__ __launch_bounds__(64 * WI * WJ, 2) void k_ortho_gemm(GemmArgs a) {
 #pragma unroll
             for (int j = 0; j < TJ; j++) {
                 const int gj = min(j0 + j * 16, right_rows - 16) + 4 * part;
-                if constexpr (MODE == POLY) f.add[j] = get4<F>(w + l.a, gi, lda, gj);
-                if constexpr (MODE >= APPLY) f.add[j] = get4<F>(w + l.x, gi, ldx, gj);
+                if constexpr (MODE == POLY) f.add[j] = get4(w + l.a, gi, lda, gj);
+                if constexpr (MODE >= APPLY) f.add[j] = get4(w + l.x, gi, ldx, gj);
                 if constexpr (MODE == LAST)
                     if (a.r.muon) {
                         if (by_row) {
@@ -946,12 +940,12 @@ __global__ __launch_bounds__(64 * WI * WJ, 2) void k_ortho_gemm(GemmArgs a) {
             __builtin_amdgcn_s_barrier();
             asm volatile("" ::: "memory");
             _Float16* own = (_Float16*)(s0 + wave * (2 * BT * 128 / (WI * WJ)));
-            constexpr int PLANES = F == TWO ? 2 : 1;
+            constexpr int PLANES = 2;
             constexpr int WIDE = TJ * 16 + 8, HIGH = TI * 16 + 8;  // pitches, off a multiple of the banks
             static_assert(16 * HIGH * 2 <= 2 * BT * 128 / (WI * WJ) && 16 * WIDE * 2 * PLANES <= 2 * BT * 128 / (WI * WJ), "LDS");
             char* to = w + (MODE == GRAM ? l.a : MODE == POLY ? l.b : l.x);
             const int64_t to_ld = MODE == APPLY ? ldx : lda;
-            auto in_row = [](int64_t c, int plane) { return F == ONE ? c : c / 32 * 64 + plane * 32 + c % 32; };
+            auto in_row = [](int64_t c, int plane) { return c / 32 * 64 + plane * 32 + c % 32; };
 #pragma unroll
             for (int i = 0; i < TI; i++) {
                 const Behind next = fetch(min(i + 1, TI - 1));
@@ -962,7 +956,7 @@ __global__ __launch_bounds__(64 * WI * WJ, 2) void k_ortho_gemm(GemmArgs a) {
                     acc[i][j] = v;
                     const half4 hi = high(v);
                     *(half4*)(own + row * WIDE + j * 16 + 4 * part) = hi;
-                    if constexpr (F == TWO) *(half4*)(own + (16 + row) * WIDE + j * 16 + 4 * part) = low(v, hi);
+                    *(half4*)(own + (16 + row) * WIDE + j * 16 + 4 * part) = low(v, hi);
                 }
                 __builtin_amdgcn_wave_barrier();
 #pragma unroll
@@ -1113,13 +1107,10 @@ template <typename T, int F, int MODE, int SPLIT, int BT> hipError_t gemm(GemmAr
     if (blocks > INT32_MAX) return hipErrorInvalidValue;
     constexpr int WJ = BT >= 192 ? 4 : 2, STAGES = BT == 64 ? 4 : BT == 192 ? 3 : 2;
     // only the last product sees the caller's type
-    using K = std::conditional_t<MODE == LAST, T, std::conditional_t<F == ONE, bf16, std::conditional_t<F == TWO, float, double>>>;
+    using K = std::conditional_t<MODE == LAST, T, std::conditional_t<F == TWO, float, double>>;
     k_ortho_gemm<K, F, MODE, SPLIT, BT, 2, WJ, STAGES><<<(unsigned)blocks, 128 * WJ, 0, s>>>(a);
     return hipGetLastError();
 }
-
-// Tile sizes that a type's calls come to (ortho_plan.cpp chooses among these).
-template <typename T, int F> constexpr int SIZES = std::is_same_v<T, bf16> && F == TWO ? 1 : 4;
 
 template <typename T, int F, int MODE> hipError_t gemm(GemmArgs a, const Chunk& c, const Choice& how, hipStream_t s) {
     if constexpr (F == DOUBLE) {
@@ -1132,18 +1123,15 @@ template <typename T, int F, int MODE> hipError_t gemm(GemmArgs a, const Chunk& 
                 if (e != hipSuccess) return e;
                 return how.which ? gemm<T, F, MODE, JOIN, 128>(a, c.batch, s) : gemm<T, F, MODE, JOIN, 64>(a, c.batch, s);
             }
-        if constexpr (SIZES<T, F> == 4) {
-            if (how.which == 1) return gemm<T, F, MODE, WHOLE, 128>(a, c.batch, s);
-            if (how.which == 2) return gemm<T, F, MODE, WHOLE, 192>(a, c.batch, s);
-            if (how.which == 3) return gemm<T, F, MODE, WHOLE, 256>(a, c.batch, s);
-        }
+        if (how.which == 1) return gemm<T, F, MODE, WHOLE, 128>(a, c.batch, s);
+        if (how.which == 2) return gemm<T, F, MODE, WHOLE, 192>(a, c.batch, s);
+        if (how.which == 3) return gemm<T, F, MODE, WHOLE, 256>(a, c.batch, s);
         return gemm<T, F, MODE, WHOLE, 64>(a, c.batch, s);
     }
 }
 
 template <typename T, int F> hipError_t run_steps(const OrthoCall& c, GemmArgs g, const Chunk& chunk, const Scales& k, hipStream_t s) {
-    constexpr int sizes = SIZES<T, F>;
-    const Choice gram = choose(F, GRAM, chunk, sizes), poly = choose(F, POLY, chunk, sizes), apply = choose(F, APPLY, chunk, sizes);
+    const Choice gram = choose(F, GRAM, chunk), poly = choose(F, POLY, chunk), apply = choose(F, APPLY, chunk);
     hipError_t e = hipSuccess;
     for (int step = 0; step < c.steps && e == hipSuccess; step++) {
         g.from = step & 1;
@@ -1187,7 +1175,7 @@ template <typename T, int F> hipError_t run_large(const OrthoCall& c, const Rule
             g.e[k] = {e.work, target_of(*entry[k], c), sh.m, sh.n, 0};
         }
         g.part = ws;
-        ws += choose(F, GRAM, chunk, SIZES<T, F>).bytes;
+        ws += choose(F, GRAM, chunk).bytes;
         if (norm_blocks > INT32_MAX) return hipErrorInvalidValue;
         k_ortho_norm<T><<<(unsigned)norm_blocks, 256, 0, s>>>(p);
         if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
@@ -1210,8 +1198,6 @@ template <typename T> hipError_t run(const OrthoCall& c, void* ws, hipStream_t s
     if constexpr (std::is_same_v<T, double>) {
         return run_large<T, DOUBLE>(c, r, (char*)ws, s);
     } else {
-        if constexpr (std::is_same_v<T, bf16>)
-            if (format_of(c.type, c.mats, c.count) == ONE) return run_large<T, ONE>(c, r, (char*)ws, s);
         return run_large<T, TWO>(c, r, (char*)ws, s);
     }
 }

@@ -8,28 +8,24 @@
 namespace qlayer {
 namespace {
 
-// Tile sizes that a type's calls come to: bfloat16 has little work in two parts.
-int sizes_of(int type, int format) { return type == E_BF16 && format == TWO ? 1 : 4; }
-
 // What a launch with tiles of a size costs, in us, from measured kernels: a
 // main-loop step of a workgroup that has its compute unit for itself, of one
 // that shares it (two of the smaller tiles fit one), and what a tile costs
-// besides its steps. One and two parts; fp64 has one tile size.
+// besides its steps. fp64 has one tile size.
 struct TileCost {
     double alone, shared, rest;
 };
-constexpr TileCost COST[2][4] = {{{0.20, 0.40, 2}, {0.42, 0.78, 8}, {0.95, 0.95, 12}, {1.1, 1.1, 20}},
-                                 {{0.25, 0.45, 2}, {0.58, 1.10, 8}, {1.00, 1.00, 12}, {1.6, 1.6, 20}}};
+constexpr TileCost COST[4] = {{0.25, 0.45, 2}, {0.58, 1.10, 8}, {1.00, 1.00, 12}, {1.6, 1.6, 20}};
 constexpr int UNITS = 256;  // compute units
 
-double launch_cost(int format, int mode, int which, int splits, const Chunk& c) {
-    const TileCost& t = COST[format == TWO][which];
+double launch_cost(int mode, int which, int splits, const Chunk& c) {
+    const TileCost& t = COST[which];
     const int64_t bt = TILES[which], slots = which < 2 ? 2 * UNITS : UNITS;
     double alone = 0, shared = 0, longest = 0;  // sums over workgroups, and the longest one
     int64_t tiles = 0;
     for (int k = 0; k < c.count; k++) {
         const int64_t n = c.batch[k] * tiles_of(mode, bt, c.shape[k].m, c.shape[k].n);
-        const int64_t whole = up64(mode == GRAM ? c.shape[k].n : c.shape[k].m) * unit_of(format) / 128;
+        const int64_t whole = up64(mode == GRAM ? c.shape[k].n : c.shape[k].m) * unit_of(TWO) / 128;
         const double steps = (double)((whole + splits - 1) / splits);
         tiles += n;
         alone += (double)(n * splits) * (steps * t.alone + t.rest);
@@ -56,20 +52,6 @@ int chunks_of(const Shape& s) {
     return (int)std::min<int64_t>(std::min(s.m, 1024), std::max<int64_t>(1, (int64_t)s.m * s.n / 4096));
 }
 
-// One part is for bfloat16 updates whose products take the time: 5e9 operations
-// of matrices of more than 64 rows, which cost 8 us more a step in two. Below,
-// launches do, and with few rows the products' rounding does not average out:
-// 12x5992 came out at 1.7 times the error of the output's own rounding.
-int format_of(int type, const ql_matrix* mats, int count) {
-    if (type != E_BF16) return type == E_F64 ? DOUBLE : TWO;
-    double work = 0;
-    for (int k = 0; k < count; k++) {
-        const Shape s = shape_of(mats[k]);
-        if (s.m > SMALL_M) work += 5.0 * (double)mats[k].batch * s.m * s.m * (3.0 * s.n + s.m);
-    }
-    return work >= 5e9 ? ONE : TWO;
-}
-
 int64_t large_bytes(int format, const Shape& s) {
     return layout_of((int)up64(s.m), (int)up64(s.n), unit_of(format)).size;
 }
@@ -93,16 +75,16 @@ int64_t tiles_of(int mode, int64_t bt, int m, int n) {
     return mode <= POLY ? mt * (mt + 1) / 2 : mt * nt;
 }
 
-Choice choose(int format, int mode, const Chunk& c, int sizes) {
+Choice choose(int format, int mode, const Chunk& c) {
     Choice best;
     if (format == DOUBLE) return best;
     double least = 0;
-    for (int which = 0; which < sizes; which++) {
+    for (int which = 0; which < 4; which++) {
         int64_t tiles = 0;
         for (int k = 0; k < c.count; k++) tiles += c.batch[k] * tiles_of(mode, TILES[which], c.shape[k].m, c.shape[k].n);
         for (int splits = 1; splits == 1 || (mode == GRAM && which < 2 && splits <= 64 && tiles * splits <= 2 * UNITS);
              splits = splits < 4 ? splits + 1 : splits * 3 / 2) {
-            const double cost = launch_cost(format, mode, which, splits, c);
+            const double cost = launch_cost(mode, which, splits, c);
             if ((which == 0 && splits == 1) || cost < least) least = cost, best.which = which, best.splits = splits;
         }
     }
@@ -157,13 +139,13 @@ bool ortho_bounds(double a, double b, double c, int steps, double& most_x, doubl
 
 size_t ortho_workspace(int type, const ql_matrix* mats, int count) {
     if (all_small(type, mats, count)) return 0;
-    const int format = format_of(type, mats, count);
+    const int format = type == E_F64 ? DOUBLE : TWO;
     int64_t bytes = 0;
     for (int at = 0; at < count;) {
         Chunk c;
         at = next_chunk(mats, count, at, c, nullptr);
         for (int k = 0; k < c.count; k++) bytes += c.batch[k] * (large_bytes(format, c.shape[k]) + norm_bytes(c.shape[k]));
-        bytes += choose(format, GRAM, c, sizes_of(type, format)).bytes;
+        bytes += choose(format, GRAM, c).bytes;
     }
     return (size_t)bytes;
 }

@@ -47,11 +47,16 @@ bool is_small(int type, const Shape& s);
 bool all_small(int type, const ql_matrix* mats, int count);
 
 // ---------------------------------------------------------------------------
-// Large matrices in the workspace. Formats of X, A and B: one fp16 part, two
-// (32 columns of hi, then the same 32 of lo), or fp64. A row of K values is
-// K * unit bytes, and 128 bytes of it are one step of a product's main loop.
-enum Format { ONE = 1, TWO = 2, DOUBLE = 3 };
-constexpr int unit_of(int format) { return format == ONE ? 2 : format == TWO ? 4 : 8; }
+// Large matrices in the workspace. Formats of X, A and B: two fp16 parts (32
+// columns of hi, then the same 32 of lo), or fp64 for QL_F64. A row of K values
+// is K * unit bytes, and 128 bytes of it are one step of a product's main loop.
+//
+// One part (11 bits) would serve no type: where an update has a few directions
+// and little beside them, as gradients do, what a product rounds off lands in
+// the small directions and is raised by 3.4 a step. bfloat16 results came out
+// 12 (1500x1500) to 16 times (900x600) their own rounding off, in two parts once.
+enum Format { TWO = 2, DOUBLE = 3 };
+constexpr int unit_of(int format) { return format == TWO ? 4 : 8; }
 
 // Padded sides: multiples of 64 hold whole main-loop steps of every format.
 // Padding is zero: zero rows and columns of X stay zero.
@@ -70,7 +75,6 @@ int64_t large_bytes(int format, const Shape& s);
 int64_t norm_bytes(const Shape& s);
 // Workgroups of the norm: each takes at least 4096 elements, and whole lines.
 int chunks_of(const Shape& s);
-int format_of(int type, const ql_matrix* mats, int count);
 
 struct Scales {  // powers of two that bring the largest possible values to at most 2^15
     double sx = 1, sa = 1, sb = 1;
@@ -99,8 +103,7 @@ struct Choice {
     int which = 0, splits = 1;
     int64_t bytes = 0;  // of the parts
 };
-// Among the first `sizes` tile sizes.
-Choice choose(int format, int mode, const Chunk& c, int sizes);
+Choice choose(int format, int mode, const Chunk& c);
 
 // The next entries that a table holds, from `at` on; empty ones are left out.
 int next_chunk(const ql_matrix* mats, int count, int at, Chunk& c, const ql_matrix** entry);
