@@ -78,8 +78,11 @@ int64_t tiles_of(int mode, int64_t bt, int m, int n) {
 Choice choose(int format, int mode, const Chunk& c) {
     Choice best;
     if (format == DOUBLE) return best;
+    // sums over a long side of few rows are for the tiles that fold them
+    bool wide = false;
+    for (int k = 0; k < c.count; k++) wide |= c.shape[k].n > 4 * (int64_t)c.shape[k].m;
     double least = 0;
-    for (int which = 0; which < 4; which++) {
+    for (int which = 0; which < (mode == GRAM && wide ? 2 : 4); which++) {
         int64_t tiles = 0;
         for (int k = 0; k < c.count; k++) tiles += c.batch[k] * tiles_of(mode, TILES[which], c.shape[k].m, c.shape[k].n);
         for (int splits = 1; splits == 1 || (mode == GRAM && which < 2 && splits <= 64 && tiles * splits <= 2 * UNITS);

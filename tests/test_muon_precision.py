@@ -107,3 +107,19 @@ def test_a_matrix_beside_a_large_one(need_gpu, name, kind):
     Q.muon_step(p, [t.cuda() for t in u], m, lr=1.0, momentum=0.0)
     for q, t, (rows, cols) in zip(p, u, shapes):
         near(q, t, TYPES[name], f"{rows}x{cols} {kind}", sign=-1 / math.sqrt(max(1.0, rows / cols)))
+
+
+@gpu
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("beside,batch", [((4096, 4096), 1), ((20, 30), 600)])
+@pytest.mark.parametrize("rows,cols", [(12, 5992), (3000, 65)])
+def test_long_sums_of_few_rows(need_gpu, rows, cols, beside, batch, kind):
+    """However many tiles the rest of a call gives the chip, so that no sum is split."""
+    u = torch.stack([update(rows, cols, kind, torch.float32, seed=k % 3) for k in range(batch)]).cuda()
+    other = update(*beside, kind, torch.float32, seed=9).cuda()
+    p = [torch.zeros_like(u), torch.zeros_like(other)]
+    m = [torch.zeros_like(t) for t in p]
+    Q.muon_step(p, [u, other], m, lr=1.0, momentum=0.0)
+    grow = math.sqrt(max(1.0, rows / cols))
+    for k in (0, batch // 2, batch - 1):
+        near(p[0][k], u[k].cpu(), torch.float32, f"{rows}x{cols} {kind}, matrix {k}", sign=-1 / grow)
