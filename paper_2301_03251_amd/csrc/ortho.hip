@@ -108,6 +108,19 @@ template <typename R> __device__ __forceinline__ int mma_row(int lane, int r) {
     return sizeof(R) == 4 ? 4 * (lane / 16) + r : lane / 16 + 4 * r;
 }
 
+// Where |U| is far below eps, X is far below 1, and fp16 parts at the scale of 1
+// would lose its bits. |X| <= 2^e (0: no information) in the Frobenius norm at
+// first, and a step multiplies it by at most 2^growth: before step s, X is held
+// times 2^raised, which is 0 until the bound leaves room.
+__device__ __forceinline__ int norm_exponent(double norm, double eps) {
+    const double f = norm / (norm + eps);
+    return f > 0 && f < 1 ? ilogb(f) + 1 : 0;  // 0 and NaN as 1
+}
+__device__ __forceinline__ int raised(int e, int step, float growth) {
+    return max(0, min(120, (int)floorf(-(float)e - (float)step * growth)));
+}
+__device__ __forceinline__ float power_of_two(int e) { return __builtin_ldexpf(1.0f, e); }
+
 // ---------------------------------------------------------------------------
 // Small matrices in fp64: one workgroup each, X, A and B in its LDS, products of 16x16x4.
 struct SmallEntry {
@@ -212,7 +225,7 @@ template <typename T> __global__ __launch_bounds__(SMALL_THREADS) void k_ortho_s
 // barrier to barrier of four phases. With the fp32 products above (16x16x4, a
 // sixteenth of the rate) it was 95 and 19 us.
 struct SmallScale {
-    float sx, sa, sb;
+    float sx, sa, sb, growth;
 };
 // A wavefront's 16x16 tile, K in steps of 32: rows p and q of two-part arrays,
 // whose second part lies `behind` values after the first.
@@ -366,7 +379,10 @@ template <typename T, int THREADS> __global__ __launch_bounds__(THREADS) void k_
     typedef uint32_t word4 __attribute__((ext_vector_type(4)));
     for (int k = threadIdx.x; k < 2 * flow / 8; k += THREADS) ((word4*)first)[k] = word4{0, 0, 0, 0};
     for (int k = threadIdx.x; k < 2 * alow / 8; k += THREADS) ((word4*)A)[k] = word4{0, 0, 0, 0};
-    const double inv = (double)sc.sx / (sqrt(group_sum<THREADS>(sq, norm_part)) + a.r.eps);
+    const double norm = sqrt(group_sum<THREADS>(sq, norm_part));
+    const int bound = norm_exponent(norm, a.r.eps);
+    int lift = raised(bound, 0, sc.growth);  // X is held times sx 2^lift
+    const double inv = (double)sc.sx * (double)power_of_two(lift) / (norm + a.r.eps);
     {
         Walk w(groups);
         for (int k = threadIdx.x; k < total; k += THREADS, w.next()) {
@@ -391,11 +407,13 @@ template <typename T, int THREADS> __global__ __launch_bounds__(THREADS) void k_
     auto tile_row = [](int t) { return (t > 0) + (t > 2) + (t > 5); };
     const int mt = (m + 15) / 16, nt = (n + 15) / 16, lower = mt * (mt + 1) / 2;
     for (int step = 0; step < a.steps; step++) {
+        const int now = lift;
+        lift = raised(bound, step + 1, sc.growth);
         float4v acc[TILES_EACH];
 #pragma unroll
         for (int which = 0; which < 2; which++) {
             const float f0 = (float)a.b * sc.sb / sc.sa;
-            const float f1 = which ? (float)a.c * sc.sb / (sc.sa * sc.sa) : sc.sa / (sc.sx * sc.sx);
+            const float f1 = which ? (float)a.c * sc.sb / (sc.sa * sc.sa) : sc.sa / (sc.sx * sc.sx) * power_of_two(-2 * now);
 #pragma unroll
             for (int c = 0; c < TILES_EACH; c++) {
                 const int t = wave + c * waves, ti = tile_row(t), tj = t - ti * (ti + 1) / 2;
@@ -420,7 +438,7 @@ template <typename T, int THREADS> __global__ __launch_bounds__(THREADS) void k_
             }
             __syncthreads();
         }
-        const float f0 = (float)a.a, f1 = 1 / sc.sb;
+        const float shift = power_of_two(lift - now), f0 = (float)a.a * shift, f1 = shift / sc.sb;
         // two columns of tiles at a time where there are many: B's rows are read half as often
         constexpr int WIDE = THREADS == 1024 ? 2 : 1;
         for (int t = WIDE * wave; t < nt; t += WIDE * waves) {
@@ -478,7 +496,7 @@ template <typename T, int THREADS> __global__ __launch_bounds__(THREADS) void k_
                 count[c] = k0 + c * THREADS < total ? min(4, wide - 4 * w.at) : 0;
                 at[c] = out + w.line * ol + 4 * w.at * os;
                 if (a.r.muon) old[c] = load_four<T>(at[c], os, count[c]);
-                if (count[c]) v[c] = get_two4(from + w.line * pitch + 4 * w.at, behind) * (1 / sc.sx);
+                if (count[c]) v[c] = get_two4(from + w.line * pitch + 4 * w.at, behind) * (power_of_two(-lift) / sc.sx);
             }
 #pragma unroll
             for (int c = 0; c < BATCH; c++)
@@ -498,13 +516,14 @@ __device__ __forceinline__ double get(const char* p, int64_t row, int64_t ld, in
 struct PackEntry {
     Source s;
     char* work;    // the first matrix's part of the workspace
-    double* part;  // [batch][chunks] sums of squares
+    double* part;  // [batch][chunks + 1]: sums of squares, then X's exponent (norm_exponent)
     int32_t m, n, first, chunks;
 };
 struct PackArgs {
     PackEntry e[ENTRIES];
     Rule r;
     double scale;  // X is stored times this
+    float growth;
     int32_t count;
 };
 
@@ -549,7 +568,7 @@ template <typename T> __global__ __launch_bounds__(256) void k_ortho_norm(PackAr
         sq += (double)u * (double)u;
     }
     sq = group_sum<256>(sq, lds);
-    if (threadIdx.x == 0) e.part[at] = sq;
+    if (threadIdx.x == 0) e.part[b * (e.chunks + 1) + chunk] = sq;
 }
 
 // X and X^T of a 64x64 tile.
@@ -562,8 +581,15 @@ template <typename T, int F> __global__ __launch_bounds__(256) void k_ortho_pack
     const int at = blockIdx.x - e.first, i0 = at / tj % ti * 64, j0 = at % tj * 64;
     const int64_t b = at / (ti * tj);
     double sq = 0;
-    for (int k = threadIdx.x; k < e.chunks; k += 256) sq += e.part[b * e.chunks + k];
-    const double inv = a.scale / (sqrt(group_sum<256>(sq, lds)) + a.r.eps);
+    double* part = e.part + b * (e.chunks + 1);
+    for (int k = threadIdx.x; k < e.chunks; k += 256) sq += part[k];
+    const double norm = sqrt(group_sum<256>(sq, lds));
+    double inv = a.scale / (norm + a.r.eps);
+    if constexpr (F == TWO) {
+        const int bound = norm_exponent(norm, a.r.eps);
+        inv *= (double)power_of_two(raised(bound, 0, a.growth));
+        if (i0 == 0 && j0 == 0 && threadIdx.x == 0) part[e.chunks] = bound;
+    }
     const bool by_row = e.s.gj == 1 || e.s.gi != 1;
     if constexpr (F == DOUBLE) {
         for (int k = threadIdx.x; k < 64 * 64; k += 256) {
@@ -621,13 +647,16 @@ template <typename T, int F> __global__ __launch_bounds__(256) void k_ortho_pack
 enum Split { WHOLE, PART, JOIN };
 struct GemmEntry {
     char* work;
+    const double* exponent;  // the first matrix's (norm_exponent), `apart` before the next one's
     Target t;
-    int32_t m, n, first;
+    int32_t m, n, first, apart;
 };
 struct GemmArgs {
     GemmEntry e[ENTRIES];
     Rule r;
     double f0, f1;  // C is stored as f0 * (what it adds to) + f1 * (the sum)
+    float growth;
+    int32_t step;
     int32_t count, from;  // from: which X^T is read
     int32_t splits;
     char* part;           // [tile][split][values of a tile] fp32, as the threads hold them
@@ -699,6 +728,7 @@ __global__ __launch_bounds__(64 * WI * WJ, 2) void k_ortho_gemm(GemmArgs a) {
     const int t = (block - e.first) % tiles;
     const int64_t b = (block - e.first) / tiles;
     char* w = e.work + b * l.size;
+    [[maybe_unused]] const int bound = F == TWO && MODE != POLY ? (int)e.exponent[b * e.apart] : 0;
     int ti, tj;
     if (MODE <= POLY) {
         ti = (int)((sqrtf(8.0f * t + 1) - 1) / 2);
@@ -932,6 +962,12 @@ __global__ __launch_bounds__(64 * WI * WJ, 2) void k_ortho_gemm(GemmArgs a) {
     } else {
         // A wavefront's tiles from the top: what a row of them is added to is read
         // while the row before is written, at places that are there for every lane.
+        float f0 = (float)a.f0, f1 = (float)a.f1;
+        if constexpr (MODE == GRAM) f1 *= power_of_two(-2 * raised(bound, a.step, a.growth));
+        if constexpr (MODE >= APPLY) {
+            const float shift = power_of_two((MODE == APPLY ? raised(bound, a.step + 1, a.growth) : 0) - raised(bound, a.step, a.growth));
+            f0 *= shift, f1 *= shift;
+        }
         const bool by_row = e.t.oj == 1 && e.n >= 4;  // LAST: four columns at a time to the caller
         struct Behind {
             float4v add[TJ];
@@ -975,8 +1011,8 @@ __global__ __launch_bounds__(64 * WI * WJ, 2) void k_ortho_gemm(GemmArgs a) {
                 const Behind next = fetch(min(i + 1, TI - 1));
 #pragma unroll
                 for (int j = 0; j < TJ; j++) {
-                    float4v v = acc[i][j] * (float)a.f1;
-                    if constexpr (MODE != GRAM) v += now.add[j] * (float)a.f0;
+                    float4v v = acc[i][j] * f1;
+                    if constexpr (MODE != GRAM) v += now.add[j] * f0;
                     acc[i][j] = v;
                     const half4 hi = high(v);
                     *(half4*)(own + row * WIDE + j * 16 + 4 * part) = hi;
@@ -1024,7 +1060,7 @@ __global__ __launch_bounds__(64 * WI * WJ, 2) void k_ortho_gemm(GemmArgs a) {
 #pragma unroll
                 for (int j = 0; j < TJ; j++) {
                     const int gj = j0 + j * 16 + 4 * part;
-                    const float4v v = acc[i][j] * (float)a.f1 + now.add[j] * (float)a.f0;
+                    const float4v v = acc[i][j] * f1 + now.add[j] * f0;
                     if (by_row && gi < e.m && gj + 4 <= e.n) {
                         Four<T> f;
 #pragma unroll
@@ -1082,7 +1118,7 @@ hipError_t allow_lds(const void* kernel, std::atomic<uint64_t>& ready, int bytes
 template <typename T, int THREADS> hipError_t launch_tiny(const SmallArgs& a, unsigned blocks, size_t lds, const Scales& k, hipStream_t s) {
     static std::atomic<uint64_t> ready{0};
     if (hipError_t e = allow_lds((const void*)k_ortho_tiny<T, THREADS>, ready, TINY_LDS); e != hipSuccess) return e;
-    k_ortho_tiny<T, THREADS><<<blocks, THREADS, lds, s>>>(a, SmallScale{(float)k.sx, (float)k.sa, (float)k.sb});
+    k_ortho_tiny<T, THREADS><<<blocks, THREADS, lds, s>>>(a, SmallScale{(float)k.sx, (float)k.sa, (float)k.sb, (float)k.growth});
     return hipGetLastError();
 }
 
@@ -1158,7 +1194,7 @@ template <typename T, int F> hipError_t run_steps(const OrthoCall& c, GemmArgs g
     const Choice gram = choose(F, GRAM, chunk), poly = choose(F, POLY, chunk), apply = choose(F, APPLY, chunk);
     hipError_t e = hipSuccess;
     for (int step = 0; step < c.steps && e == hipSuccess; step++) {
-        g.from = step & 1;
+        g.from = step & 1, g.step = step;
         g.f0 = 0, g.f1 = k.sa / (k.sx * k.sx);
         e = gemm<T, F, GRAM>(g, chunk, gram, s);
         if (e != hipSuccess) break;
@@ -1186,7 +1222,7 @@ template <typename T, int F> hipError_t run_large(const OrthoCall& c, const Rule
         PackArgs p{};
         GemmArgs g{};
         int64_t norm_blocks = 0, pack_blocks = 0;
-        p.r = g.r = rule, p.scale = scales.sx, p.count = g.count = chunk.count;
+        p.r = g.r = rule, p.scale = scales.sx, p.growth = g.growth = (float)scales.growth, p.count = g.count = chunk.count;
         for (int k = 0; k < chunk.count; k++) {
             const Shape& sh = chunk.shape[k];
             PackEntry& e = p.e[k];
@@ -1196,7 +1232,7 @@ template <typename T, int F> hipError_t run_large(const OrthoCall& c, const Rule
             ws += chunk.batch[k] * norm_bytes(sh);
             e.first = (int32_t)norm_blocks;
             norm_blocks += chunk.batch[k] * e.chunks;
-            g.e[k] = {e.work, target_of(*entry[k], c), sh.m, sh.n, 0};
+            g.e[k] = {e.work, e.part + e.chunks, target_of(*entry[k], c), sh.m, sh.n, 0, e.chunks + 1};
         }
         g.part = ws;
         ws += choose(F, GRAM, chunk).bytes;

@@ -55,7 +55,7 @@ int chunks_of(const Shape& s) {
 int64_t large_bytes(int format, const Shape& s) {
     return layout_of((int)up64(s.m), (int)up64(s.n), unit_of(format)).size;
 }
-int64_t norm_bytes(const Shape& s) { return (chunks_of(s) * 8 + 255) / 256 * 256; }
+int64_t norm_bytes(const Shape& s) { return ((chunks_of(s) + 1) * 8 + 255) / 256 * 256; }
 
 bool all_small(int type, const ql_matrix* mats, int count) {
     for (int k = 0; k < count; k++)
@@ -66,8 +66,14 @@ bool all_small(int type, const ql_matrix* mats, int count) {
 Scales scales_of(const OrthoCall& c) {
     double most_x = 1, most_q = 1;
     ortho_bounds(c.a, c.b, c.c, c.steps, most_x, most_q);
+    // |a + b t + c t^2| over t = x^2 from 0 on, at its ends and its extremum
+    const double most_t = most_x * most_x, inner = c.c != 0 ? -c.b / (2 * c.c) : 0;
+    auto factor = [&](double t) { return std::fabs(c.a + t * (c.b + c.c * t)); };
+    double most = std::max(factor(0), factor(most_t));
+    if (inner > 0 && inner < most_t) most = std::max(most, factor(inner));
+    const double growth = std::log2(std::max(most, 1e-30)) + std::log2(1 + 1.0 / 256);  // the margin of ortho_bounds
     return {std::exp2(std::floor(std::log2(32768 / most_x))), std::exp2(std::floor(std::log2(32768 / (most_x * most_x)))),
-            std::exp2(std::floor(std::log2(32768 / std::max(most_q, 1e-3))))};
+            std::exp2(std::floor(std::log2(32768 / std::max(most_q, 1e-3)))), growth};
 }
 
 int64_t tiles_of(int mode, int64_t bt, int m, int n) {

@@ -70,7 +70,7 @@ constexpr Layout layout_of(int mp, int np, int unit) {
     return {0, x, 3 * x, 3 * x + s, 3 * x + 2 * s};
 }
 
-// Workspace of a matrix: X, A and B, then the norm's sums.
+// Workspace of a matrix: X, A and B, then the norm's sums and X's exponent.
 int64_t large_bytes(int format, const Shape& s);
 int64_t norm_bytes(const Shape& s);
 // Workgroups of the norm: each takes at least 4096 elements, and whole lines.
@@ -78,6 +78,7 @@ int chunks_of(const Shape& s);
 
 struct Scales {  // powers of two that bring the largest possible values to at most 2^15
     double sx = 1, sa = 1, sb = 1;
+    double growth = 0;  // log2 of what a step multiplies a singular value by at most
 };
 Scales scales_of(const OrthoCall& c);
 

@@ -123,3 +123,45 @@ def test_long_sums_of_few_rows(need_gpu, rows, cols, beside, batch, kind):
     grow = math.sqrt(max(1.0, rows / cols))
     for k in (0, batch // 2, batch - 1):
         near(p[0][k], u[k].cpu(), torch.float32, f"{rows}x{cols} {kind}, matrix {k}", sign=-1 / grow)
+
+
+def low_model(u, steps, coef, eps):
+    """The model with X held as finely below 1 as at 1: at its own norm's bound,
+    which no step raises by more than the polynomial's largest slope from 0."""
+    if u.shape[0] > u.shape[1]:
+        return low_model(u.T.contiguous(), steps, coef, eps).T
+    a, b, c = coef
+    product = lambda p, q: torch.matmul((p * 2.0 ** 40).float(), q.float()).double() * 2.0 ** -40  # noqa: E731
+    size = min(1.0, (u.norm() / (u.norm() + eps)).item())
+    x = held(u / (u.norm() + eps), size)
+    for _ in range(steps):
+        x1 = x / size
+        g = held(product(x1, x1.T.contiguous()) * size * size, 1.0)
+        grown = min(1.0, size * a)
+        x = held(a * x + product(held(b * g + c * product(g, g), 4.0), x1) * size, grown)
+        size = grown
+    return x
+
+
+@gpu
+@pytest.mark.parametrize("steps,coef", [(5, COEF), (1, COEF), (64, (1.5, -0.5, 0.0))])
+@pytest.mark.parametrize("norm", [1e-5, 1e-7, 3e-10, 1e-12, 1e-15, 3e-17, 1e-20, 1e-30])
+@pytest.mark.parametrize("name,rows,cols", [("f32", 12, 30), ("bf16", 40, 30), ("f32", 100, 130), ("f32", 500, 300), ("f32", 40, 3000)])
+def test_updates_far_below_eps(need_gpu, name, rows, cols, norm, steps, coef):
+    """X = U / (|U| + eps) is then small, and so is the result: no fewer of its
+    bits are right for that."""
+    u = update(rows, cols, "noise", torch.float64, seed=rows)
+    u = (u * (norm / u.norm())).to(TYPES[name])
+    got = Q.orthogonalize(u.cuda(), steps, coef).cpu().double()
+    d = u.double()
+    want = d if rows <= cols else d.T
+    want = want / (d.norm() + EPS)
+    for _ in range(steps):
+        g = want @ want.T
+        want = coef[0] * want + (coef[1] * g + coef[2] * g @ g) @ want
+    want = want if rows <= cols else want.T
+    size = want.norm().item()
+    bound = (3 * (low_model(d, steps, coef, EPS) - want).norm().item() + 2e-6 * size
+             + 1.1 * (want.to(TYPES[name]).double() - want).norm().item())
+    off = (got - want).norm().item()
+    assert off <= bound, f"{off / size:.3e} of the result, bound {bound / size:.3e}"
