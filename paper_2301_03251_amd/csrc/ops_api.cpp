@@ -51,7 +51,7 @@ int check_shapes(int type, const ql_matrix* mats, int32_t count) {
     if (!known_type(type)) return fail(QL_EINVAL, "unknown type");
     if (count < 0) return fail(QL_EINVAL, "count must be >= 0");
     if (count > 0 && !mats) return fail(QL_EINVAL, "matrices is NULL");
-    int64_t tiles = 0;  // of 64x64, as launches count them
+    int64_t tiles = 0;  // of 64x64, and rows
     for (int32_t k = 0; k < count; k++) {
         const ql_matrix& q = mats[k];
         if (q.rows < 1 || q.cols < 1 || q.rows > 65536 || q.cols > 65536)
@@ -61,6 +61,7 @@ int check_shapes(int type, const ql_matrix* mats, int32_t count) {
         tiles += q.batch * each;
         if (tiles > INT32_MAX) return fail(QL_EINVAL, "too many matrices for one call");
     }
+    if (!ortho_launchable(type, mats, count)) return fail(QL_EINVAL, "too many matrices for one call");
     return QL_OK;
 }
 

@@ -126,7 +126,7 @@ __device__ __forceinline__ float power_of_two(int e) { return __builtin_ldexpf(1
 struct SmallEntry {
     Source s;
     Target t;
-    int32_t m, n, first, batch;
+    int32_t m, n, first;
 };
 struct SmallArgs {
     SmallEntry e[ENTRIES];
@@ -1123,20 +1123,29 @@ template <typename T, int THREADS> hipError_t launch_tiny(const SmallArgs& a, un
 }
 
 template <typename T> hipError_t run_small(const OrthoCall& c, const Rule& rule, hipStream_t s) {
+    constexpr int64_t SIZE = sizeof(T), STATE = sizeof(Acc<T>);
+    int64_t done = 0;  // matrices of entry `at` that earlier launches took
     for (int at = 0; at < c.count;) {
         SmallArgs a{};
         a.r = rule, a.a = c.a, a.b = c.b, a.c = c.c, a.steps = c.steps;
         size_t lds = 0;
         int64_t blocks = 0, most = 0;
-        for (; at < c.count && a.count < ENTRIES; at++) {
+        while (at < c.count && a.count < ENTRIES && blocks < MOST_SMALL) {
             const ql_matrix& q = c.mats[at];
-            if (q.batch == 0) continue;
-            const Shape sh = shape_of(q);
-            if (blocks + q.batch > INT32_MAX) break;
-            a.e[a.count++] = {source_of(q, c.muon), target_of(q, c), sh.m, sh.n, (int32_t)blocks, (int32_t)q.batch};
-            blocks += q.batch;
-            most = std::max(most, (int64_t)sh.m * sh.n);
-            lds = std::max(lds, std::is_same_v<T, double> ? small_lds(sh.m, sh.n, 8) : tiny_lds(sh.m, sh.n));
+            const int64_t n = std::min(q.batch - done, MOST_SMALL - blocks);
+            if (n > 0) {
+                const Shape sh = shape_of(q);
+                SmallEntry& e = a.e[a.count++];
+                e = {source_of(q, c.muon), target_of(q, c), sh.m, sh.n, (int32_t)blocks};
+                e.s.grad = (const char*)e.s.grad + done * e.s.gb * SIZE;
+                if (c.muon) e.s.momentum = (char*)e.s.momentum + done * e.s.mb * STATE;
+                e.t.out = (char*)e.t.out + done * e.t.ob * SIZE;
+                blocks += n;
+                most = std::max(most, (int64_t)sh.m * sh.n);
+                lds = std::max(lds, std::is_same_v<T, double> ? small_lds(sh.m, sh.n, 8) : tiny_lds(sh.m, sh.n));
+            }
+            done += n;
+            if (done == q.batch) at++, done = 0;
         }
         if (!blocks) continue;
         hipError_t e;
@@ -1164,7 +1173,6 @@ template <typename T, int F, int MODE, int SPLIT, int BT> hipError_t gemm(GemmAr
         blocks += batch[k] * tiles_of(MODE, BT, a.e[k].m, a.e[k].n);
     }
     if (SPLIT == PART) blocks *= a.splits;
-    if (blocks > INT32_MAX) return hipErrorInvalidValue;
     constexpr int WJ = BT >= 192 ? 4 : 2, STAGES = BT == 64 ? 4 : BT == 192 ? 3 : 2;
     // only the last product sees the caller's type
     using K = std::conditional_t<MODE == LAST, T, std::conditional_t<F == TWO, float, double>>;
@@ -1236,14 +1244,12 @@ template <typename T, int F> hipError_t run_large(const OrthoCall& c, const Rule
         }
         g.part = ws;
         ws += choose(F, GRAM, chunk).bytes;
-        if (norm_blocks > INT32_MAX) return hipErrorInvalidValue;
         k_ortho_norm<T><<<(unsigned)norm_blocks, 256, 0, s>>>(p);
         if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
         for (int k = 0; k < chunk.count; k++) {
             p.e[k].first = (int32_t)pack_blocks;
             pack_blocks += chunk.batch[k] * (up64(p.e[k].m) / 64) * (up64(p.e[k].n) / 64);
         }
-        if (pack_blocks > INT32_MAX) return hipErrorInvalidValue;
         k_ortho_pack<T, F><<<(unsigned)pack_blocks, 256, 0, s>>>(p);
         if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
         if (hipError_t e = run_steps<T, F>(c, g, chunk, scales, s); e != hipSuccess) return e;

@@ -27,6 +27,9 @@ struct OrthoCall {
 // past 64, or is no number.
 bool ortho_bounds(double a, double b, double c, int steps, double& most_x, double& most_q);
 
+// Whether every launch of a call stays below 2^32 threads. (What fails it has a
+// workspace of more than 288 GB.)
+bool ortho_launchable(int type, const ql_matrix* mats, int count);
 size_t ortho_workspace(int type, const ql_matrix* mats, int count);
 hipError_t launch_ortho(const OrthoCall& c, void* ws, hipStream_t s);
 

@@ -146,6 +146,18 @@ bool ortho_bounds(double a, double b, double c, int steps, double& most_x, doubl
     return true;
 }
 
+bool ortho_launchable(int type, const ql_matrix* mats, int count) {
+    if (all_small(type, mats, count)) return true;
+    // no launch has more workgroups than one for every 64x64 of X (the norm's take
+    // 4096 elements or more, and what a split adds stays below 2 UNITS), of at most 512 threads
+    int64_t tiles = 0;
+    for (int k = 0; k < count; k++) {
+        const Shape s = shape_of(mats[k]);
+        tiles += mats[k].batch * tiles_of(APPLY, 64, s.m, s.n);
+    }
+    return tiles < ((int64_t)1 << 32) / 512;
+}
+
 size_t ortho_workspace(int type, const ql_matrix* mats, int count) {
     if (all_small(type, mats, count)) return 0;
     const int format = type == E_F64 ? DOUBLE : TWO;

@@ -45,6 +45,8 @@ inline size_t tiny_lds(int m, int n) {
 // Whether one workgroup's LDS holds the matrix; all of the call's.
 bool is_small(int type, const Shape& s);
 bool all_small(int type, const ql_matrix* mats, int count);
+// Matrices of a launch: a launch's threads number less than 2^32, of 1024 at most each.
+constexpr int64_t MOST_SMALL = (1 << 22) - 1;
 
 // ---------------------------------------------------------------------------
 // Large matrices in the workspace. Formats of X, A and B: two fp16 parts (32

@@ -93,3 +93,56 @@ def test_growth_between_zero_and_one_is_seen(a, b, c):
         reach = max(abs(x * (a + x * x * (b + c * x * x))) for x in (reach * i / 1000 for i in range(1001)))
     assert reach > 64
     assert orthogonalize([(200, 300, 1)], ortho=Ortho(a, b, c, 1e-7, 4), ws=FAKE, ws_bytes=1 << 40) == -1
+
+
+def workspace(entries, type_=F32):
+    words = array.array("q", [v for r, c, b in entries for v in (r, c, b, *(0,) * 12)])
+    out = ctypes.c_size_t()
+    return Q.load().ql_orthogonalize_workspace_bytes(type_, words.buffer_info()[0], len(entries), ctypes.byref(out)), out.value
+
+
+@pytest.mark.parametrize("type_", [F32, F64, BF16])
+def test_matrices_of_a_call(type_):
+    """2^32 threads in workgroups of 512, one for each 64x64: 2^23 of them are refused before anything runs."""
+    most = (1 << 23) - 1
+    assert workspace([(65, 65, most // 4)], type_)[0] == 0
+    assert workspace([(65, 65, most // 4 + 1)], type_)[0] == -1
+    assert workspace([(65, 65, 1), (3, 3, most - 4)], type_)[0] == 0
+    assert workspace([(65, 65, 1), (3, 3, most - 3)], type_)[0] == -1
+    assert orthogonalize([(65, 65, most // 4 + 1)], type_, ws=FAKE, ws_bytes=1 << 62) == -1
+    # matrices that one workgroup holds go in as many launches as it takes
+    assert workspace([(3, 3, 1 << 28)], type_) == (0, 0)
+
+
+@gpu
+@pytest.mark.parametrize("name,rows,cols,batch", [("float32", 2, 2, (1 << 23) + 5), ("float64", 1, 2, (1 << 23) + 5),
+                                                  ("bfloat16", 33, 64, (1 << 22) + 5)])
+def test_batches_of_more_threads_than_a_launch(need_gpu, name, rows, cols, batch):
+    """As the same matrices in a smaller batch, bit by bit, past the first launch too."""
+    torch.manual_seed(0)
+    dtype = getattr(torch, name)
+    few = torch.randn(7, rows, cols, device="cuda").to(dtype)
+    want = Q.orthogonalize(few)
+    out = torch.zeros(batch, rows, cols, dtype=dtype, device="cuda")
+    if rows * cols < 10:
+        g = few.repeat(batch // 7 + 1, 1, 1)[:batch]
+        Q.orthogonalize(g, out=out)
+        assert torch.equal(out, want.repeat(batch // 7 + 1, 1, 1)[:batch])
+    else:  # one matrix throughout: 18 GB of results are enough
+        Q.orthogonalize(few[:1].expand(batch, rows, cols), out=out)
+        assert (out == want[:1]).all()
+
+
+@gpu
+def test_muon_steps_of_more_threads_than_a_launch(need_gpu):
+    torch.manual_seed(1)
+    batch = (1 << 22) + 9
+    p = [torch.randn(s, device="cuda") for s in ((3, 2, 3), (batch, 2, 2), (5, 4, 4))]
+    g, m = [torch.randn_like(t) for t in p], [torch.randn_like(t) for t in p]
+    q, n = [t.clone() for t in p], [t.clone() for t in m]
+    Q.muon_step(p, g, m)
+    half = batch // 2
+    for part in (slice(0, half), slice(half, None)):
+        Q.muon_step([q[1][part]], [g[1][part]], [n[1][part]])
+    Q.muon_step([q[0], q[2]], [g[0], g[2]], [n[0], n[2]])
+    assert all(torch.equal(a, b) for a, b in zip(p + m, q + n))
