@@ -99,14 +99,9 @@ template <typename E> __device__ __forceinline__ int entry_of(const E* e, int co
 __device__ __forceinline__ double4v mma4(double a, double b, double4v c) {
     return __builtin_amdgcn_mfma_f64_16x16x4f64(a, b, c, 0, 0, 0);
 }
-template <typename R> struct Quad;
-template <> struct Quad<float> { using type = float4v; };
-template <> struct Quad<double> { using type = double4v; };
-// Where register r of lane l of a 16x16 product lies: the row (the first
+// Where register r of lane l of such a 16x16 product lies: the row (the first
 // operand's); the column (the second's) is l % 16.
-template <typename R> __device__ __forceinline__ int mma_row(int lane, int r) {
-    return sizeof(R) == 4 ? 4 * (lane / 16) + r : lane / 16 + 4 * r;
-}
+__device__ __forceinline__ int mma4_row(int lane, int r) { return lane / 16 + 4 * r; }
 
 // Where |U| is far below eps, X is far below 1, and fp16 parts at the scale of 1
 // would lose its bits. |X| <= 2^e (0: no information) in the Frobenius norm at
@@ -135,30 +130,28 @@ struct SmallArgs {
     int32_t count, steps;
 };
 
-template <typename T> __global__ __launch_bounds__(SMALL_THREADS) void k_ortho_small(SmallArgs a) {
-    using R = Acc<T>;
-    using Q = typename Quad<R>::type;
+__global__ __launch_bounds__(SMALL_THREADS) void k_ortho_small(SmallArgs a) {
     extern __shared__ double lds_small[];
     __shared__ double norm_part[SMALL_THREADS / 64];
     const SmallEntry& e = a.e[entry_of(a.e, a.count, blockIdx.x)];
     const int64_t b = blockIdx.x - e.first;
     const int m = e.m, n = e.n, mp = up16(m), np = up16(n), ldx = np + 4, lda = mp + 4;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = SMALL_THREADS / 64;
-    R *X = (R*)lds_small, *A = X + mp * ldx, *B = A + mp * lda;
+    double *X = lds_small, *A = X + mp * ldx, *B = A + mp * lda;
 
     const bool by_row = e.s.gj == 1 || e.s.gi != 1;  // the order of the addresses
     double sq = 0;
     for (int k = threadIdx.x; k < mp * np; k += SMALL_THREADS) {
         const int i = by_row ? k / np : k % mp, j = by_row ? k % np : k / mp;
-        R u = 0;
-        if (i < m && j < n) u = first_update<T>(e.s, a.r, b, i, j);
+        double u = 0;
+        if (i < m && j < n) u = first_update<double>(e.s, a.r, b, i, j);
         X[i * ldx + j] = u;
-        sq += (double)u * (double)u;
+        sq += u * u;
     }
     const double inv = 1.0 / (sqrt(group_sum<SMALL_THREADS>(sq, norm_part)) + a.r.eps);
     for (int k = threadIdx.x; k < mp * np; k += SMALL_THREADS) {
-        R& x = X[(k / np) * ldx + k % np];
-        x = (R)((double)x * inv);
+        double& x = X[(k / np) * ldx + k % np];
+        x *= inv;
     }
     __syncthreads();
 
@@ -166,23 +159,23 @@ template <typename T> __global__ __launch_bounds__(SMALL_THREADS) void k_ortho_s
     for (int step = 0; step < a.steps; step++) {
         // A = X X^T, then B = b A + c A A: tiles on and below the diagonal, each written twice
         for (int which = 0; which < 2; which++) {
-            const R *S = which ? A : X;
-            R* D = which ? B : A;
+            const double *S = which ? A : X;
+            double* D = which ? B : A;
             const int ld = which ? lda : ldx, depth = which ? mp : np;
             for (int t = wave; t < mt * (mt + 1) / 2; t += waves) {
                 int ti = 0, tj = t;
                 while (tj > ti) tj -= ++ti;
-                Q acc[2] = {};
-                const R *p = S + (ti * 16 + row) * ld + part, *q = S + (tj * 16 + row) * ld + part;
+                double4v acc[2] = {};
+                const double *p = S + (ti * 16 + row) * ld + part, *q = S + (tj * 16 + row) * ld + part;
                 for (int k = 0; k < depth; k += 8) {
                     acc[0] = mma4(p[k], q[k], acc[0]);
                     acc[1] = mma4(p[k + 4], q[k + 4], acc[1]);
                 }
 #pragma unroll
                 for (int r = 0; r < 4; r++) {
-                    const int i = ti * 16 + mma_row<R>(lane, r), j = tj * 16 + row;
-                    R v = acc[0][r] + acc[1][r];
-                    if (which) v = (R)a.b * A[i * lda + j] + (R)a.c * v;
+                    const int i = ti * 16 + mma4_row(lane, r), j = tj * 16 + row;
+                    double v = acc[0][r] + acc[1][r];
+                    if (which) v = a.b * A[i * lda + j] + a.c * v;
                     D[i * lda + j] = v;
                     if (ti != tj) D[j * lda + i] = v;
                 }
@@ -191,9 +184,9 @@ template <typename T> __global__ __launch_bounds__(SMALL_THREADS) void k_ortho_s
         }
         // X = a X + B X, 16 columns at a time: only their own wavefront reads or writes them
         for (int t = wave; t < nt; t += waves) {
-            Q acc[SMALL_M / 16] = {};
+            double4v acc[SMALL_M / 16] = {};
             for (int k = 0; k < mp; k += 4) {
-                const R x = X[(k + part) * ldx + t * 16 + row];
+                const double x = X[(k + part) * ldx + t * 16 + row];
 #pragma unroll
                 for (int i = 0; i < SMALL_M / 16; i++)
                     if (i < mt) acc[i] = mma4(B[(i * 16 + row) * lda + k + part], x, acc[i]);
@@ -203,8 +196,8 @@ template <typename T> __global__ __launch_bounds__(SMALL_THREADS) void k_ortho_s
                 if (i < mt)
 #pragma unroll
                     for (int r = 0; r < 4; r++) {
-                        R& x = X[(i * 16 + mma_row<R>(lane, r)) * ldx + t * 16 + row];
-                        x = (R)a.a * x + acc[i][r];
+                        double& x = X[(i * 16 + mma4_row(lane, r)) * ldx + t * 16 + row];
+                        x = a.a * x + acc[i][r];
                     }
         }
         __syncthreads();
@@ -212,7 +205,7 @@ template <typename T> __global__ __launch_bounds__(SMALL_THREADS) void k_ortho_s
     const bool out_by_row = e.t.oj == 1 || e.t.oi != 1;
     for (int k = threadIdx.x; k < m * n; k += SMALL_THREADS) {
         const int i = out_by_row ? k / n : k % m, j = out_by_row ? k % n : k / m;
-        write_out<T>(e.t, a.r, b, i, j, X[i * ldx + j]);
+        write_out<double>(e.t, a.r, b, i, j, X[i * ldx + j]);
     }
 }
 
@@ -713,8 +706,7 @@ template <typename T, int F, int MODE, int SPLIT, int BT, int WI, int WJ, int ST
 __global__ __launch_bounds__(64 * WI * WJ, 2) void k_ortho_gemm(GemmArgs a) {
     constexpr int U = unit_of(F), THREADS = 64 * WI * WJ, TI = BT / WI / 16, TJ = BT / WJ / 16;
     constexpr int LOADS = BT * 8 / THREADS;  // of a thread, for each operand
-    using R = Acc<T>;
-    using Q = typename Quad<R>::type;
+    using Q = std::conditional_t<F == DOUBLE, double4v, float4v>;
     STAGE(s0);
     STAGE(s1);
     const int all = SPLIT == PART ? gridDim.x / a.splits : gridDim.x;
@@ -944,7 +936,7 @@ __global__ __launch_bounds__(64 * WI * WJ, 2) void k_ortho_gemm(GemmArgs a) {
             for (int j = 0; j < TJ; j++)
 #pragma unroll
                 for (int r = 0; r < 4; r++) {
-                    const int gi = i0 + i * 16, gj = j0 + j * 16 + mma_row<R>(lane, r);
+                    const int gi = i0 + i * 16, gj = j0 + j * 16 + mma4_row(lane, r);
                     if (gi >= left_rows || gj >= right_rows) continue;
                     double v = a.f1 * acc[i][j][r];
                     if constexpr (MODE == POLY) v += a.f0 * get(w + l.a, gi, lda, gj);
@@ -1151,9 +1143,9 @@ template <typename T> hipError_t run_small(const OrthoCall& c, const Rule& rule,
         hipError_t e;
         if constexpr (std::is_same_v<T, double>) {
             static std::atomic<uint64_t> ready{0};
-            e = allow_lds((const void*)k_ortho_small<T>, ready, SMALL_LDS);
+            e = allow_lds((const void*)k_ortho_small, ready, SMALL_LDS);
             if (e != hipSuccess) return e;
-            k_ortho_small<T><<<(unsigned)blocks, SMALL_THREADS, lds, s>>>(a);
+            k_ortho_small<<<(unsigned)blocks, SMALL_THREADS, lds, s>>>(a);
             e = hipGetLastError();
         } else {
             const Scales k = scales_of(c);
