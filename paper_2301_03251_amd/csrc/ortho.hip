@@ -211,9 +211,9 @@ __global__ __launch_bounds__(SMALL_THREADS) void k_ortho_small(SmallArgs a) {
 
 // Small matrices of the other types: as above with the fp16 products of the
 // large ones, X, its transpose and A (then B in its place) in LDS in two parts.
-// Each of the 16 wavefronts (8 for little work) takes a 16x16 tile of A and of
+// Each of the 16 wavefronts (8 for up to 128 columns) takes a 16x16 tile of A and of
 // B, and 16 or 32 columns of X, which nobody else reads or writes until the step's
-// end. 16 matrices of 64x256 take 36 us, one of 20x72 15 us: 11 and 6 us of them
+// end. 16 matrices of 64x256 take 37 us, one of 20x72 16 us: 11 and 6 us of them
 // for reading, the norm and writing, 5 and 1.8 us a step, which is the way from
 // barrier to barrier of four phases. With the fp32 products above (16x16x4, a
 // sixteenth of the rate) it was 95 and 19 us.
@@ -1121,7 +1121,8 @@ template <typename T> hipError_t run_small(const OrthoCall& c, const Rule& rule,
         SmallArgs a{};
         a.r = rule, a.a = c.a, a.b = c.b, a.c = c.c, a.steps = c.steps;
         size_t lds = 0;
-        int64_t blocks = 0, most = 0;
+        int64_t blocks = 0;
+        int widest = 0;
         while (at < c.count && a.count < ENTRIES && blocks < MOST_SMALL) {
             const ql_matrix& q = c.mats[at];
             const int64_t n = std::min(q.batch - done, MOST_SMALL - blocks);
@@ -1133,7 +1134,7 @@ template <typename T> hipError_t run_small(const OrthoCall& c, const Rule& rule,
                 if (c.muon) e.s.momentum = (char*)e.s.momentum + done * e.s.mb * STATE;
                 e.t.out = (char*)e.t.out + done * e.t.ob * SIZE;
                 blocks += n;
-                most = std::max(most, (int64_t)sh.m * sh.n);
+                widest = std::max(widest, sh.n);
                 lds = std::max(lds, std::is_same_v<T, double> ? small_lds(sh.m, sh.n, 8) : tiny_lds(sh.m, sh.n));
             }
             done += n;
@@ -1149,7 +1150,10 @@ template <typename T> hipError_t run_small(const OrthoCall& c, const Rule& rule,
             e = hipGetLastError();
         } else {
             const Scales k = scales_of(c);
-            e = most <= 2048 ? launch_tiny<T, 512>(a, (unsigned)blocks, lds, k, s) : launch_tiny<T, 1024>(a, (unsigned)blocks, lds, k, s);
+            // eight wavefronts hold 128 columns at once; sixteen then only wait for each other
+            // (32x128 16.5 us with 8 and 19.2 with 16, 64x128 27.1 and 28.8, 600 of 64x64 48 and
+            // 80), but share what is wider (8x144 15.8 and 15.0, 64x144 34.4 and 30.3, 64x256 42 and 37)
+            e = widest <= 128 ? launch_tiny<T, 512>(a, (unsigned)blocks, lds, k, s) : launch_tiny<T, 1024>(a, (unsigned)blocks, lds, k, s);
         }
         if (e != hipSuccess) return e;
     }
