@@ -26,7 +26,8 @@ struct NormArgs {
     void* grad_weight;   // [D] or null (backward)
     void* grad_bias;     // [D] or null (backward)
     void* part;          // workspace: the column sums of each workgroup,
-    void* sums;          // and of long rows the sums of each segment
+    void* sums;          // of long rows the sums of each segment,
+    void* joined;        // and of very long ones the rows' own, or null
     int64_t rows, D, x_stride, grad_stride;
     double eps;
 };

@@ -146,3 +146,64 @@ def test_muon_steps_of_more_threads_than_a_launch(need_gpu):
         Q.muon_step([q[1][part]], [g[1][part]], [n[1][part]])
     Q.muon_step([q[0], q[2]], [g[0], g[2]], [n[0], n[2]])
     assert all(torch.equal(a, b) for a, b in zip(p + m, q + n))
+
+
+def norm_near(rows, n, dtype, segment):
+    """y, grad_x and the column sums of n features in segments, against 64 bits; the bounds as above."""
+    torch.manual_seed(n)
+    x = (torch.randn(rows, n, device="cuda") + 0.5).to(dtype)
+    w = (1 + 0.2 * torch.randn(n, device="cuda")).to(dtype)
+    g = torch.randn(rows, n, device="cuda").to(dtype)
+    y, mean, rstd = Q.layer_norm_forward(x, w)
+    gx, gw, gb = Q.layer_norm_backward(g, x, mean, rstd, w)
+    u = 2.0 ** -53 if dtype == torch.float64 else 2.0 ** -24
+    out = 1.01 * {torch.float64: 2.0 ** -53, torch.float32: 2.0 ** -24, torch.bfloat16: 2.0 ** -8}[dtype]
+    s = 80 + n / segment / 64
+    xd, gd, wd = x.double(), g.double(), w.double()
+    m = xd.mean(1, keepdim=True)
+    r = 1 / ((xd - m).square().mean(1, keepdim=True) + 1e-5).sqrt()
+    h = (xd - m) * r
+    off = s * u * xd.abs().amax(1, keepdim=True) * r + (s + 4) * u
+    dh = (1 + h.abs()) * off
+    v = gd * wd
+    within(y, h * wd, wd.abs() * dh + (3 * u + out) * (h * wd).abs(), "y")
+    c1, c2 = v.mean(1, keepdim=True), (v * h).mean(1, keepdim=True)
+    want = r * (v - c1 - h * c2)
+    e1 = (s + 2) * u * v.abs().mean(1, keepdim=True)
+    e2 = (s + 4) * u * (v * h).abs().mean(1, keepdim=True) + (v.abs() * dh).mean(1, keepdim=True)
+    bound = r * (4 * u * (v.abs() + c1.abs() + (h * c2).abs()) + e1 + h.abs() * e2 + c2.abs() * dh)
+    within(gx, want, bound + want.abs() * (2 * off + out), "grad_x")
+    gh = gd * h
+    within(gw, gh.sum(0), (gd.abs() * dh).sum(0) + (rows + 7) * u * gh.abs().sum(0) + out * gh.sum(0).abs(), "grad_weight")
+    within(gb, gd.sum(0), (rows + 7) * u * gd.abs().sum(0) + out * gd.sum(0).abs(), "grad_bias")
+
+
+@gpu
+@pytest.mark.parametrize("name,segment", [("float32", 1024), ("float64", 512), ("bfloat16", 2048)])
+@pytest.mark.parametrize("rows", [1, 3])
+@pytest.mark.parametrize("past", [-1, 0, 1, 700])
+def test_norm_where_segments_are_joined_apart(need_gpu, name, segment, rows, past):
+    norm_near(rows, 256 * segment + past, getattr(torch, name), segment)
+
+
+@gpu
+def test_norm_takes_time_as_its_row_is_long(need_gpu):
+    """Four times the features take about four times as long: joined again for every
+    segment they took 13 times, and 2^30 of them seconds."""
+    times = []
+    for n in (1 << 24, 1 << 26):
+        x, g = torch.randn(1, n, device="cuda"), torch.randn(1, n, device="cuda")
+        y, m, r = Q.layer_norm_forward(x)
+        ways = (lambda: Q.layer_norm_forward(x), lambda: Q.layer_norm_backward(g, x, m, r))
+        for f in ways:
+            f()
+            least = math.inf
+            for _ in range(3):
+                a, b = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+                a.record()
+                f()
+                b.record()
+                torch.cuda.synchronize()
+                least = min(least, a.elapsed_time(b))
+            times.append(least)
+    assert times[2] < 8 * times[0] and times[3] < 8 * times[1], times
