@@ -405,14 +405,17 @@ int ql_layer_norm_backward(ql_type type, ql_type weight_type, int64_t rows, int6
  * be grad's array in ql_orthogonalize where the strides are equal. All entries of
  * a call run together: give a network's matrices in one call.
  *
- * Precision: QL_F64 in fp64. Other products are fp16 ones that keep 22 bits of
- * every factor (in two parts); sums are fp32, norms fp64. A matrix's last bits
- * can depend on what else the call holds (the tiles follow from all of it), and
- * nothing else: the same call gives the same bits.
+ * Precision: QL_F64 in fp64 (updates whose squares leave its range are not
+ * scaled). Other products are fp16 ones that keep 22 bits of every factor (in two
+ * parts); sums are fp32, norms fp64. A matrix's last bits can depend on what else
+ * the call holds (the tiles follow from all of it), and nothing else: the same
+ * call gives the same bits.
  *
  * options NULL: the defaults in braces. rows, cols in [1, 65536], steps in
  * [1, 64]; coefficients that let a singular value in [0, 1] grow past 64 before
- * the last step are refused. The entries are read during the call only. */
+ * the last step are refused, and so are 2^23 or more 64x64 blocks of matrices of
+ * which one is too large for a workgroup's LDS. The entries are read during the
+ * call only. */
 typedef struct {
     int64_t rows, cols, batch;
     const void* grad;

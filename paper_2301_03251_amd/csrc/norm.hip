@@ -101,7 +101,9 @@ __global__ __launch_bounds__(G > 256 ? G : 256) void k_norm_fwd(NormArgs a) {
 // Long rows go through the chip in segments of 256 vectors, one workgroup each,
 // in two launches: every segment's mean and sum of squares about it; then each
 // workgroup joins its row's (in the same order everywhere) and writes its
-// segment of y. x is read twice, by as many workgroups as there are segments.
+// segment of y. x is read twice, by as many workgroups as there are segments: no
+// workgroup's registers hold such a row. That is 1.5 times the bytes where the
+// array is larger than the caches; where it is not, the second read is theirs.
 template <typename T> constexpr int SEGMENT = 256 * VEC<T>;
 
 template <typename T> __global__ __launch_bounds__(256) void k_norm_fwd_sums(NormArgs a, int segments) {
@@ -206,8 +208,8 @@ template <typename T, typename W> __global__ __launch_bounds__(256) void k_norm_
 // every lane sums its columns' g h and g over the rows that its group takes
 // (row, row + stride, ...). The next row's loads are under way while a row is
 // worked on. part[workgroup][2][D] gets the workgroup's sums, joined over its
-// groups in LDS; a null part leaves them out. 16384x8192 bf16: 150 us, 5.4 TB/s,
-// a copy's rate (one kernel for dx and one for the columns: 310 us).
+// groups in LDS; a null part leaves them out. 16384x8192 bf16: 156 us (median),
+// 5.2 of a copy's 5.3 TB/s (one kernel for dx and one for the columns: 310 us).
 template <typename T, typename W, int V, int G, int K>
 __global__ __launch_bounds__(G > 256 ? G : 256) void k_norm_bwd(NormArgs a) {
     using R = Acc<T>;
@@ -478,8 +480,8 @@ template <typename T, typename W, int G, int K, int V = VEC<T>> hipError_t forwa
     constexpr int threads = G > 256 ? G : 256, rows = threads / G;
     // many more workgroups than run at once, which leaves them out of step, but
     // few enough that each reads weight and bias for several rows: 16384x8192
-    // bf16 takes 100 us with 4096 of them (5.4 TB/s, a copy's rate), 111 with
-    // 512 and 124 with one for every row
+    // bf16 takes 113 us (median between events; a copy of as much 102) with 4096
+    // of them, 119 with 512 and 142 with one for every row
     k_norm_fwd<T, W, V, G, K><<<grid_of((a.rows + rows - 1) / rows), threads, 0, s>>>(a);
     return hipGetLastError();
 }

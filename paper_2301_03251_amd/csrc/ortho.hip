@@ -3,8 +3,8 @@
 //   X = U / (|U|_F + eps), m <= n;   steps times:  A = X X^T,  B = b A + c A^2,
 //   X = a X + B X.
 //
-// m^2 n + m^3 + 2 m^2 n operations a step (A and A^2 are symmetric: half of
-// each is computed) on m n values: matrix products. If all matrices of a call
+// 3 m^2 n + m^3 operations a step (A and A^2 are symmetric: half of each is
+// computed) on m n values: matrix products. If all matrices of a call
 // are small (m <= 64, and X, A and B fit one workgroup's LDS), they take one
 // launch, bound by its steps' latency; else all run together, tile by tile, in
 // three launches a step: bound by the launches up to some 1000 rows and columns,
@@ -215,8 +215,8 @@ __global__ __launch_bounds__(SMALL_THREADS) void k_ortho_small(SmallArgs a) {
 // B, and 16 or 32 columns of X, which nobody else reads or writes until the step's
 // end. 16 matrices of 64x256 take 37 us, one of 20x72 16 us: 11 and 6 us of them
 // for reading, the norm and writing, 5 and 1.8 us a step, which is the way from
-// barrier to barrier of four phases. With the fp32 products above (16x16x4, a
-// sixteenth of the rate) it was 95 and 19 us.
+// barrier to barrier of four phases. With fp32 products (16x16x4, a sixteenth of
+// the rate) it was 95 and 19 us.
 struct SmallScale {
     float sx, sa, sb, growth;
 };
@@ -694,14 +694,12 @@ template <int READS> __device__ __forceinline__ void spread() {
 // row are on their way to LDS, STAGES steps ahead, while the products of a step
 // run. Chunk q (16 bytes) of a row r lies at q ^ (r % 8): the rows that a
 // wavefront reads together start in different banks (no conflicts counted).
-// 256 is the tile whose products (2048 clocks of a unit a step in one part)
-// take as long as its LDS traffic; smaller ones fill the chip where there are
-// fewer tiles than units. Measured: X of 4096x4096 in one part 117 us (1.17
-// PFLOP/s; the clock falls to 2 GHz under it, and lower with inputs of wider
-// spread: 145 us), in two parts of 2048x8192 170 us (0.40 PFLOP/s, 1.2 of fp16
-// products); a step takes 1.49 us of 1.28 for its products alone. What is left is
-// the end: X read, X and X^T written at once by all units. Four wavefronts
-// instead of eight a tile, with fewer LDS reads, took 1.1 to 1.3 times as long.
+// 256 is the tile whose products take longer than its LDS traffic; smaller ones
+// fill the chip where there are fewer tiles than units. Measured: X of 4096x4096
+// in 312 us (median; 0.44 PFLOP/s, 1.32 of fp16 products, of the 1.43 that a large
+// fp16 product reaches), of 2048x8192 in 176 (0.39 and 1.17). What is left is the
+// end: X read, X and X^T written at once by all units. Four wavefronts instead of
+// eight a tile, with fewer LDS reads, took 1.1 to 1.3 times as long.
 template <typename T, int F, int MODE, int SPLIT, int BT, int WI, int WJ, int STAGES>
 __global__ __launch_bounds__(64 * WI * WJ, 2) void k_ortho_gemm(GemmArgs a) {
     constexpr int U = unit_of(F), THREADS = 64 * WI * WJ, TI = BT / WI / 16, TJ = BT / WJ / 16;
