@@ -834,14 +834,14 @@ __global__ __launch_bounds__(64 * WI * WJ, 2) void k_ortho_gemm(GemmArgs a) {
         __builtin_amdgcn_sched_barrier(0);
     };
     // Sums of squares grow with every product, and the matrix cores round each sum
-    // towards zero: after some 500 of K the sums so far are put aside. Sums of
+    // towards zero: after FOLDED of K the sums so far are put aside. Sums of
     // 5992 of twelve rows, for which nothing averages that out, were 6e-6 off in
     // one chain, 1e-6 so. Tiles past 128 have no registers for it (choose()).
     constexpr bool FOLD = MODE == GRAM && F == TWO && BT <= 128;
     [[maybe_unused]] Q aside[FOLD ? TI : 1][FOLD ? TJ : 1] = {};
     auto fold = [&](int k) {
         if constexpr (FOLD)
-            if ((k - begin) % (16 * 128) == 0) {
+            if ((k - begin) % (FOLDED * U) == 0) {
 #pragma unroll
                 for (int i = 0; i < TI; i++)
 #pragma unroll

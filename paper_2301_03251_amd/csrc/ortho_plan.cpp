@@ -86,7 +86,7 @@ Choice choose(int format, int mode, const Chunk& c) {
     if (format == DOUBLE) return best;
     // sums over a long side of few rows are for the tiles that fold them
     bool wide = false;
-    for (int k = 0; k < c.count; k++) wide |= c.shape[k].n > 4 * (int64_t)c.shape[k].m;
+    for (int k = 0; k < c.count; k++) wide |= c.shape[k].n > std::max<int64_t>(FOLDED, 4 * (int64_t)c.shape[k].m);
     double least = 0;
     for (int which = 0; which < (mode == GRAM && wide ? 2 : 4); which++) {
         int64_t tiles = 0;

@@ -92,6 +92,7 @@ Scales scales_of(const OrthoCall& c);
 enum Mode { GRAM, POLY, APPLY, LAST };
 
 constexpr int TILES[] = {64, 128, 192, 256};
+constexpr int FOLDED = 512;  // values after which a Gram product's sums are put aside, in tiles up to 128
 int64_t tiles_of(int mode, int64_t bt, int m, int n);
 
 // The entries of a table and their batches, as the costs go by them.

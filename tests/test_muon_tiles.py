@@ -68,6 +68,11 @@ def test_every_tile_size_is_reached(tmp_path):
         "small workspace 0", plan((0, [((1 << 23) - 1, 2, 65)] * 2))[0], "small workspace 0", plan((0, [(1, 65, 65)] * 60))[0]]
     assert plan((0, [(1 << 21, 65, 65)])) == ["refused"]
 
+    # a long side beside a large matrix keeps the Gram products to the tiles that fold their sums; a short one does not
+    gram = [int(re.search(r"gram (\d+)", line)[1]) for line in plan(*((0, [(1, 4096, 4096), *also]) for also in (
+        (), ((1, 6, 30),), ((1, 100, 512),), ((1, 12, 5992),), ((2, 700, 100),))))]
+    assert gram[0] > 128 and gram[1] == gram[2] == gram[0] and gram[3] <= 128 and gram[4] <= 128
+
 
 # ---------------------------------------------------------------------------
 # results
