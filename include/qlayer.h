@@ -447,6 +447,52 @@ int ql_muon_step(ql_type type, const ql_matrix* matrices, int32_t count,
                  const ql_muon_options* muon, const ql_ortho_options* options, void* workspace,
                  size_t workspace_bytes, hipStream_t stream);
 
+/* ---- operators of a network that reads sequences ---------------------------
+ *
+ * What stands in front of a quantum layer where features come from sequences of
+ * tokens. As the operators above: no circuit, no allocation, nothing kept, the
+ * given stream, capture in a graph, pointers that are multiples of the element's
+ * size, outputs and the workspace overlap nothing. Sums are fp64 for QL_F64 and fp32
+ * otherwise (fp64 where sums of workgroups are joined), in a fixed order. */
+
+/* Root-mean-square norm of rows of features, with the residual's addition:
+ *   s = x + residual (rounded to its type),  rstd = 1 / sqrt(sum s^2 / features + eps),
+ *   y = s * rstd * weight.
+ * Rows of x and residual start x_stride and residual_stride elements apart (>= 0);
+ * summed[rows][features] = s and y[rows][features] are contiguous. residual may
+ * be NULL (s = x, and summed is not written), weight too (1); its type is the
+ * rows', or QL_F32 beside 16-bit rows. rstd[rows] (QL_F64 for QL_F64, else
+ * QL_F32) is what the backward call needs and may be NULL. A row that holds NaN
+ * gives NaN in that row alone; one whose sum of squares is infinite has rstd 0, as
+ * the formula says (zeros, and NaN for an infinity itself). features in [1, 2^30];
+ * rows = 0 does nothing.
+ *
+ * scale not NULL: y is bytes in e4m3 (OCP FP8, largest value 448) instead, and
+ * scale[rows] (QL_F32) = max |s * rstd * weight| / 448 is what they are multiples of; a
+ * row of zeros has scale 0, and where the row holds an infinity or NaN the scale is
+ * NaN. Not for QL_F64 (QL_EUNSUPPORTED).
+ *
+ * The backward call: with h = s * rstd,
+ *   grad_x      = rstd * (g w - h * mean(g w h)) + grad_summed (NULL: 0),
+ *   grad_weight = sum over rows of g h,
+ * each of which may be NULL (not computed). grad_x is the residual's gradient too.
+ * The rows of s, grad_y and grad_summed start their strides apart.
+ *
+ * ql_rms_norm_workspace_bytes gives the device workspace of a forward (backward
+ * = 0) or backward call; where it is 0 the workspace may be NULL. */
+int ql_rms_norm_forward(ql_type type, ql_type weight_type, int64_t rows, int64_t features,
+                        const void* x, int64_t x_stride, const void* residual,
+                        int64_t residual_stride, const void* weight, double eps, void* summed,
+                        void* y, void* rstd, float* scale, void* workspace,
+                        size_t workspace_bytes, hipStream_t stream);
+int ql_rms_norm_workspace_bytes(ql_type type, int64_t rows, int64_t features, int backward,
+                                size_t* out);
+int ql_rms_norm_backward(ql_type type, ql_type weight_type, int64_t rows, int64_t features,
+                         const void* grad_y, int64_t grad_stride, const void* grad_summed,
+                         int64_t grad_summed_stride, const void* s, int64_t s_stride,
+                         const void* rstd, const void* weight, void* grad_x, void* grad_weight,
+                         void* workspace, size_t workspace_bytes, hipStream_t stream);
+
 /* Message of the last failing call on this thread ("" if none). */
 const char* ql_last_error(void);
 

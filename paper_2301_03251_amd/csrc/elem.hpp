@@ -1,5 +1,5 @@
-// elem.hpp -- device helpers of norm.hip and ortho.hip: element types, vectors
-// of them at any alignment, and sums over groups of lanes.
+// elem.hpp -- device helpers of the operators' kernels: element types, vectors of
+// them at any alignment, and sums over groups of lanes.
 #pragma once
 
 #include <hip/hip_runtime.h>
@@ -146,6 +146,35 @@ template <int N, typename R> __device__ __forceinline__ R group_sum(R v, R* lds)
 #pragma unroll
         for (int i = 0; i < N / 64; i++) t += lds[i];
         return t;
+    }
+}
+
+__device__ __forceinline__ float larger(float a, float b) { return fmaxf(a, b); }
+__device__ __forceinline__ double larger(double a, double b) { return fmax(a, b); }
+
+// The largest value over aligned groups of N = 16 or 64 lanes; every lane gets it.
+template <int N, typename R> __device__ __forceinline__ R lanes_max(R v) {
+    v = larger(v, dpp_move<0xB1>(v));
+    v = larger(v, dpp_move<0x4E>(v));
+    v = larger(v, dpp_move<0x141>(v));
+    v = larger(v, dpp_move<0x140>(v));
+    if constexpr (N == 64) {
+        v = larger(v, __shfl_xor(v, 16, 64));
+        v = larger(v, __shfl_xor(v, 32, 64));
+    }
+    return v;
+}
+
+// The sum of s and the largest m >= 0 over a row's group, as group_sum, behind one barrier.
+template <int N, typename R> __device__ __forceinline__ void group_sum_max(R& s, R& m, R* lds_s, R* lds_m) {
+    s = lanes_sum<N <= 64 ? N : 64>(s);
+    m = lanes_max<N <= 64 ? N : 64>(m);
+    if constexpr (N > 64) {
+        if ((threadIdx.x & 63) == 0) lds_s[threadIdx.x >> 6] = s, lds_m[threadIdx.x >> 6] = m;
+        __syncthreads();
+        s = 0, m = 0;
+#pragma unroll
+        for (int i = 0; i < N / 64; i++) s += lds_s[i], m = larger(m, lds_m[i]);
     }
 }
 

@@ -3,40 +3,12 @@
 // no state and allocate nothing.
 #include <hip/hip_runtime.h>
 
-#include <cmath>
-#include <cstdint>
-
-#include "errors.hpp"
-#include "norm.hpp"
+#include "checks.hpp"
 #include "ortho.hpp"
-#include "qlayer.h"
 
 using namespace qlayer;
 
 namespace {
-
-int fail(int code, const char* what, const char* detail = nullptr) { return set_error(code, what, detail); }
-
-bool known_type(int t) { return t >= QL_F32 && t <= QL_F16; }
-
-// A device array's address is a multiple of its element's size (NULL is).
-bool aligned(const void* p, int type) { return (uintptr_t)p % elem_size(type) == 0; }
-
-const int64_t MOST_ELEMENTS = (int64_t)1 << 46;
-
-int check_norm(int type, int wtype, int64_t rows, int64_t features) {
-    if (!known_type(type) || !known_type(wtype)) return fail(QL_EINVAL, "unknown type");
-    if (wtype != type && !(wtype == QL_F32 && (type == QL_BF16 || type == QL_F16)))
-        return fail(QL_EUNSUPPORTED, "weight_type is neither the rows' type nor QL_F32 beside 16-bit rows");
-    if (rows < 0) return fail(QL_EINVAL, "rows must be >= 0");
-    if (features < 1 || features > 1 << 30) return fail(QL_EINVAL, "features out of range [1, 2^30]");
-    if (rows > MOST_ELEMENTS / features) return fail(QL_EINVAL, "rows * features too large");
-    return QL_OK;
-}
-
-bool stride_ok(int64_t rows, int64_t stride) {
-    return stride >= 0 && (rows <= 1 || stride <= MOST_ELEMENTS / rows);
-}
 
 // The array's addresses: strides that are no overflow, and for one that is
 // written, no two elements at one address by a stride of 0.

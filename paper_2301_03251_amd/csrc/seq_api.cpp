@@ -1,0 +1,70 @@
+// seq_api.cpp -- C entries of the operators of a network that reads sequences
+// (qlayer.h): argument checks, workspace layout, launches on the caller's
+// stream. They hold no state and allocate nothing.
+#include <hip/hip_runtime.h>
+
+#include "checks.hpp"
+#include "rms.hpp"
+
+using namespace qlayer;
+
+namespace {
+
+int launched(hipError_t e, const char* what) {
+    if (e != hipSuccess) return fail(QL_EHIP, what, hipGetErrorString(e));
+    return set_error(QL_OK, "");
+}
+
+}  // namespace
+
+extern "C" {
+
+int ql_rms_norm_forward(ql_type type, ql_type weight_type, int64_t rows, int64_t features, const void* x,
+                        int64_t x_stride, const void* residual, int64_t residual_stride, const void* weight, double eps,
+                        void* summed, void* y, void* rstd, float* scale, void* ws, size_t ws_bytes, hipStream_t stream) {
+    if (int rc = check_norm(type, weight_type, rows, features)) return rc;
+    if (scale && type == QL_F64) return fail(QL_EUNSUPPORTED, "no output in 8 bits for QL_F64 rows");
+    if (!(eps >= 0) || std::isinf(eps)) return fail(QL_EINVAL, "eps must be finite and >= 0");
+    if (!stride_ok(rows, x_stride) || (residual && !stride_ok(rows, residual_stride)))
+        return fail(QL_EINVAL, "stride out of range");
+    if (rows > 0 && (!x || !y || (residual && !summed))) return fail(QL_EINVAL, "x, y or summed is NULL");
+    if (!aligned(x, type) || !aligned(residual, type) || !aligned(summed, type) || (!scale && !aligned(y, type)) ||
+        !aligned(weight, weight_type) || !aligned(rstd, wide_type(type)) || !aligned(scale, QL_F32))
+        return fail(QL_EINVAL, "misaligned pointer");
+    if (int rc = check_workspace(ws, ws_bytes, rms_workspace(type, rows, features, false))) return rc;
+    RmsArgs a{};
+    a.x = x, a.residual = residual, a.weight = weight, a.summed = summed, a.y = y, a.rstd = rstd, a.scale = scale;
+    a.rows = rows, a.D = features, a.x_stride = x_stride, a.residual_stride = residual_stride, a.eps = eps;
+    return launched(launch_rms_forward(type, weight_type, a, ws, stream), "rms norm");
+}
+
+int ql_rms_norm_workspace_bytes(ql_type type, int64_t rows, int64_t features, int backward, size_t* out) {
+    if (!out) return fail(QL_EINVAL, "NULL argument");
+    if (int rc = check_norm(type, type, rows, features)) return rc;
+    *out = rms_workspace(type, rows, features, backward != 0);
+    return set_error(QL_OK, "");
+}
+
+int ql_rms_norm_backward(ql_type type, ql_type weight_type, int64_t rows, int64_t features, const void* grad_y,
+                         int64_t grad_stride, const void* grad_summed, int64_t grad_summed_stride, const void* s,
+                         int64_t s_stride, const void* rstd, const void* weight, void* grad_x, void* grad_weight,
+                         void* ws, size_t ws_bytes, hipStream_t stream) {
+    if (int rc = check_norm(type, weight_type, rows, features)) return rc;
+    if (!stride_ok(rows, s_stride) || !stride_ok(rows, grad_stride) ||
+        (grad_summed && !stride_ok(rows, grad_summed_stride)))
+        return fail(QL_EINVAL, "stride out of range");
+    if (rows > 0 && (!grad_y || !s || !rstd)) return fail(QL_EINVAL, "grad_y, s or rstd is NULL");
+    if (!aligned(grad_y, type) || !aligned(grad_summed, type) || !aligned(s, type) || !aligned(grad_x, type) ||
+        !aligned(weight, weight_type) || !aligned(grad_weight, weight_type) || !aligned(rstd, wide_type(type)))
+        return fail(QL_EINVAL, "misaligned pointer");
+    if (grad_x || grad_weight)
+        if (int rc = check_workspace(ws, ws_bytes, rms_workspace(type, rows, features, true))) return rc;
+    RmsArgs a{};
+    a.grad = grad_y, a.grad_sum = grad_summed, a.x = s, a.rstd = (void*)rstd, a.weight = weight;
+    a.grad_x = grad_x, a.grad_weight = grad_weight;
+    a.rows = rows, a.D = features, a.x_stride = s_stride, a.grad_stride = grad_stride;
+    a.grad_sum_stride = grad_summed_stride;
+    return launched(launch_rms_backward(type, weight_type, a, ws, stream), "rms norm backward");
+}
+
+}  // extern "C"

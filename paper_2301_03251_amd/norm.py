@@ -54,7 +54,7 @@ def _rows(t, shape):
     """(tensor, rows, stride between rows) of t's rows along its last axis; a
     copy where they do not lie a fixed stride apart."""
     n = shape[-1]
-    if n == 1:  # with more features a view of negatives has no unit stride and is copied
+    if t.is_neg():
         t = t.resolve_neg()
     if len(shape) == 2:
         stride, unit = t.stride()
