@@ -493,6 +493,19 @@ int ql_rms_norm_backward(ql_type type, ql_type weight_type, int64_t rows, int64_
                          const void* rstd, const void* weight, void* grad_x, void* grad_weight,
                          void* workspace, size_t workspace_bytes, hipStream_t stream);
 
+/* Dropout: y_i = x_i / (1 - p) where word(i) >= p * 2^32 (rounded), 0 elsewhere
+ * whatever x_i is. i is the element's place in row-major order, word(i) word i mod
+ * 4 of Philox 4x32 with 10 rounds of the counter (i / 4, offset), low words first, under
+ * the key seed: the mask depends on nothing else, and the gradient is the same call
+ * on grad_y. p in [0, 1]; 1 gives zeros. key NULL, or the device address of seed and
+ * offset, which are then read when the kernel runs (a graph's replays draw new masks
+ * if the caller changes them) in place of the arguments. x's rows start x_stride
+ * elements apart, y[rows][features] is contiguous. features in [1, 2^30]; rows = 0
+ * does nothing. */
+int ql_dropout(ql_type type, int64_t rows, int64_t features, const void* x, int64_t x_stride,
+               double p, uint64_t seed, uint64_t offset, const uint64_t* key, void* y,
+               hipStream_t stream);
+
 /* Message of the last failing call on this thread ("" if none). */
 const char* ql_last_error(void);
 

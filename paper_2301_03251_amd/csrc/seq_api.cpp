@@ -4,6 +4,7 @@
 #include <hip/hip_runtime.h>
 
 #include "checks.hpp"
+#include "dropout.hpp"
 #include "rms.hpp"
 
 using namespace qlayer;
@@ -65,6 +66,21 @@ int ql_rms_norm_backward(ql_type type, ql_type weight_type, int64_t rows, int64_
     a.rows = rows, a.D = features, a.x_stride = s_stride, a.grad_stride = grad_stride;
     a.grad_sum_stride = grad_summed_stride;
     return launched(launch_rms_backward(type, weight_type, a, ws, stream), "rms norm backward");
+}
+
+int ql_dropout(ql_type type, int64_t rows, int64_t features, const void* x, int64_t x_stride, double p, uint64_t seed,
+               uint64_t offset, const uint64_t* key, void* y, hipStream_t stream) {
+    if (int rc = check_norm(type, type, rows, features)) return rc;
+    if (!(p >= 0 && p <= 1)) return fail(QL_EINVAL, "p out of range [0, 1]");
+    if (!stride_ok(rows, x_stride)) return fail(QL_EINVAL, "x_stride out of range");
+    if (rows > 0 && (!x || !y)) return fail(QL_EINVAL, "x or y is NULL");
+    if (!aligned(x, type) || !aligned(y, type) || !aligned(key, QL_F64)) return fail(QL_EINVAL, "misaligned pointer");
+    const double t = std::nearbyint(std::ldexp(p, 32));
+    DropoutArgs a{};
+    a.x = x, a.y = y, a.key = key, a.seed = seed, a.offset = offset;
+    a.rows = rows, a.D = features, a.x_stride = x_stride;
+    a.none = t >= 4294967296.0, a.threshold = a.none ? 0 : (uint32_t)t, a.scale = a.none ? 0 : 1 / (1 - p);
+    return launched(launch_dropout(type, a, stream), "dropout");
 }
 
 }  // extern "C"

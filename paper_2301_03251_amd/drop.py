@@ -1,0 +1,118 @@
+"""Dropout on the library's HIP kernel (``ql_dropout``): the mask comes from a
+counter-based generator and is drawn again where the gradient needs it, so none
+is stored, and a captured graph draws a new one at every replay.
+"""
+
+from __future__ import annotations
+
+import functools
+
+from .norm import _check_rows, _rows, has_tangent, on_device
+from .qlayer import _check, _stream, _torch, load
+
+
+def _numbers(key):
+    """(seed, offset, device address) of a key."""
+    torch = _torch()
+    if isinstance(key, torch.Tensor):
+        return 0, 0, key.data_ptr()
+    seed, offset = (int(k) for k in key)
+    if not (0 <= seed < 1 << 64 and 0 <= offset < 1 << 64):
+        raise ValueError("seed and offset must be in [0, 2^64)")
+    return seed, offset, None
+
+
+def dropout_forward(x, p, key):
+    """y = x / (1 - p) for elements that a generator keeps with probability 1 - p,
+    0 for the others (NaN and infinities among them). The mask depends on the
+    key and each element's place in x's row-major order alone, so the same
+    call takes a gradient back. Autograd does not see the call.
+
+    ``key`` is (seed, offset), each in [0, 2^64), or an int64 CUDA tensor of the
+    two, which is read when the kernel runs. Element i is kept where word i mod 4
+    of Philox 4x32-10 of the counter (i // 4, offset) under the key seed is at
+    least p * 2^32."""
+    torch = _torch()
+    device, shape, xt = _check_rows(x)
+    if isinstance(key, torch.Tensor) and (key.dtype != torch.int64 or key.shape != (2,) or key.get_device() != device
+                                          or not key.is_contiguous()):
+        raise ValueError("key must be (seed, offset) or a contiguous int64 tensor of the two on x's device")
+    seed, offset, address = _numbers(key)
+    there = on_device(device)
+    if there is not None:
+        with there:
+            return dropout_forward(x, p, key)
+    xr, rows, stride = _rows(x, shape)
+    y = x.new_empty(shape)
+    _check(load().ql_dropout(xt, rows, shape[-1], xr.data_ptr(), stride, p, seed, offset, address, y.data_ptr(),
+                             _stream(x.device)))
+    return y
+
+
+@functools.lru_cache(maxsize=None)
+def _function():
+    torch = _torch()
+
+    class DropoutFn(torch.autograd.Function):
+        @staticmethod
+        def forward(ctx, x, p, key):
+            ctx.p = p
+            if isinstance(key, torch.Tensor):
+                ctx.key = None
+                ctx.save_for_backward(key)
+            else:
+                ctx.key = key
+            return dropout_forward(x, p, key)
+
+        @staticmethod
+        @torch.autograd.function.once_differentiable
+        def backward(ctx, grad_y):
+            return dropout_forward(grad_y, ctx.p, ctx.saved_tensors[0] if ctx.key is None else ctx.key), None, None
+
+    return DropoutFn
+
+
+def dropout(x, p, key):
+    """``dropout_forward`` of x (CUDA tensor [..., features] of float32, float64,
+    bfloat16 or float16), differentiable once, in reverse mode (forward mode
+    raises). A key tensor must not change before the backward pass."""
+    if (_torch().is_grad_enabled() and x.requires_grad) or has_tangent(x):
+        return _function().apply(x, p, key)
+    return dropout_forward(x, p, key)
+
+
+@functools.lru_cache(maxsize=None)
+def _module_class():
+    torch = _torch()
+
+    class DropoutModule(torch.nn.Module):
+        def __init__(self, p, seed, device):
+            super().__init__()
+            self.p = float(p)
+            if not 0 <= self.p <= 1:
+                raise ValueError("p must be in [0, 1]")
+            if seed is None:
+                seed = int(torch.randint((1 << 63) - 1, ()))
+            # the seed, and the number of calls so far
+            self.register_buffer("key", torch.tensor([int(seed), 0], dtype=torch.int64, device=device))
+
+        def forward(self, x):
+            if not self.training or self.p == 0:
+                return x
+            key = self.key.clone()
+            self.key[1].add_(1)
+            return dropout(x, self.p, key)
+
+        def extra_repr(self):
+            return f"p={self.p}"
+
+    return DropoutModule
+
+
+def Dropout(p=0.1, seed=None, device="cuda"):
+    """``dropout`` as a ``torch.nn.Module``; the identity in evaluation. Its buffer
+    ``key`` holds the seed (in [0, 2^63); None draws one from torch's generator)
+    and the number of calls so far, which is the offset: every call has a mask of
+    its own, in replays of a captured graph too, and a loaded state goes on where
+    the saved one was. Processes that train together give each its own seed."""
+    return _module_class()(p, seed, device)

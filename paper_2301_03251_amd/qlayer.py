@@ -103,6 +103,7 @@ def load():
     lib.ql_rms_norm_forward.argtypes = [T, T, I64, I64, P, I64, P, I64, P, D, P, P, P, P, P, SZ, P]
     lib.ql_rms_norm_workspace_bytes.argtypes = [T, I64, I64, T, ctypes.POINTER(SZ)]
     lib.ql_rms_norm_backward.argtypes = [T, T, I64, I64, P, I64, P, I64, P, I64, P, P, P, P, P, SZ, P]
+    lib.ql_dropout.argtypes = [T, I64, I64, P, I64, D, ctypes.c_uint64, ctypes.c_uint64, P, P, P]
     lib.ql_last_error.argtypes = []
     lib.ql_last_error.restype = ctypes.c_char_p
     lib.ql_plan_info_get.argtypes = [P, ctypes.c_int, ctypes.POINTER(_PlanInfo)]
