@@ -493,6 +493,29 @@ int ql_rms_norm_backward(ql_type type, ql_type weight_type, int64_t rows, int64_
                          const void* rstd, const void* weight, void* grad_x, void* grad_weight,
                          void* workspace, size_t workspace_bytes, hipStream_t stream);
 
+/* Embedding: y_i = scale * W[t_i] for `count` tokens, W of rows x features whose rows
+ * start weight_stride elements apart, y[count][features] contiguous. Tokens are int64
+ * (tokens_64 not 0) or int32. With has_padding, tokens equal to `padding` (in the
+ * table or not) give zeros. Other tokens outside [0, rows) give NaN.
+ *
+ * The backward call: grad_weight[v] = scale * (sum over i with t_i = v of grad_y_i),
+ * [rows][features] contiguous, in the order of i: the same bits every time. Tokens that
+ * are the padding or outside the table have no gradient, rows without tokens get zeros.
+ *
+ * count in [0, 2^31), rows in [1, 2^31), features in [1, 2^22], scale finite.
+ * ql_embedding_workspace_bytes gives the backward call's device workspace. */
+int ql_embedding_forward(ql_type type, int tokens_64, int64_t count, int64_t rows, int64_t features,
+                         const void* tokens, const void* weight, int64_t weight_stride,
+                         double scale, int has_padding, int64_t padding, void* y,
+                         hipStream_t stream);
+int ql_embedding_workspace_bytes(ql_type type, int64_t count, int64_t rows, int64_t features,
+                                 size_t* out);
+int ql_embedding_backward(ql_type type, int tokens_64, int64_t count, int64_t rows,
+                          int64_t features, const void* tokens, const void* grad_y,
+                          int64_t grad_stride, double scale, int has_padding, int64_t padding,
+                          void* grad_weight, void* workspace, size_t workspace_bytes,
+                          hipStream_t stream);
+
 /* Dropout: y_i = x_i / (1 - p) where word(i) >= p * 2^32 (rounded), 0 elsewhere
  * whatever x_i is. i is the element's place in row-major order, word(i) word i mod
  * 4 of Philox 4x32 with 10 rounds of the counter (i / 4, offset), low words first, under

@@ -1,0 +1,499 @@
+// embed.hip -- rows of a table for tokens, times a scale, and the table's gradient.
+//
+//   y_i = scale W[t_i],   dW[v] = scale sum over i with t_i = v of g_i
+//
+// Tokens that are the padding have a row of zeros and no gradient. One outside the
+// table has a row of NaN, as nothing on the host sees it, and no gradient.
+//
+// The gradient's sums run in the order of the tokens' places, whatever the
+// grid: places are sorted by token (a stable radix sort), and a wavefront sums the
+// rows of a chunk of sorted places, token by token. A token whose rows lie in one
+// chunk is done there; of one that goes on in the next chunk the parts are joined
+// in a second launch. Rows without tokens are zeros, written beside the sort. HBM
+// bounds large calls (N rows of g read, the table written), launches the others.
+#include <algorithm>
+
+#include "elem.hpp"
+#include "embed.hpp"
+
+namespace qlayer {
+namespace {
+
+template <typename T> constexpr int VEC = 16 / (int)sizeof(T);
+
+__device__ __forceinline__ int64_t token_at(const EmbedArgs& a, int64_t i) {
+    return a.wide ? ((const int64_t*)a.tokens)[i] : (int64_t)((const int32_t*)a.tokens)[i];
+}
+
+// A group of G lanes copies token after token's row.
+template <typename T, int V, int G> __global__ __launch_bounds__(256) void k_embed_fwd(EmbedArgs a) {
+    using R = Acc<T>;
+    constexpr int ROWS = 256 / G;
+    const int lane = threadIdx.x % G, D = (int)a.D;
+    const R scale = (R)a.scale;
+    for (int64_t i = (int64_t)blockIdx.x * ROWS + threadIdx.x / G; i < a.n; i += (int64_t)gridDim.x * ROWS) {
+        const int64_t t = token_at(a, i);
+        const bool pad = a.padded && t == a.padding, in = t >= 0 && t < a.rows;
+        const T* src = (const T*)a.weight + (in ? t : 0) * a.weight_stride;
+        T* dst = (T*)a.y + i * a.D;
+#pragma unroll 2
+        for (int c = lane * V; c < D; c += G * V) {
+            const int at = min(c, D - V);
+            Vec<T, V> v;
+            if (in && !pad) v = load_vec<T, V>(src + at);
+#pragma unroll
+            for (int e = 0; e < V; e++)
+                v.v[e] = down<T>(pad ? (R)0 : in ? up(v.v[e]) * scale : (R)__builtin_nanf(""));
+            store_vec<T, V>(dst + at, v);
+        }
+    }
+}
+
+// ---------------------------------------------------------------------------
+// The sort: keys (the token; `rows` for what has no gradient) with their places.
+
+__device__ __forceinline__ uint32_t key_at(const EmbedArgs& a, int64_t i) {
+    const int64_t t = token_at(a, i);
+    return t < 0 || t >= a.rows || (a.padded && t == a.padding) ? (uint32_t)a.rows : (uint32_t)t;
+}
+
+// Zeros for the whole table: the share of workgroup `part` of `parts`.
+template <typename T> __device__ void clear_table(const EmbedArgs& a, int64_t part, int64_t parts) {
+    constexpr int V = VEC<T>;
+    const int64_t n = a.rows * a.D, vectors = n / V;
+    T* out = (T*)a.grad_weight;
+    Vec<T, V> zero;
+#pragma unroll
+    for (int e = 0; e < V; e++) zero.v[e] = down<T>((Acc<T>)0);
+    for (int64_t i = part * blockDim.x + threadIdx.x; i < vectors; i += parts * blockDim.x) store_vec<T, V>(out + i * V, zero);
+    if (part == 0 && threadIdx.x < n % V) out[vectors * V + threadIdx.x] = zero.v[0];
+}
+
+// The lanes of the wavefront with the same digit, of those that take part.
+__device__ __forceinline__ uint64_t lanes_alike(uint32_t digit, int bits, bool takes_part) {
+    uint64_t m = __ballot(takes_part);
+    for (int b = 0; b < bits; b++) {
+        const uint64_t has = __ballot((digit >> b) & 1);
+        m &= (digit >> b) & 1 ? has : ~has;
+    }
+    return m;
+}
+
+// Where an element comes among its wavefront's with its digit, which `counts` counts on.
+__device__ __forceinline__ uint32_t rank_of(uint32_t digit, int bits, bool takes_part, uint32_t* counts) {
+    const int lane = threadIdx.x & 63;
+    const uint64_t alike = lanes_alike(digit, bits, takes_part);
+    const int first = takes_part ? __ffsll((unsigned long long)alike) - 1 : lane;
+    uint32_t before = 0;
+    if (takes_part && lane == first) before = atomicAdd(&counts[digit], (uint32_t)__popcll(alike));
+    before = __shfl(before, first, 64);
+    return before + (uint32_t)__popcll(alike & ((1ull << lane) - 1));
+}
+
+// Sum of the values before the thread's own over a workgroup of T threads.
+template <int T> __device__ __forceinline__ uint32_t sum_before(uint32_t v, uint32_t* lds) {
+    const int lane = threadIdx.x & 63;
+    uint32_t s = v;
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) {
+        const uint32_t t = __shfl_up(s, d, 64);
+        if (lane >= d) s += t;
+    }
+    if (lane == 63) lds[threadIdx.x >> 6] = s;
+    __syncthreads();
+    uint32_t base = 0;
+#pragma unroll
+    for (int w = 0; w < T / 64; w++) base += w < (int)(threadIdx.x >> 6) ? lds[w] : 0;
+    __syncthreads();
+    return base + s - v;
+}
+
+// Up to 4096 places: sorted in the LDS of workgroup 0, in digits of 8 bits,
+// while the others clear the table.
+constexpr int SMALL = 4096;
+
+template <typename T> __global__ __launch_bounds__(1024) void k_embed_sort_small(EmbedArgs a, int bits, uint32_t* keys, uint32_t* places) {
+    if (blockIdx.x > 0) {
+        clear_table<T>(a, blockIdx.x - 1, gridDim.x - 1);
+        return;
+    }
+    constexpr int ITEMS = SMALL / 1024;
+    __shared__ uint32_t key[SMALL];
+    __shared__ uint16_t place[SMALL];
+    __shared__ uint32_t counts[16][256];
+    __shared__ uint32_t sums[16];
+    const int n = (int)a.n, wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+    const int items = (n + 1023) / 1024;
+    for (int i = threadIdx.x; i < n; i += 1024) key[i] = key_at(a, i), place[i] = (uint16_t)i;
+    for (int shift = 0; shift < bits; shift += 8) {
+        const int width = min(8, bits - shift);
+        for (int i = threadIdx.x; i < 16 * 256; i += 1024) counts[i / 256][i % 256] = 0;
+        __syncthreads();
+        uint32_t k[ITEMS], rank[ITEMS];
+        uint16_t from[ITEMS];
+#pragma unroll
+        for (int j = 0; j < ITEMS; j++) {
+            const int i = (wave * items + j) * 64 + lane;
+            if (j >= items) break;
+            k[j] = i < n ? key[i] : 0, from[j] = i < n ? place[i] : 0;
+            rank[j] = rank_of((k[j] >> shift) & ((1u << width) - 1), width, i < n, counts[wave]);
+        }
+        __syncthreads();
+        // thread d: digit d's elements before each wavefront's, then before the digit
+        uint32_t total = 0;
+        if (threadIdx.x < 256)
+            for (int w = 0; w < 16; w++) {
+                const uint32_t c = counts[w][threadIdx.x];
+                counts[w][threadIdx.x] = total;
+                total += c;
+            }
+        const uint32_t base = sum_before<1024>(total, sums);
+        if (threadIdx.x < 256)
+            for (int w = 0; w < 16; w++) counts[w][threadIdx.x] += base;
+        __syncthreads();
+#pragma unroll
+        for (int j = 0; j < ITEMS; j++) {
+            const int i = (wave * items + j) * 64 + lane;
+            if (j >= items) break;
+            if (i < n) {
+                const uint32_t to = counts[wave][(k[j] >> shift) & ((1u << width) - 1)] + rank[j];
+                key[to] = k[j], place[to] = from[j];
+            }
+        }
+        __syncthreads();
+    }
+    for (int i = threadIdx.x; i < n; i += 1024) keys[i] = key[i], places[i] = place[i];
+}
+
+// More: digits of up to 10 bits, each in three launches over tiles of 2048
+// places: the tiles' counts of the digit's values, their sums over the tiles before,
+// and the move. Pass 0 reads the tokens.
+constexpr int TILE = 2048, MOST_VALUES = 1024;
+
+struct SortPass {
+    const uint32_t *keys, *places;  // null: the tokens
+    uint32_t *to_keys, *to_places;
+    uint32_t* counts;  // [tiles][values], then the sums over the tiles before
+    uint32_t* totals;  // [values]
+    int shift, width;
+    int64_t tiles;
+};
+
+template <typename T> __global__ __launch_bounds__(256) void k_embed_count(EmbedArgs a, SortPass p, int64_t clearing) {
+    if (blockIdx.x >= p.tiles) {
+        clear_table<T>(a, blockIdx.x - p.tiles, clearing);
+        return;
+    }
+    __shared__ uint32_t counts[MOST_VALUES];
+    const int values = 1 << p.width;
+    for (int v = threadIdx.x; v < values; v += 256) counts[v] = 0;
+    __syncthreads();
+    const int64_t first = (int64_t)blockIdx.x * TILE;
+#pragma unroll
+    for (int j = 0; j < TILE / 256; j++) {
+        const int64_t i = first + j * 256 + threadIdx.x;
+        if (i < a.n) atomicAdd(&counts[((p.keys ? p.keys[i] : key_at(a, i)) >> p.shift) & (values - 1)], 1u);
+    }
+    __syncthreads();
+    for (int v = threadIdx.x; v < values; v += 256) p.counts[(int64_t)blockIdx.x * values + v] = counts[v];
+}
+
+// 16 values a workgroup, 64 threads for each value's tiles.
+__global__ __launch_bounds__(1024) void k_embed_sum_tiles(SortPass p) {
+    __shared__ uint32_t parts[64][17];
+    const int values = 1 << p.width, v = blockIdx.x * 16 + threadIdx.x % 16, g = threadIdx.x / 16;
+    const int64_t each = (p.tiles + 63) / 64, t0 = min(g * each, p.tiles), t1 = min(t0 + each, p.tiles);
+    uint32_t sum = 0;
+    if (v < values)
+#pragma unroll 8
+        for (int64_t t = t0; t < t1; t++) sum += p.counts[t * values + v];
+    parts[g][threadIdx.x % 16] = sum;
+    __syncthreads();
+    if (v >= values) return;
+    uint32_t before = 0;
+    for (int h = 0; h < g; h++) before += parts[h][threadIdx.x % 16];
+    if (g == 63) p.totals[v] = before + sum;
+#pragma unroll 8
+    for (int64_t t = t0; t < t1; t++) {
+        const uint32_t c = p.counts[t * values + v];
+        p.counts[t * values + v] = before;
+        before += c;
+    }
+}
+
+__global__ __launch_bounds__(256) void k_embed_move(EmbedArgs a, SortPass p) {
+    constexpr int ITEMS = TILE / 256, EACH = MOST_VALUES / 256;
+    __shared__ uint32_t counts[4][MOST_VALUES];
+    __shared__ uint32_t base[MOST_VALUES];
+    __shared__ uint32_t sums[4];
+    const int values = 1 << p.width, wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+    for (int i = threadIdx.x; i < 4 * MOST_VALUES; i += 256) counts[i / MOST_VALUES][i % MOST_VALUES] = 0;
+    // thread t: values EACH t ... EACH t + EACH - 1
+    uint32_t total[EACH], sum = 0;
+#pragma unroll
+    for (int e = 0; e < EACH; e++) {
+        const int v = threadIdx.x * EACH + e;
+        total[e] = v < values ? p.totals[v] : 0;
+        sum += total[e];
+    }
+    uint32_t before = sum_before<256>(sum, sums);
+#pragma unroll
+    for (int e = 0; e < EACH; e++) {
+        const int v = threadIdx.x * EACH + e;
+        if (v < values) base[v] = before + p.counts[(int64_t)blockIdx.x * values + v];
+        before += total[e];
+    }
+    __syncthreads();
+    const int64_t first = (int64_t)blockIdx.x * TILE + wave * (TILE / 4);
+    uint32_t key[ITEMS], place[ITEMS], rank[ITEMS];
+#pragma unroll
+    for (int j = 0; j < ITEMS; j++) {
+        const int64_t i = first + j * 64 + lane;
+        key[j] = i < a.n ? p.keys ? p.keys[i] : key_at(a, i) : 0;
+        place[j] = i < a.n && p.places ? p.places[i] : (uint32_t)i;
+    }
+#pragma unroll
+    for (int j = 0; j < ITEMS; j++)
+        rank[j] = rank_of((key[j] >> p.shift) & (values - 1), p.width, first + j * 64 + lane < a.n, counts[wave]);
+    __syncthreads();
+    for (int v = threadIdx.x; v < values; v += 256) {
+        uint32_t t = base[v];
+#pragma unroll
+        for (int w = 0; w < 4; w++) {
+            const uint32_t c = counts[w][v];
+            counts[w][v] = t;
+            t += c;
+        }
+    }
+    __syncthreads();
+#pragma unroll
+    for (int j = 0; j < ITEMS; j++)
+        if (first + j * 64 + lane < a.n) {
+            const uint32_t to = counts[wave][(key[j] >> p.shift) & (values - 1)] + rank[j];
+            p.to_keys[to] = key[j], p.to_places[to] = place[j];
+        }
+}
+
+// ---------------------------------------------------------------------------
+// The sums.
+
+// Places of a chunk, whose rows one group of lanes sums.
+constexpr int CHUNK = 64;
+
+struct Sums {
+    const uint32_t *keys, *places;
+    void* parts;  // [chunks][2][D]: of the token that goes on from the chunk before, and on to the next
+    int64_t chunks;
+};
+
+// A group of G lanes takes a chunk's rows in a tile of G V columns.
+template <typename T, int V, int G> __global__ __launch_bounds__(256) void k_embed_sums(EmbedArgs a, Sums q) {
+    using R = Acc<T>;
+    constexpr int GROUPS = 256 / G, AHEAD = 8;
+    const int lane = threadIdx.x % G, D = (int)a.D;
+    const int c = (blockIdx.y * G + lane) * V;
+    if (c >= D) return;
+    const int at = min(c, D - V);
+    const T* g = (const T*)a.grad + at;
+    const R scale = (R)a.scale;
+    const uint32_t none = (uint32_t)a.rows;
+    for (int64_t chunk = (int64_t)blockIdx.x * GROUPS + threadIdx.x / G; chunk < q.chunks; chunk += (int64_t)gridDim.x * GROUPS) {
+        const int64_t lo = chunk * CHUNK, hi = min(lo + CHUNK, a.n);
+        R sum[V] = {};
+        uint32_t current = q.keys[lo];
+        bool from_before = lo > 0 && q.keys[lo - 1] == current;
+        auto finish = [&](bool goes_on) {
+            if (current == none) return;
+            if (from_before || goes_on) {
+                Vec<R, V> r;
+#pragma unroll
+                for (int e = 0; e < V; e++) r.v[e] = sum[e];
+                store_vec<R, V>((R*)q.parts + (2 * chunk + (from_before ? 0 : 1)) * a.D + at, r);
+            } else {
+                Vec<T, V> r;
+#pragma unroll
+                for (int e = 0; e < V; e++) r.v[e] = down<T>(sum[e] * scale);
+                store_vec<T, V>((T*)a.grad_weight + (int64_t)current * a.D + at, r);
+            }
+        };
+        for (int64_t i = lo; i < hi; i += AHEAD) {
+            uint32_t key[AHEAD];
+            Vec<T, V> row[AHEAD];
+#pragma unroll
+            for (int j = 0; j < AHEAD; j++) key[j] = q.keys[min(i + j, hi - 1)];
+            if (key[0] == none) break;  // and so are all that follow
+#pragma unroll
+            for (int j = 0; j < AHEAD; j++)
+                row[j] = load_vec<T, V>(g + (int64_t)q.places[min(i + j, hi - 1)] * a.grad_stride);
+#pragma unroll
+            for (int j = 0; j < AHEAD; j++) {
+                if (i + j >= hi) break;
+                if (key[j] != current) {
+                    finish(false);
+                    current = key[j], from_before = false;
+#pragma unroll
+                    for (int e = 0; e < V; e++) sum[e] = 0;
+                }
+#pragma unroll
+                for (int e = 0; e < V; e++) sum[e] += up(row[j].v[e]);
+            }
+        }
+        finish(hi < a.n && q.keys[hi] == current);
+    }
+}
+
+// The parts of a token that begins in a chunk and goes on past it, in fp64: the
+// workgroup's wavefronts take every eighth and meet in LDS.
+template <typename T, int V> __global__ __launch_bounds__(512) void k_embed_join(EmbedArgs a, Sums q) {
+    using R = Acc<T>;
+    __shared__ double lds[8][64 * V];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, D = (int)a.D;
+    for (int64_t chunk = blockIdx.x; chunk < q.chunks - 1; chunk += gridDim.x) {
+        const int64_t lo = chunk * CHUNK, hi = lo + CHUNK;
+        const uint32_t key = q.keys[hi - 1];
+        if (key == (uint32_t)a.rows || q.keys[hi] != key || (lo > 0 && q.keys[lo] == key && q.keys[lo - 1] == key)) continue;
+        // the last chunk that begins with the token
+        int64_t last = chunk + 1;
+        for (;;) {
+            const int64_t j = last + 1 + lane;
+            const uint64_t other = ~__ballot(j < q.chunks && q.keys[min(j, q.chunks - 1) * CHUNK] == key);
+            const int alike = other ? __ffsll((unsigned long long)other) - 1 : 64;
+            last += alike;
+            if (alike < 64) break;
+        }
+        const int c = (blockIdx.y * 64 + lane) * V, at = max(0, min(c, D - V));
+        double sum[V] = {};
+        const R* parts = (const R*)q.parts + at;
+#pragma unroll 4
+        for (int64_t j = chunk + wave; j <= last; j += 8) {
+            const Vec<R, V> r = load_vec<R, V>(parts + (2 * j + (j == chunk ? 1 : 0)) * a.D);
+#pragma unroll
+            for (int e = 0; e < V; e++) sum[e] += (double)r.v[e];
+        }
+#pragma unroll
+        for (int e = 0; e < V; e++) lds[wave][lane * V + e] = sum[e];
+        __syncthreads();
+        if (wave == 0 && c < D) {
+            Vec<T, V> out;
+#pragma unroll
+            for (int e = 0; e < V; e++) {
+                double t = 0;
+#pragma unroll
+                for (int w = 0; w < 8; w++) t += lds[w][lane * V + e];
+                out.v[e] = down<T>((R)(t * a.scale));
+            }
+            store_vec<T, V>((T*)a.grad_weight + (int64_t)key * a.D + at, out);
+        }
+        __syncthreads();
+    }
+}
+
+// ---------------------------------------------------------------------------
+
+int bits_of(int64_t rows) { return 64 - __builtin_clzll((unsigned long long)rows); }  // of keys 0 ... rows
+
+struct Layout {
+    size_t keys[2], places[2], counts, totals, parts, bytes;
+    int64_t tiles, chunks;
+    int bits, passes, width;
+};
+Layout layout_of(int type, int64_t n, int64_t rows, int64_t D) {
+    Layout l{};
+    auto take = [&](size_t bytes) {
+        const size_t at = l.bytes;
+        l.bytes += (bytes + 255) & ~(size_t)255;
+        return at;
+    };
+    l.bits = bits_of(rows);
+    l.chunks = (n + CHUNK - 1) / CHUNK;
+    const bool small = n <= SMALL;
+    for (int k = 0; k < (small ? 1 : 2); k++) l.keys[k] = take((size_t)n * 4), l.places[k] = take((size_t)n * 4);
+    if (!small) {
+        l.tiles = (n + TILE - 1) / TILE;
+        l.passes = (l.bits + 9) / 10;
+        l.width = (l.bits + l.passes - 1) / l.passes;
+        l.counts = take((size_t)l.tiles * 4 << l.width);
+        l.totals = take((size_t)4 << l.width);
+    }
+    l.parts = take((size_t)l.chunks * 2 * (size_t)D * (type == E_F64 ? 8 : 4));
+    return l;
+}
+
+// Workgroups of 512 threads: 2^22 of them stay below a launch's 2^32 threads.
+unsigned grid_x(int64_t groups, int64_t y) { return (unsigned)std::max<int64_t>(1, std::min<int64_t>(groups, ((int64_t)1 << 22) / y)); }
+
+template <typename T, int V, int G> void sums(const EmbedArgs& a, const Sums& q, hipStream_t s) {
+    const int64_t tiles = (a.D + G * V - 1) / (G * V), wide = (a.D + 64 * V - 1) / (64 * V);
+    k_embed_sums<T, V, G><<<dim3(grid_x((q.chunks * G + 255) / 256, tiles), (unsigned)tiles), 256, 0, s>>>(a, q);
+    if (q.chunks > 1) k_embed_join<T, V><<<dim3(grid_x(q.chunks - 1, wide), (unsigned)wide), 512, 0, s>>>(a, q);
+}
+
+template <typename T> hipError_t backward(int type, const EmbedArgs& a, void* ws, hipStream_t s) {
+    const Layout l = layout_of(type, a.n, a.rows, a.D);
+    char* base = (char*)ws;
+    uint32_t *keys[2], *places[2];
+    for (int k = 0; k < 2; k++) keys[k] = (uint32_t*)(base + l.keys[k]), places[k] = (uint32_t*)(base + l.places[k]);
+    // a workgroup clears 16 KB or more
+    const int64_t clearing = std::max<int64_t>(1, std::min<int64_t>(2048, a.rows * a.D * (int64_t)sizeof(T) >> 14));
+    int at = 0;
+    if (a.n <= SMALL) {
+        k_embed_sort_small<T><<<(unsigned)(1 + clearing), 1024, 0, s>>>(a, l.bits, keys[0], places[0]);
+        if (a.n == 0) return hipGetLastError();
+    } else {
+        for (int k = 0; k < l.passes; k++, at ^= 1) {
+            SortPass p{};
+            if (k > 0) p.keys = keys[at ^ 1], p.places = places[at ^ 1];
+            p.to_keys = keys[at], p.to_places = places[at];
+            p.counts = (uint32_t*)(base + l.counts), p.totals = (uint32_t*)(base + l.totals);
+            p.shift = k * l.width, p.width = std::min(l.width, l.bits - p.shift), p.tiles = l.tiles;
+            const int64_t more = k == 0 ? clearing : 0;
+            k_embed_count<T><<<(unsigned)(l.tiles + more), 256, 0, s>>>(a, p, more);
+            k_embed_sum_tiles<<<((1 << p.width) + 15) / 16, 1024, 0, s>>>(p);
+            k_embed_move<<<(unsigned)l.tiles, 256, 0, s>>>(a, p);
+        }
+        at ^= 1;
+    }
+    const Sums q{keys[at], places[at], base + l.parts, l.chunks};
+    if (a.D < VEC<T>) sums<T, 1, 16>(a, q, s);
+    else if (a.D <= 16 * VEC<T>) sums<T, VEC<T>, 16>(a, q, s);
+    else sums<T, VEC<T>, 64>(a, q, s);
+    return hipGetLastError();
+}
+
+template <typename T, int V, int G> hipError_t rows_of(const EmbedArgs& a, hipStream_t s) {
+    constexpr int ROWS = 256 / G;
+    k_embed_fwd<T, V, G><<<(unsigned)std::min<int64_t>((a.n + ROWS - 1) / ROWS, 1 << 20), 256, 0, s>>>(a);
+    return hipGetLastError();
+}
+
+template <typename T> hipError_t forward(const EmbedArgs& a, hipStream_t s) {
+    constexpr int V = VEC<T>;
+    if (a.D < V) return rows_of<T, 1, 16>(a, s);
+    if (a.D <= 16 * V) return rows_of<T, V, 16>(a, s);
+    if (a.D <= 128 * V) return rows_of<T, V, 64>(a, s);
+    return rows_of<T, V, 256>(a, s);
+}
+
+template <typename F> hipError_t by_type(int type, F f) {
+    switch (type) {
+        case E_F64: return f(double{});
+        case E_BF16: return f(bf16{});
+        case E_F16: return f(_Float16{});
+        default: return f(float{});
+    }
+}
+
+}  // namespace
+
+size_t embed_workspace(int type, int64_t n, int64_t rows, int64_t D) { return layout_of(type, n, rows, D).bytes; }
+
+hipError_t launch_embed_forward(int type, const EmbedArgs& a, hipStream_t s) {
+    if (a.n == 0) return hipSuccess;
+    return by_type(type, [&](auto t) { return forward<decltype(t)>(a, s); });
+}
+
+hipError_t launch_embed_backward(int type, const EmbedArgs& a, void* ws, hipStream_t s) {
+    return by_type(type, [&](auto t) { return backward<decltype(t)>(type, a, ws, s); });
+}
+
+}  // namespace qlayer

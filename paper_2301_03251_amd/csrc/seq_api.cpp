@@ -3,13 +3,25 @@
 // stream. They hold no state and allocate nothing.
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
+
 #include "checks.hpp"
 #include "dropout.hpp"
+#include "embed.hpp"
 #include "rms.hpp"
 
 using namespace qlayer;
 
 namespace {
+
+int check_embedding(int type, int64_t count, int64_t rows, int64_t features) {
+    if (!known_type(type)) return fail(QL_EINVAL, "unknown type");
+    if (count < 0 || count > INT32_MAX) return fail(QL_EINVAL, "count out of range [0, 2^31)");
+    if (rows < 1 || rows > INT32_MAX) return fail(QL_EINVAL, "rows out of range [1, 2^31)");
+    if (features < 1 || features > 1 << 22) return fail(QL_EINVAL, "features out of range [1, 2^22]");
+    if (std::max(rows, count) > MOST_ELEMENTS / features) return fail(QL_EINVAL, "too many elements");
+    return QL_OK;
+}
 
 int launched(hipError_t e, const char* what) {
     if (e != hipSuccess) return fail(QL_EHIP, what, hipGetErrorString(e));
@@ -66,6 +78,47 @@ int ql_rms_norm_backward(ql_type type, ql_type weight_type, int64_t rows, int64_
     a.rows = rows, a.D = features, a.x_stride = s_stride, a.grad_stride = grad_stride;
     a.grad_sum_stride = grad_summed_stride;
     return launched(launch_rms_backward(type, weight_type, a, ws, stream), "rms norm backward");
+}
+
+int ql_embedding_forward(ql_type type, int tokens_64, int64_t count, int64_t rows, int64_t features, const void* tokens,
+                         const void* weight, int64_t weight_stride, double scale, int has_padding, int64_t padding,
+                         void* y, hipStream_t stream) {
+    if (int rc = check_embedding(type, count, rows, features)) return rc;
+    if (!std::isfinite(scale)) return fail(QL_EINVAL, "scale must be finite");
+    if (!stride_ok(rows, weight_stride)) return fail(QL_EINVAL, "weight_stride out of range");
+    if (count > 0 && (!tokens || !weight || !y)) return fail(QL_EINVAL, "tokens, weight or y is NULL");
+    if (!aligned(tokens, tokens_64 ? QL_F64 : QL_F32) || !aligned(weight, type) || !aligned(y, type))
+        return fail(QL_EINVAL, "misaligned pointer");
+    EmbedArgs a{};
+    a.tokens = tokens, a.weight = weight, a.y = y, a.n = count, a.rows = rows, a.D = features;
+    a.weight_stride = weight_stride, a.padding = padding, a.padded = has_padding != 0, a.wide = tokens_64 != 0;
+    a.scale = scale;
+    return launched(launch_embed_forward(type, a, stream), "embedding");
+}
+
+int ql_embedding_workspace_bytes(ql_type type, int64_t count, int64_t rows, int64_t features, size_t* out) {
+    if (!out) return fail(QL_EINVAL, "NULL argument");
+    if (int rc = check_embedding(type, count, rows, features)) return rc;
+    *out = embed_workspace(type, count, rows, features);
+    return set_error(QL_OK, "");
+}
+
+int ql_embedding_backward(ql_type type, int tokens_64, int64_t count, int64_t rows, int64_t features,
+                          const void* tokens, const void* grad_y, int64_t grad_stride, double scale, int has_padding,
+                          int64_t padding, void* grad_weight, void* ws, size_t ws_bytes, hipStream_t stream) {
+    if (int rc = check_embedding(type, count, rows, features)) return rc;
+    if (!std::isfinite(scale)) return fail(QL_EINVAL, "scale must be finite");
+    if (!stride_ok(count, grad_stride)) return fail(QL_EINVAL, "grad_stride out of range");
+    if (!grad_weight || (count > 0 && (!tokens || !grad_y)))
+        return fail(QL_EINVAL, "tokens, grad_y or grad_weight is NULL");
+    if (!aligned(tokens, tokens_64 ? QL_F64 : QL_F32) || !aligned(grad_y, type) || !aligned(grad_weight, type))
+        return fail(QL_EINVAL, "misaligned pointer");
+    if (int rc = check_workspace(ws, ws_bytes, embed_workspace(type, count, rows, features))) return rc;
+    EmbedArgs a{};
+    a.tokens = tokens, a.grad = grad_y, a.grad_weight = grad_weight, a.n = count, a.rows = rows, a.D = features;
+    a.grad_stride = grad_stride, a.padding = padding, a.padded = has_padding != 0, a.wide = tokens_64 != 0;
+    a.scale = scale;
+    return launched(launch_embed_backward(type, a, ws, stream), "embedding backward");
 }
 
 int ql_dropout(ql_type type, int64_t rows, int64_t features, const void* x, int64_t x_stride, double p, uint64_t seed,
