@@ -529,6 +529,49 @@ int ql_dropout(ql_type type, int64_t rows, int64_t features, const void* x, int6
                double p, uint64_t seed, uint64_t offset, const uint64_t* key, void* y,
                hipStream_t stream);
 
+/* Gated linear recurrence over the steps of sequences:
+ *   a_t = 1 / (1 + exp(-gate_t)),  h_t = a_t h_{t-1} + (1 - a_t) x_t.
+ * x and gate are [batch][steps][features] arrays whose sequences and steps start
+ * x_batch and x_step (gate_batch, gate_step) elements apart (>= 0: the halves of one
+ * projection, say); h is contiguous. States are QL_F64 for QL_F64 and QL_F32
+ * otherwise: initial[batch][features] before the first step (NULL: 0), last[batch]
+ * [features] after the last one (may be NULL), and for the backward call states[batch]
+ * [ceil(steps / QL_SCAN_BLOCK)][features], the state before every QL_SCAN_BLOCK
+ * steps (may be NULL). starts[batch][steps] (may be NULL) is not 0 where a sequence
+ * begins: the state before that step is taken as 0, whatever it holds. A state that is not finite
+ * makes its sequence's later ones infinite or NaN, and no others.
+ *
+ * The backward call: with G_t = grad_h_t + a_{t+1} G_{t+1} (grad_last, which may be NULL, behind the last
+ * step; nothing comes back past a start),
+ *   grad_x = (1 - a) G,  grad_gate = G (h_{t-1} - x) a (1 - a),  grad_initial = a_0 G_0
+ * (may be NULL). grad_x and grad_gate are contiguous.
+ *
+ * The step call is one step of each sequence: x and gate [batch] rows x_batch and
+ * gate_batch elements apart, starts[batch], state[batch][features] in place,
+ * h[batch][features].
+ *
+ * features in [1, 2^22], steps in [0, 2^31), batch * features in [0, 2^27]; batch = 0 does
+ * nothing. ql_gated_scan_workspace_bytes gives the device workspace of a forward or
+ * backward call; where it is 0 the workspace may be NULL. */
+#define QL_SCAN_BLOCK 16
+int ql_gated_scan_forward(ql_type type, int64_t batch, int64_t steps, int64_t features,
+                          const void* x, int64_t x_batch, int64_t x_step, const void* gate,
+                          int64_t gate_batch, int64_t gate_step, const uint8_t* starts,
+                          const void* initial, void* h, void* last, void* states,
+                          void* workspace, size_t workspace_bytes, hipStream_t stream);
+int ql_gated_scan_workspace_bytes(ql_type type, int64_t batch, int64_t steps, int64_t features,
+                                  size_t* out);
+int ql_gated_scan_backward(ql_type type, int64_t batch, int64_t steps, int64_t features,
+                           const void* grad_h, int64_t grad_batch, int64_t grad_step,
+                           const void* x, int64_t x_batch, int64_t x_step, const void* gate,
+                           int64_t gate_batch, int64_t gate_step, const void* states,
+                           const uint8_t* starts, const void* grad_last, void* grad_x,
+                           void* grad_gate, void* grad_initial, void* workspace,
+                           size_t workspace_bytes, hipStream_t stream);
+int ql_gated_scan_step(ql_type type, int64_t batch, int64_t features, const void* x,
+                       int64_t x_batch, const void* gate, int64_t gate_batch,
+                       const uint8_t* starts, void* state, void* h, hipStream_t stream);
+
 /* Message of the last failing call on this thread ("" if none). */
 const char* ql_last_error(void);
 

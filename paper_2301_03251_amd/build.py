@@ -21,7 +21,8 @@ ROOT = os.path.dirname(PKG)
 CSRC = os.path.join(PKG, "csrc")
 BUILD = os.path.join(ROOT, "_build")
 LIB = os.path.join(PKG, "libqlayer.so")
-SOURCES = ["tile.hip", "kernels.hip", "runs.hip", "norm.hip", "ortho.hip", "rms.hip", "dropout.hip", "embed.hip", "api.cpp", "ops_api.cpp", "seq_api.cpp",
+SOURCES = ["tile.hip", "kernels.hip", "runs.hip", "norm.hip", "ortho.hip", "rms.hip", "dropout.hip", "embed.hip", "scan.hip",
+           "api.cpp", "ops_api.cpp", "seq_api.cpp",
            "plan.cpp", "runs.cpp", "ortho_plan.cpp"]
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")

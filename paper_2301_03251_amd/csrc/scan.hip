@@ -1,0 +1,385 @@
+// scan.hip -- gated linear recurrence over the steps of sequences, forward,
+// backward and one step.
+//
+//   a_t = 1 / (1 + exp(-z_t)),  h_t = a_t h_{t-1} + (1 - a_t) x_t
+//   G_t = g_t + a_{t+1} G_{t+1},  dx_t = (1 - a_t) G_t,
+//   dz_t = G_t (h_{t-1} - x_t) a_t (1 - a_t),  dh_{-1} = a_0 G_0
+//
+// Where a sequence starts, h_{t-1} is 0 and nothing of G_t goes back past it. It is
+// chosen, not multiplied by 0: what another sequence held (infinities, NaN) does not come in.
+//
+// A step is the map h -> a h + b, and a row of steps one such map again: (A, B) then
+// (a, b) is (a A, a B + b). So the steps go in blocks of 16, one a wavefront, with a
+// column (sequence and feature) a lane: a wavefront reads its block into registers and
+// makes its map, the workgroup's wavefronts exchange maps through LDS, and each runs
+// its block again from the state before it. Arrays are read once. Where there are
+// fewer columns than fill the chip, the steps are split into segments: a launch
+// makes the segments' maps, which reads what they need a second time, and the main
+// launch begins each segment with the maps before it.
+//
+// Backward the maps run from the end, of what comes back to a step, and the states
+// h_{t-1} are computed again from the one that the forward call kept before each
+// block (in fp32: 1/16 of an array's elements).
+//
+// HBM bounds long calls; about 25 operations an element forward and 45 backward
+// come next.
+#include <algorithm>
+
+#include "elem.hpp"
+#include "scan.hpp"
+
+namespace qlayer {
+namespace {
+
+constexpr int L = SCAN_BLOCK;
+
+// a = sigmoid(z) and 1 - a, neither as a difference from 1.
+__device__ __forceinline__ void gates(float z, float& a, float& rest) {
+    const float e = __builtin_amdgcn_exp2f(-1.44269504f * fabsf(z)), r = __builtin_amdgcn_rcpf(1 + e);
+    a = z >= 0 ? r : e * r, rest = z >= 0 ? e * r : r;
+}
+__device__ __forceinline__ void gates(double z, double& a, double& rest) {
+    const double e = exp(-fabs(z)), r = 1 / (1 + e);
+    a = z >= 0 ? r : e * r, rest = z >= 0 ? e * r : r;
+}
+
+// The map of a row of steps. A < 0 (a cut): the state is B whatever it was before.
+template <typename R> struct Map {
+    R A, B;
+    __device__ __forceinline__ R operator()(R h) const { return A < 0 ? B : A * h + B; }
+    // this one, then m
+    __device__ __forceinline__ void then(const Map& m) {
+        B = m(B);
+        A = m.A < 0 || A < 0 ? (R)-1 : A * m.A;
+    }
+};
+
+// A lane's column.
+struct Column {
+    bool live;
+    int64_t at, batch, d;  // among all columns; its sequence and feature
+    __device__ __forceinline__ Column(const ScanArgs& a) {
+        const int64_t c = (int64_t)blockIdx.x * 64 + (threadIdx.x & 63), n = a.batch * a.D;
+        live = c < n, at = min(c, n - 1), batch = at / a.D, d = at % a.D;
+    }
+    template <typename T> __device__ __forceinline__ const T* of(const Strided& s) const {
+        return (const T*)s.p + batch * s.batch + d;
+    }
+};
+
+// The steps of block k that start a sequence, as bits.
+template <bool STARTS> __device__ __forceinline__ uint32_t starts_of(const ScanArgs& a, const Column& c, int64_t k) {
+    uint32_t bits = 0;
+    if constexpr (STARTS) {
+        const uint8_t* s = a.starts + c.batch * a.steps;
+#pragma unroll
+        for (int j = 0; j < L; j++) {
+            const int64_t t = k * L + j;
+            bits |= (uint32_t)(s[min(t, a.steps - 1)] != 0 && t < a.steps) << j;
+        }
+    }
+    return bits;
+}
+
+// Block k's elements of a column; past the end the last step's, which the caller leaves out.
+template <typename T> __device__ __forceinline__ void load_block(T (&v)[L], const T* p, int64_t step, int64_t k, int64_t steps) {
+#pragma unroll
+    for (int j = 0; j < L; j++) v[j] = p[min(k * L + j, steps - 1) * step];
+}
+
+// The map of a forward block, and its factors.
+template <typename T, bool STARTS, typename R>
+__device__ __forceinline__ Map<R> forward_map(const T (&x)[L], const T (&z)[L], uint32_t starts, int64_t left, R (&f)[L], R (&b)[L]) {
+    Map<R> m{1, 0};
+    bool cut = false;
+#pragma unroll
+    for (int j = 0; j < L; j++) {
+        R rest;
+        gates(up(z[j]), f[j], rest);
+        b[j] = rest * up(x[j]);
+        if (j >= left) f[j] = 1, b[j] = 0;
+        if (STARTS && ((starts >> j) & 1)) m.B = b[j], cut = true;
+        else m.B = f[j] * m.B + b[j];
+        m.A *= f[j];
+    }
+    if (cut) m.A = -1;
+    return m;
+}
+
+// The map of a backward block, last step first, of what comes back to a step.
+template <bool STARTS, typename R>
+__device__ __forceinline__ Map<R> backward_map(const R (&f)[L], const R (&g)[L], uint32_t starts) {
+    Map<R> m{1, 0};
+    bool cut = false;
+#pragma unroll
+    for (int j = L - 1; j >= 0; j--) {
+        if (STARTS && ((starts >> j) & 1)) m.B = 0, cut = true;
+        else m.B = f[j] * (m.B + g[j]);
+        m.A *= f[j];
+    }
+    if (cut) m.A = -1;
+    return m;
+}
+
+// Where the segment begins: the maps of the segments that come before it, each
+// wavefront a share of them, on the state that the row begins with.
+template <int W, typename R>
+__device__ __forceinline__ R begin_segment(R state, const R* maps, int64_t columns, int64_t column, int first, int count, int dir, R (&A)[W][64], R (&B)[W][64]) {
+    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, each = (count + W - 1) / W;
+    Map<R> m{1, 0};
+#pragma unroll 4
+    for (int i = wave * each; i < min(count, (wave + 1) * each); i++) {
+        const R* p = maps + (int64_t)(first + dir * i) * 2 * columns + column;
+        m.then(Map<R>{p[0], p[columns]});
+    }
+    A[wave][lane] = m.A, B[wave][lane] = m.B;
+    __syncthreads();
+#pragma unroll
+    for (int w = 0; w < W; w++) state = Map<R>{A[w][lane], B[w][lane]}(state);
+    __syncthreads();
+    return state;
+}
+
+template <typename T, int W, bool STARTS> __global__ __launch_bounds__(64 * W) void k_scan_fwd(ScanArgs a, int64_t blocks, int64_t each) {
+    using R = Acc<T>;
+    __shared__ R A[2][W][64], B[2][W][64];
+    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+    const Column c(a);
+    const T *x = c.of<T>(a.x), *z = c.of<T>(a.gate);
+    const int64_t k0 = blockIdx.y * each, k1 = min(k0 + each, blocks);
+    R state = a.initial ? ((const R*)a.initial)[c.at] : 0;
+    if (blockIdx.y > 0) state = begin_segment<W, R>(state, (const R*)a.ws, a.batch * a.D, c.at, 0, blockIdx.y, 1, A[0], B[0]);
+    int turn = 0;
+    for (int64_t base = k0; base < k1; base += W, turn ^= 1) {
+        const int64_t k = base + wave, left = k < k1 ? a.steps - k * L : 0;
+        T vx[L], vz[L];
+        load_block(vx, x, a.x.step, k, a.steps);
+        load_block(vz, z, a.gate.step, k, a.steps);
+        const uint32_t starts = left > 0 ? starts_of<STARTS>(a, c, k) : 0;
+        R f[L], b[L];
+        const Map<R> m = forward_map<T, STARTS, R>(vx, vz, starts, left, f, b);
+        A[turn][wave][lane] = m.A, B[turn][wave][lane] = m.B;
+        __syncthreads();
+        R h = state;
+#pragma unroll
+        for (int w = 0; w < W; w++) {
+            if (w == wave) h = state;
+            state = Map<R>{A[turn][w][lane], B[turn][w][lane]}(state);
+        }
+        if (left <= 0 || !c.live) continue;
+        if (a.states) ((R*)a.states)[(c.batch * blocks + k) * a.D + c.d] = h;
+        T* out = (T*)a.h + (c.batch * a.steps + k * L) * a.D + c.d;
+#pragma unroll
+        for (int j = 0; j < L; j++) {
+            h = STARTS && ((starts >> j) & 1) ? b[j] : f[j] * h + b[j];
+            if (j < left) out[j * a.D] = down<T>(h);
+        }
+    }
+    if (a.last && k1 == blocks && wave == 0 && c.live) ((R*)a.last)[c.at] = state;
+}
+
+// ws[segment][2][columns]: the segments' maps, forward or backward.
+template <typename T, int W, bool STARTS, bool BACK>
+__global__ __launch_bounds__(64 * W) void k_scan_maps(ScanArgs a, int64_t blocks, int64_t each) {
+    using R = Acc<T>;
+    __shared__ R A[W][64], B[W][64];
+    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+    const Column c(a);
+    const T *v = c.of<T>(BACK ? a.grad : a.x), *z = c.of<T>(a.gate);
+    const int64_t k0 = blockIdx.y * each, k1 = min(k0 + each, blocks), share = (each + W - 1) / W;
+    // wavefront 0 has the blocks that come first in the maps' direction
+    const int64_t n = k1 - k0, i0 = min(wave * share, n), i1 = min(i0 + share, n);
+    Map<R> m{1, 0};
+    for (int64_t i = i0; i < i1; i++) {
+        const int64_t k = BACK ? k1 - 1 - i : k0 + i, left = a.steps - k * L;
+        T vv[L], vz[L];
+        load_block(vv, v, BACK ? a.grad.step : a.x.step, k, a.steps);
+        load_block(vz, z, a.gate.step, k, a.steps);
+        const uint32_t starts = starts_of<STARTS>(a, c, k);
+        R f[L], b[L];
+        if constexpr (BACK) {
+#pragma unroll
+            for (int j = 0; j < L; j++) {
+                R rest;
+                gates(up(vz[j]), f[j], rest);
+                b[j] = up(vv[j]);
+                if (j >= left) f[j] = 1, b[j] = 0;
+            }
+            m.then(backward_map<STARTS, R>(f, b, starts));
+        } else {
+            m.then(forward_map<T, STARTS, R>(vv, vz, starts, left, f, b));
+        }
+    }
+    A[wave][lane] = m.A, B[wave][lane] = m.B;
+    __syncthreads();
+    if (wave > 0 || !c.live) return;
+#pragma unroll
+    for (int w = 1; w < W; w++) m.then(Map<R>{A[w][lane], B[w][lane]});
+    R* out = (R*)a.ws + (int64_t)blockIdx.y * 2 * a.batch * a.D + c.at;
+    out[0] = m.A, out[a.batch * a.D] = m.B;
+}
+
+template <typename T, int W, bool STARTS> __global__ __launch_bounds__(64 * W) void k_scan_bwd(ScanArgs a, int64_t blocks, int64_t each) {
+    using R = Acc<T>;
+    __shared__ R A[2][W][64], B[2][W][64];
+    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+    const Column c(a);
+    const T *x = c.of<T>(a.x), *z = c.of<T>(a.gate), *g = c.of<T>(a.grad);
+    const int64_t k0 = blockIdx.y * each, k1 = min(k0 + each, blocks);
+    const int behind = gridDim.y - 1 - blockIdx.y;
+    R back = a.grad_last ? ((const R*)a.grad_last)[c.at] : 0;
+    if (behind > 0) back = begin_segment<W, R>(back, (const R*)a.ws, a.batch * a.D, c.at, gridDim.y - 1, behind, -1, A[0], B[0]);
+    int turn = 0;
+    for (int64_t top = k1; top > k0; top -= W, turn ^= 1) {
+        const int64_t k = max(top - 1 - wave, k0), left = top - 1 - wave >= k0 ? a.steps - k * L : 0;
+        T vx[L], vz[L], vg[L];
+        load_block(vx, x, a.x.step, k, a.steps);
+        load_block(vz, z, a.gate.step, k, a.steps);
+        load_block(vg, g, a.grad.step, k, a.steps);
+        R h = ((const R*)a.states)[(c.batch * blocks + k) * a.D + c.d];
+        const uint32_t starts = left > 0 ? starts_of<STARTS>(a, c, k) : 0;
+        // f = a, r = 1 - a, q = dz / G, b = g
+        R f[L], r[L], q[L], b[L];
+#pragma unroll
+        for (int j = 0; j < L; j++) {
+            gates(up(vz[j]), f[j], r[j]);
+            const R v = up(vx[j]), before = STARTS && ((starts >> j) & 1) ? 0 : h;
+            q[j] = (before - v) * (f[j] * r[j]);
+            h = f[j] * before + r[j] * v;
+            b[j] = up(vg[j]);
+            if (j >= left) f[j] = 1, b[j] = 0;
+        }
+        const Map<R> m = backward_map<STARTS, R>(f, b, starts);
+        A[turn][wave][lane] = m.A, B[turn][wave][lane] = m.B;
+        __syncthreads();
+        R s = back;
+#pragma unroll
+        for (int w = 0; w < W; w++) {
+            if (w == wave) s = back;
+            back = Map<R>{A[turn][w][lane], B[turn][w][lane]}(back);
+        }
+        if (left <= 0 || !c.live) continue;
+        const int64_t at = (c.batch * a.steps + k * L) * a.D + c.d;
+        T *dx = (T*)a.grad_x + at, *dz = (T*)a.grad_gate + at;
+#pragma unroll
+        for (int j = L - 1; j >= 0; j--) {
+            const R G = b[j] + s;
+            s = STARTS && ((starts >> j) & 1) ? 0 : f[j] * G;
+            if (j < left) {
+                dx[j * a.D] = down<T>(r[j] * G);
+                dz[j * a.D] = down<T>(q[j] * G);
+            }
+        }
+    }
+    if (a.grad_initial && k0 == 0 && wave == 0 && c.live) ((R*)a.grad_initial)[c.at] = back;
+}
+
+// One step: V elements a thread.
+template <typename T, int V> __global__ __launch_bounds__(256) void k_scan_step(ScanArgs a, void* state) {
+    using R = Acc<T>;
+    const int64_t per = a.D / V, n = a.batch * per;
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256) {
+        const int64_t b = i / per, d = (i % per) * V;
+        const Vec<T, V> x = load_vec<T, V>((const T*)a.x.p + b * a.x.batch + d);
+        const Vec<T, V> z = load_vec<T, V>((const T*)a.gate.p + b * a.gate.batch + d);
+        Vec<R, V> s = load_vec<R, V>((const R*)state + b * a.D + d);
+        const bool start = a.starts && a.starts[b];
+        Vec<T, V> h;
+#pragma unroll
+        for (int e = 0; e < V; e++) {
+            R f, rest;
+            gates(up(z.v[e]), f, rest);
+            const R in = rest * up(x.v[e]);
+            s.v[e] = start ? in : f * s.v[e] + in;
+            h.v[e] = down<T>(s.v[e]);
+        }
+        store_vec<R, V>((R*)state + b * a.D + d, s);
+        store_vec<T, V>((T*)a.h + b * a.D + d, h);
+    }
+}
+
+// How a call is split: wavefronts of a workgroup, blocks of a segment, segments.
+struct Split {
+    int waves;
+    int64_t groups, blocks, each, segments;
+};
+Split split_of(const int64_t batch, int64_t steps, int64_t D) {
+    Split p{};
+    p.groups = (batch * D + 63) / 64;
+    p.blocks = (steps + L - 1) / L;
+    p.waves = p.blocks <= 1 ? 1 : p.blocks <= 4 ? 4 : 16;
+    const int64_t turns = std::max<int64_t>(1, (p.blocks + p.waves - 1) / p.waves);
+    // segments of whole turns, as many as give every compute unit a workgroup
+    const int64_t want = std::min<int64_t>(turns, std::max<int64_t>(1, 256 / p.groups));
+    p.each = (turns + want - 1) / want * p.waves;
+    p.segments = std::max<int64_t>(1, (p.blocks + p.each - 1) / p.each);
+    return p;
+}
+
+template <typename T, int W, bool STARTS> hipError_t run(const ScanArgs& a, const Split& p, bool back, hipStream_t s) {
+    const dim3 grid((unsigned)p.groups, (unsigned)p.segments);
+    if (back) {
+        if (p.segments > 1) k_scan_maps<T, W, STARTS, true><<<grid, 64 * W, 0, s>>>(a, p.blocks, p.each);
+        k_scan_bwd<T, W, STARTS><<<grid, 64 * W, 0, s>>>(a, p.blocks, p.each);
+    } else {
+        if (p.segments > 1) k_scan_maps<T, W, STARTS, false><<<grid, 64 * W, 0, s>>>(a, p.blocks, p.each);
+        k_scan_fwd<T, W, STARTS><<<grid, 64 * W, 0, s>>>(a, p.blocks, p.each);
+    }
+    return hipGetLastError();
+}
+
+template <typename T, bool STARTS> hipError_t run(const ScanArgs& a, const Split& p, bool back, hipStream_t s) {
+    switch (p.waves) {
+        case 1: return run<T, 1, STARTS>(a, p, back, s);
+        case 4: return run<T, 4, STARTS>(a, p, back, s);
+        default: return run<T, 16, STARTS>(a, p, back, s);
+    }
+}
+
+// Vectors where no step passes a row's end: the state changes in place, so no two
+// lanes may share an element.
+template <typename T> hipError_t step(const ScanArgs& a, void* state, hipStream_t s) {
+    constexpr int V = 16 / (int)sizeof(T);
+    const bool whole = a.D % V == 0;
+    const int64_t n = a.batch * (whole ? a.D / V : a.D);
+    const unsigned grid = (unsigned)std::min<int64_t>((n + 255) / 256, 1 << 20);
+    if (whole) k_scan_step<T, V><<<grid, 256, 0, s>>>(a, state);
+    else k_scan_step<T, 1><<<grid, 256, 0, s>>>(a, state);
+    return hipGetLastError();
+}
+
+template <typename F> hipError_t by_type(int type, F f) {
+    switch (type) {
+        case E_F64: return f(double{});
+        case E_BF16: return f(bf16{});
+        case E_F16: return f(_Float16{});
+        default: return f(float{});
+    }
+}
+
+hipError_t launch(int type, const ScanArgs& a, bool back, hipStream_t s) {
+    if (a.batch == 0) return hipSuccess;
+    const Split p = split_of(a.batch, a.steps, a.D);
+    return by_type(type, [&](auto t) {
+        using T = decltype(t);
+        return a.starts ? run<T, true>(a, p, back, s) : run<T, false>(a, p, back, s);
+    });
+}
+
+}  // namespace
+
+size_t scan_workspace(int type, int64_t batch, int64_t steps, int64_t D) {
+    if (batch == 0) return 0;
+    const Split p = split_of(batch, steps, D);
+    return p.segments > 1 ? (size_t)(p.segments * 2 * batch * D) * (type == E_F64 ? 8 : 4) : 0;
+}
+
+hipError_t launch_scan_forward(int type, const ScanArgs& a, hipStream_t s) { return launch(type, a, false, s); }
+hipError_t launch_scan_backward(int type, const ScanArgs& a, hipStream_t s) { return launch(type, a, true, s); }
+
+hipError_t launch_scan_step(int type, const ScanArgs& a, void* state, hipStream_t s) {
+    if (a.batch == 0) return hipSuccess;
+    return by_type(type, [&](auto t) { return step<decltype(t)>(a, state, s); });
+}
+
+}  // namespace qlayer

@@ -9,6 +9,7 @@
 #include "dropout.hpp"
 #include "embed.hpp"
 #include "rms.hpp"
+#include "scan.hpp"
 
 using namespace qlayer;
 
@@ -21,6 +22,21 @@ int check_embedding(int type, int64_t count, int64_t rows, int64_t features) {
     if (features < 1 || features > 1 << 22) return fail(QL_EINVAL, "features out of range [1, 2^22]");
     if (std::max(rows, count) > MOST_ELEMENTS / features) return fail(QL_EINVAL, "too many elements");
     return QL_OK;
+}
+
+static_assert(QL_SCAN_BLOCK == SCAN_BLOCK, "the header's block is the kernels'");
+
+int check_scan(int type, int64_t batch, int64_t steps, int64_t features) {
+    if (!known_type(type)) return fail(QL_EINVAL, "unknown type");
+    if (steps < 0 || steps > INT32_MAX) return fail(QL_EINVAL, "steps out of range [0, 2^31)");
+    if (features < 1 || features > 1 << 22) return fail(QL_EINVAL, "features out of range [1, 2^22]");
+    if (batch < 0 || batch > ((int64_t)1 << 27) / features) return fail(QL_EINVAL, "batch * features out of range [0, 2^27]");
+    if (batch * features > MOST_ELEMENTS / std::max<int64_t>(steps, 1)) return fail(QL_EINVAL, "too many elements");
+    return QL_OK;
+}
+
+bool strided_ok(int64_t batch, int64_t steps, const Strided& s) {
+    return stride_ok(batch, s.batch) && stride_ok(steps, s.step);
 }
 
 int launched(hipError_t e, const char* what) {
@@ -119,6 +135,70 @@ int ql_embedding_backward(ql_type type, int tokens_64, int64_t count, int64_t ro
     a.grad_stride = grad_stride, a.padding = padding, a.padded = has_padding != 0, a.wide = tokens_64 != 0;
     a.scale = scale;
     return launched(launch_embed_backward(type, a, ws, stream), "embedding backward");
+}
+
+int ql_gated_scan_forward(ql_type type, int64_t batch, int64_t steps, int64_t features, const void* x, int64_t x_batch,
+                          int64_t x_step, const void* gate, int64_t gate_batch, int64_t gate_step,
+                          const uint8_t* starts, const void* initial, void* h, void* last, void* states, void* ws,
+                          size_t ws_bytes, hipStream_t stream) {
+    if (int rc = check_scan(type, batch, steps, features)) return rc;
+    ScanArgs a{};
+    a.x = {(void*)x, x_batch, x_step}, a.gate = {(void*)gate, gate_batch, gate_step};
+    if (!strided_ok(batch, steps, a.x) || !strided_ok(batch, steps, a.gate))
+        return fail(QL_EINVAL, "stride out of range");
+    if (batch > 0 && steps > 0 && (!x || !gate || !h)) return fail(QL_EINVAL, "x, gate or h is NULL");
+    const int wide = wide_type(type);
+    if (!aligned(x, type) || !aligned(gate, type) || !aligned(h, type) || !aligned(initial, wide) ||
+        !aligned(last, wide) || !aligned(states, wide))
+        return fail(QL_EINVAL, "misaligned pointer");
+    if (int rc = check_workspace(ws, ws_bytes, scan_workspace(type, batch, steps, features))) return rc;
+    a.starts = starts, a.initial = initial, a.h = h, a.last = last, a.states = states, a.ws = ws;
+    a.batch = batch, a.steps = steps, a.D = features;
+    return launched(launch_scan_forward(type, a, stream), "gated scan");
+}
+
+int ql_gated_scan_workspace_bytes(ql_type type, int64_t batch, int64_t steps, int64_t features, size_t* out) {
+    if (!out) return fail(QL_EINVAL, "NULL argument");
+    if (int rc = check_scan(type, batch, steps, features)) return rc;
+    *out = scan_workspace(type, batch, steps, features);
+    return set_error(QL_OK, "");
+}
+
+int ql_gated_scan_backward(ql_type type, int64_t batch, int64_t steps, int64_t features, const void* grad_h,
+                           int64_t grad_batch, int64_t grad_step, const void* x, int64_t x_batch, int64_t x_step,
+                           const void* gate, int64_t gate_batch, int64_t gate_step, const void* states,
+                           const uint8_t* starts, const void* grad_last, void* grad_x, void* grad_gate,
+                           void* grad_initial, void* ws, size_t ws_bytes, hipStream_t stream) {
+    if (int rc = check_scan(type, batch, steps, features)) return rc;
+    ScanArgs a{};
+    a.x = {(void*)x, x_batch, x_step}, a.gate = {(void*)gate, gate_batch, gate_step};
+    a.grad = {(void*)grad_h, grad_batch, grad_step};
+    if (!strided_ok(batch, steps, a.x) || !strided_ok(batch, steps, a.gate) || !strided_ok(batch, steps, a.grad))
+        return fail(QL_EINVAL, "stride out of range");
+    if (batch > 0 && steps > 0 && (!grad_h || !x || !gate || !states || !grad_x || !grad_gate))
+        return fail(QL_EINVAL, "grad_h, x, gate, states, grad_x or grad_gate is NULL");
+    const int wide = wide_type(type);
+    if (!aligned(grad_h, type) || !aligned(x, type) || !aligned(gate, type) || !aligned(grad_x, type) ||
+        !aligned(grad_gate, type) || !aligned(states, wide) || !aligned(grad_last, wide) || !aligned(grad_initial, wide))
+        return fail(QL_EINVAL, "misaligned pointer");
+    if (int rc = check_workspace(ws, ws_bytes, scan_workspace(type, batch, steps, features))) return rc;
+    a.states = (void*)states, a.starts = starts, a.grad_last = grad_last, a.ws = ws;
+    a.grad_x = grad_x, a.grad_gate = grad_gate, a.grad_initial = grad_initial;
+    a.batch = batch, a.steps = steps, a.D = features;
+    return launched(launch_scan_backward(type, a, stream), "gated scan backward");
+}
+
+int ql_gated_scan_step(ql_type type, int64_t batch, int64_t features, const void* x, int64_t x_batch, const void* gate,
+                       int64_t gate_batch, const uint8_t* starts, void* state, void* h, hipStream_t stream) {
+    if (int rc = check_scan(type, batch, 1, features)) return rc;
+    ScanArgs a{};
+    a.x = {(void*)x, x_batch, 0}, a.gate = {(void*)gate, gate_batch, 0};
+    if (!strided_ok(batch, 1, a.x) || !strided_ok(batch, 1, a.gate)) return fail(QL_EINVAL, "stride out of range");
+    if (batch > 0 && (!x || !gate || !state || !h)) return fail(QL_EINVAL, "x, gate, state or h is NULL");
+    if (!aligned(x, type) || !aligned(gate, type) || !aligned(h, type) || !aligned(state, wide_type(type)))
+        return fail(QL_EINVAL, "misaligned pointer");
+    a.starts = starts, a.h = h, a.batch = batch, a.steps = 1, a.D = features;
+    return launched(launch_scan_step(type, a, state, stream), "gated scan step");
 }
 
 int ql_dropout(ql_type type, int64_t rows, int64_t features, const void* x, int64_t x_stride, double p, uint64_t seed,

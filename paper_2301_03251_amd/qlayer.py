@@ -107,6 +107,11 @@ def load():
     lib.ql_embedding_forward.argtypes = [T, T, I64, I64, I64, P, P, I64, D, T, I64, P, P]
     lib.ql_embedding_workspace_bytes.argtypes = [T, I64, I64, I64, ctypes.POINTER(SZ)]
     lib.ql_embedding_backward.argtypes = [T, T, I64, I64, I64, P, P, I64, D, T, I64, P, P, SZ, P]
+    lib.ql_gated_scan_forward.argtypes = [T, I64, I64, I64, P, I64, I64, P, I64, I64, P, P, P, P, P, P, SZ, P]
+    lib.ql_gated_scan_workspace_bytes.argtypes = [T, I64, I64, I64, ctypes.POINTER(SZ)]
+    lib.ql_gated_scan_backward.argtypes = [T, I64, I64, I64, P, I64, I64, P, I64, I64, P, I64, I64, P, P, P, P, P, P, P,
+                                           SZ, P]
+    lib.ql_gated_scan_step.argtypes = [T, I64, I64, P, I64, P, I64, P, P, P, P]
     lib.ql_last_error.argtypes = []
     lib.ql_last_error.restype = ctypes.c_char_p
     lib.ql_plan_info_get.argtypes = [P, ctypes.c_int, ctypes.POINTER(_PlanInfo)]

@@ -120,8 +120,10 @@ def check(t, w, grad, name, scale=1.0, padding=None):
     assert y.dtype == w.dtype and y.shape == (n, d)
     assert ((y.double() - want).abs() <= want.abs() * (u + out) + tiny).all()
     got = Q.embedding_backward(grad, t, rows, scale, padding)
-    total = torch.zeros(rows, d, dtype=torch.float64, device="cuda").index_add_(0, t.long()[keep], grad.double()[keep])
-    size = torch.zeros(rows, d, dtype=torch.float64, device="cuda").index_add_(0, t.long()[keep], grad.double()[keep].abs())
+    # summed on the host, in order
+    at, kept = t.long()[keep].cpu(), grad.double()[keep].cpu()
+    total = torch.zeros(rows, d, dtype=torch.float64).index_add_(0, at, kept).cuda()
+    size = torch.zeros(rows, d, dtype=torch.float64).index_add_(0, at, kept.abs()).cuda()
     bound = (size * 67 * u + total.abs() * out) * abs(scale) + tiny
     if name == "f64":  # the order of the reference's own sums counts too
         bound += size * abs(scale) * 2.0 ** -53 * (8 + torch.bincount(t.long()[keep], minlength=rows).max().item())
