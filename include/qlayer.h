@@ -550,7 +550,7 @@ int ql_dropout(ql_type type, int64_t rows, int64_t features, const void* x, int6
  * gate_batch elements apart, starts[batch], state[batch][features] in place,
  * h[batch][features].
  *
- * features in [1, 2^22], steps in [0, 2^31), batch * features in [0, 2^27]; batch = 0 does
+ * features in [1, 2^22], steps in [0, 2^30], batch * features in [0, 2^27]; batch = 0 does
  * nothing. ql_gated_scan_workspace_bytes gives the device workspace of a forward or
  * backward call; where it is 0 the workspace may be NULL. */
 #define QL_SCAN_BLOCK 16

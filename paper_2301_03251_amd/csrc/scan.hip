@@ -24,6 +24,7 @@
 // HBM bounds long calls; about 25 operations an element forward and 45 backward
 // come next.
 #include <algorithm>
+#include <type_traits>
 
 #include "elem.hpp"
 #include "scan.hpp"
@@ -32,6 +33,9 @@ namespace qlayer {
 namespace {
 
 constexpr int L = SCAN_BLOCK;
+
+// The wavefront's number, known to be the same in its lanes.
+__device__ __forceinline__ int wavefront() { return __builtin_amdgcn_readfirstlane(threadIdx.x >> 6); }
 
 // a = sigmoid(z) and 1 - a, neither as a difference from 1.
 __device__ __forceinline__ void gates(float z, float& a, float& rest) {
@@ -43,61 +47,116 @@ __device__ __forceinline__ void gates(double z, double& a, double& rest) {
     a = z >= 0 ? r : e * r, rest = z >= 0 ? e * r : r;
 }
 
-// The map of a row of steps. A < 0 (a cut): the state is B whatever it was before.
-template <typename R> struct Map {
+// The map of a row of steps. Where sequences may start in it, A < 0 is a cut: the
+// state is B whatever it was before.
+template <typename R, bool STARTS> struct Map {
     R A, B;
-    __device__ __forceinline__ R operator()(R h) const { return A < 0 ? B : A * h + B; }
+    __device__ __forceinline__ R operator()(R h) const { return STARTS && A < 0 ? B : A * h + B; }
     // this one, then m
     __device__ __forceinline__ void then(const Map& m) {
         B = m(B);
-        A = m.A < 0 || A < 0 ? (R)-1 : A * m.A;
+        A = STARTS && (m.A < 0 || A < 0) ? (R)-1 : A * m.A;
     }
 };
 
-// A lane's column.
+// A lane's column. The workgroup's first sequence gives the address that all lanes
+// share, and a lane adds the bytes from there to its own column (OFF: 32 bits where
+// they fit, which leaves one register and one instruction to an access).
 struct Column {
     bool live;
-    int64_t at, batch, d;  // among all columns; its sequence and feature
+    int64_t at, batch, first, d;  // among all columns; its sequence, the workgroup's first one, its feature
     __device__ __forceinline__ Column(const ScanArgs& a) {
-        const int64_t c = (int64_t)blockIdx.x * 64 + (threadIdx.x & 63), n = a.batch * a.D;
-        live = c < n, at = min(c, n - 1), batch = at / a.D, d = at % a.D;
+        const int64_t c0 = (int64_t)blockIdx.x * 64, c = c0 + (threadIdx.x & 63), n = a.batch * a.D;
+        live = c < n, at = min(c, n - 1), first = c0 / a.D;
+        batch = first, d = at - first * a.D;
+        if (d >= a.D) batch = at / a.D, d = at % a.D;
     }
-    template <typename T> __device__ __forceinline__ const T* of(const Strided& s) const {
-        return (const T*)s.p + batch * s.batch + d;
+};
+
+// An array's column. Rows (steps) are walked with an address in scalar registers,
+// which the compiler must not fold into the lanes' own: an access then is that
+// address and the lane's bytes.
+typedef __attribute__((address_space(1))) char* Row;
+
+template <typename T, typename OFF> struct Lane {
+    Row base;
+    int64_t step;  // bytes
+    OFF off;
+    __device__ __forceinline__ Lane(const Column& c, const Strided& s) : Lane(c, s.p, s.batch, s.step) {}
+    __device__ __forceinline__ Lane(const Column& c, const void* p, int64_t batch, int64_t step_)
+        : base((Row)p + c.first * batch * (int64_t)sizeof(T)),
+          step(step_ * (int64_t)sizeof(T)),
+          off((OFF)(((c.batch - c.first) * batch + c.d) * (int64_t)sizeof(T))) {}
+    __device__ __forceinline__ Row row(int t) const { return base + t * step; }
+    // the lane's bytes as the compiler finds them anew where a block's accesses begin
+    __device__ __forceinline__ OFF here() const {
+        OFF o = off;
+        asm("" : "+v"(o));
+        return o;
+    }
+    using Bits = std::conditional_t<sizeof(T) == 2, uint16_t, std::conditional_t<sizeof(T) == 4, uint32_t, uint64_t>>;
+    using Place = __attribute__((address_space(1))) Bits*;
+    __device__ __forceinline__ T load(Row row, OFF o) const {
+        asm("" : "+s"(row));
+        return __builtin_bit_cast(T, *(Place)(row + o));
+    }
+    __device__ __forceinline__ void store(Row row, OFF o, T v) const {
+        asm("" : "+s"(row));
+        *(Place)(row + o) = __builtin_bit_cast(Bits, v);
     }
 };
 
 // The steps of block k that start a sequence, as bits.
-template <bool STARTS> __device__ __forceinline__ uint32_t starts_of(const ScanArgs& a, const Column& c, int64_t k) {
+template <bool STARTS> __device__ __forceinline__ uint32_t starts_of(const ScanArgs& a, const Column& c, int k, int steps) {
     uint32_t bits = 0;
     if constexpr (STARTS) {
         const uint8_t* s = a.starts + c.batch * a.steps;
 #pragma unroll
         for (int j = 0; j < L; j++) {
-            const int64_t t = k * L + j;
-            bits |= (uint32_t)(s[min(t, a.steps - 1)] != 0 && t < a.steps) << j;
+            const int t = k * L + j;
+            bits |= (uint32_t)(s[min(t, steps - 1)] != 0 && t < steps) << j;
         }
     }
     return bits;
 }
 
 // Block k's elements of a column; past the end the last step's, which the caller leaves out.
-template <typename T> __device__ __forceinline__ void load_block(T (&v)[L], const T* p, int64_t step, int64_t k, int64_t steps) {
+template <typename T, typename OFF>
+__device__ __forceinline__ void load_block(T (&v)[L], const Lane<T, OFF>& p, int k, int steps) {
+    const OFF o = p.here();
+    if (steps - k * L >= L) {
+        Row row = p.row(k * L);
 #pragma unroll
-    for (int j = 0; j < L; j++) v[j] = p[min(k * L + j, steps - 1) * step];
+        for (int j = 0; j < L; j++, row += p.step) v[j] = p.load(row, o);
+    } else {
+#pragma unroll
+        for (int j = 0; j < L; j++) v[j] = p.load(p.row(min(k * L + j, steps - 1)), o);
+        asm volatile("");  // the two ways stay apart: their addresses would not fit the scalar registers
+    }
+}
+
+// Steps past the end leave the state as it is.
+template <typename R> __device__ __forceinline__ void leave_out(int left, R (&f)[L], R (&b)[L]) {
+    if (left >= L) return;
+#pragma unroll
+    for (int j = 0; j < L; j++)
+        if (j >= left) f[j] = 1, b[j] = 0;
 }
 
 // The map of a forward block, and its factors.
 template <typename T, bool STARTS, typename R>
-__device__ __forceinline__ Map<R> forward_map(const T (&x)[L], const T (&z)[L], uint32_t starts, int64_t left, R (&f)[L], R (&b)[L]) {
-    Map<R> m{1, 0};
+__device__ __forceinline__ Map<R, STARTS> forward_map(const T (&x)[L], const T (&z)[L], uint32_t starts, int left, R (&f)[L], R (&b)[L]) {
+    Map<R, STARTS> m{1, 0};
     bool cut = false;
 #pragma unroll
     for (int j = 0; j < L; j++) {
         R rest;
         gates(up(z[j]), f[j], rest);
         b[j] = rest * up(x[j]);
-        if (j >= left) f[j] = 1, b[j] = 0;
+    }
+    leave_out(left, f, b);
+#pragma unroll
+    for (int j = 0; j < L; j++) {
         if (STARTS && ((starts >> j) & 1)) m.B = b[j], cut = true;
         else m.B = f[j] * m.B + b[j];
         m.A *= f[j];
@@ -108,8 +167,8 @@ __device__ __forceinline__ Map<R> forward_map(const T (&x)[L], const T (&z)[L], 
 
 // The map of a backward block, last step first, of what comes back to a step.
 template <bool STARTS, typename R>
-__device__ __forceinline__ Map<R> backward_map(const R (&f)[L], const R (&g)[L], uint32_t starts) {
-    Map<R> m{1, 0};
+__device__ __forceinline__ Map<R, STARTS> backward_map(const R (&f)[L], const R (&g)[L], uint32_t starts) {
+    Map<R, STARTS> m{1, 0};
     bool cut = false;
 #pragma unroll
     for (int j = L - 1; j >= 0; j--) {
@@ -123,79 +182,85 @@ __device__ __forceinline__ Map<R> backward_map(const R (&f)[L], const R (&g)[L],
 
 // Where the segment begins: the maps of the segments that come before it, each
 // wavefront a share of them, on the state that the row begins with.
-template <int W, typename R>
+template <int W, bool STARTS, typename R>
 __device__ __forceinline__ R begin_segment(R state, const R* maps, int64_t columns, int64_t column, int first, int count, int dir, R (&A)[W][64], R (&B)[W][64]) {
-    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, each = (count + W - 1) / W;
-    Map<R> m{1, 0};
+    const int wave = wavefront(), lane = threadIdx.x & 63, each = (count + W - 1) / W;
+    Map<R, STARTS> m{1, 0};
 #pragma unroll 4
     for (int i = wave * each; i < min(count, (wave + 1) * each); i++) {
         const R* p = maps + (int64_t)(first + dir * i) * 2 * columns + column;
-        m.then(Map<R>{p[0], p[columns]});
+        m.then(Map<R, STARTS>{p[0], p[columns]});
     }
     A[wave][lane] = m.A, B[wave][lane] = m.B;
     __syncthreads();
 #pragma unroll
-    for (int w = 0; w < W; w++) state = Map<R>{A[w][lane], B[w][lane]}(state);
+    for (int w = 0; w < W; w++) state = Map<R, STARTS>{A[w][lane], B[w][lane]}(state);
     __syncthreads();
     return state;
 }
 
-template <typename T, int W, bool STARTS> __global__ __launch_bounds__(64 * W) void k_scan_fwd(ScanArgs a, int64_t blocks, int64_t each) {
+template <typename T, typename OFF, int W, bool STARTS> __global__ __launch_bounds__(64 * W) void k_scan_fwd(ScanArgs a, int blocks, int each) {
     using R = Acc<T>;
     __shared__ R A[2][W][64], B[2][W][64];
-    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+    const int wave = wavefront(), lane = threadIdx.x & 63;
     const Column c(a);
-    const T *x = c.of<T>(a.x), *z = c.of<T>(a.gate);
-    const int64_t k0 = blockIdx.y * each, k1 = min(k0 + each, blocks);
+    const Lane<T, OFF> x(c, a.x), z(c, a.gate), out(c, a.h, a.steps * a.D, a.D);
+    const Lane<R, OFF> kept(c, a.states, blocks * a.D, a.D);
+    const int steps = (int)a.steps, k0 = blockIdx.y * each, k1 = min(k0 + each, blocks);
     R state = a.initial ? ((const R*)a.initial)[c.at] : 0;
-    if (blockIdx.y > 0) state = begin_segment<W, R>(state, (const R*)a.ws, a.batch * a.D, c.at, 0, blockIdx.y, 1, A[0], B[0]);
+    if (blockIdx.y > 0) state = begin_segment<W, STARTS, R>(state, (const R*)a.ws, a.batch * a.D, c.at, 0, blockIdx.y, 1, A[0], B[0]);
     int turn = 0;
-    for (int64_t base = k0; base < k1; base += W, turn ^= 1) {
-        const int64_t k = base + wave, left = k < k1 ? a.steps - k * L : 0;
+    for (int base = k0; base < k1; base += W, turn ^= 1) {
+        const int k = base + wave, left = k < k1 ? steps - k * L : 0;
         T vx[L], vz[L];
-        load_block(vx, x, a.x.step, k, a.steps);
-        load_block(vz, z, a.gate.step, k, a.steps);
-        const uint32_t starts = left > 0 ? starts_of<STARTS>(a, c, k) : 0;
+        load_block(vx, x, k, steps);
+        load_block(vz, z, k, steps);
+        const uint32_t starts = left > 0 ? starts_of<STARTS>(a, c, k, steps) : 0;
         R f[L], b[L];
-        const Map<R> m = forward_map<T, STARTS, R>(vx, vz, starts, left, f, b);
+        const Map<R, STARTS> m = forward_map<T, STARTS, R>(vx, vz, starts, left, f, b);
         A[turn][wave][lane] = m.A, B[turn][wave][lane] = m.B;
         __syncthreads();
         R h = state;
 #pragma unroll
         for (int w = 0; w < W; w++) {
             if (w == wave) h = state;
-            state = Map<R>{A[turn][w][lane], B[turn][w][lane]}(state);
+            state = Map<R, STARTS>{A[turn][w][lane], B[turn][w][lane]}(state);
         }
         if (left <= 0 || !c.live) continue;
-        if (a.states) ((R*)a.states)[(c.batch * blocks + k) * a.D + c.d] = h;
-        T* out = (T*)a.h + (c.batch * a.steps + k * L) * a.D + c.d;
+        if (a.states) kept.store(kept.row(k), kept.here(), h);
+        auto apply = [&](auto whole) {
+            Row row = out.row(k * L);
+            const OFF o = out.here();
 #pragma unroll
-        for (int j = 0; j < L; j++) {
-            h = STARTS && ((starts >> j) & 1) ? b[j] : f[j] * h + b[j];
-            if (j < left) out[j * a.D] = down<T>(h);
-        }
+            for (int j = 0; j < L; j++, row += out.step) {
+                h = STARTS && ((starts >> j) & 1) ? b[j] : f[j] * h + b[j];
+                if (decltype(whole)::value || j < left) out.store(row, o, down<T>(h));
+            }
+        };
+        if (left >= L) apply(std::true_type{});
+        else apply(std::false_type{});
     }
     if (a.last && k1 == blocks && wave == 0 && c.live) ((R*)a.last)[c.at] = state;
 }
 
 // ws[segment][2][columns]: the segments' maps, forward or backward.
-template <typename T, int W, bool STARTS, bool BACK>
-__global__ __launch_bounds__(64 * W) void k_scan_maps(ScanArgs a, int64_t blocks, int64_t each) {
+template <typename T, typename OFF, int W, bool STARTS, bool BACK>
+__global__ __launch_bounds__(64 * W) void k_scan_maps(ScanArgs a, int blocks, int each) {
     using R = Acc<T>;
     __shared__ R A[W][64], B[W][64];
-    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+    const int wave = wavefront(), lane = threadIdx.x & 63;
     const Column c(a);
-    const T *v = c.of<T>(BACK ? a.grad : a.x), *z = c.of<T>(a.gate);
-    const int64_t k0 = blockIdx.y * each, k1 = min(k0 + each, blocks), share = (each + W - 1) / W;
+    const Lane<T, OFF> v(c, BACK ? a.grad : a.x), z(c, a.gate);
+    const int steps = (int)a.steps, k0 = blockIdx.y * each, k1 = min(k0 + each, blocks), share = (each + W - 1) / W;
     // wavefront 0 has the blocks that come first in the maps' direction
-    const int64_t n = k1 - k0, i0 = min(wave * share, n), i1 = min(i0 + share, n);
-    Map<R> m{1, 0};
-    for (int64_t i = i0; i < i1; i++) {
-        const int64_t k = BACK ? k1 - 1 - i : k0 + i, left = a.steps - k * L;
+    const int n = k1 - k0, i0 = min(wave * share, n), i1 = min(i0 + share, n);
+    Map<R, STARTS> m{1, 0};
+    for (int i = i0; i < i1; i++) {
+        const int k = BACK ? k1 - 1 - i : k0 + i, left = steps - k * L;
         T vv[L], vz[L];
-        load_block(vv, v, BACK ? a.grad.step : a.x.step, k, a.steps);
-        load_block(vz, z, a.gate.step, k, a.steps);
-        const uint32_t starts = starts_of<STARTS>(a, c, k);
+        load_block(vv, v, k, steps);
+        load_block(vz, z, k, steps);
+        const uint32_t starts = starts_of<STARTS>(a, c, k, steps);
         R f[L], b[L];
         if constexpr (BACK) {
 #pragma unroll
@@ -203,8 +268,8 @@ __global__ __launch_bounds__(64 * W) void k_scan_maps(ScanArgs a, int64_t blocks
                 R rest;
                 gates(up(vz[j]), f[j], rest);
                 b[j] = up(vv[j]);
-                if (j >= left) f[j] = 1, b[j] = 0;
             }
+            leave_out(left, f, b);
             m.then(backward_map<STARTS, R>(f, b, starts));
         } else {
             m.then(forward_map<T, STARTS, R>(vv, vz, starts, left, f, b));
@@ -214,62 +279,72 @@ __global__ __launch_bounds__(64 * W) void k_scan_maps(ScanArgs a, int64_t blocks
     __syncthreads();
     if (wave > 0 || !c.live) return;
 #pragma unroll
-    for (int w = 1; w < W; w++) m.then(Map<R>{A[w][lane], B[w][lane]});
+    for (int w = 1; w < W; w++) m.then(Map<R, STARTS>{A[w][lane], B[w][lane]});
     R* out = (R*)a.ws + (int64_t)blockIdx.y * 2 * a.batch * a.D + c.at;
     out[0] = m.A, out[a.batch * a.D] = m.B;
 }
 
-template <typename T, int W, bool STARTS> __global__ __launch_bounds__(64 * W) void k_scan_bwd(ScanArgs a, int64_t blocks, int64_t each) {
+template <typename T, typename OFF, int W, bool STARTS> __global__ __launch_bounds__(64 * W) void k_scan_bwd(ScanArgs a, int blocks, int each) {
     using R = Acc<T>;
     __shared__ R A[2][W][64], B[2][W][64];
-    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+    const int wave = wavefront(), lane = threadIdx.x & 63;
     const Column c(a);
-    const T *x = c.of<T>(a.x), *z = c.of<T>(a.gate), *g = c.of<T>(a.grad);
-    const int64_t k0 = blockIdx.y * each, k1 = min(k0 + each, blocks);
+    const Lane<T, OFF> x(c, a.x), z(c, a.gate), g(c, a.grad);
+    const Lane<T, OFF> dx(c, a.grad_x, a.steps * a.D, a.D), dz(c, a.grad_gate, a.steps * a.D, a.D);
+    const Lane<R, OFF> kept(c, a.states, blocks * a.D, a.D);
+    const int steps = (int)a.steps, k0 = blockIdx.y * each, k1 = min(k0 + each, blocks);
     const int behind = gridDim.y - 1 - blockIdx.y;
     R back = a.grad_last ? ((const R*)a.grad_last)[c.at] : 0;
-    if (behind > 0) back = begin_segment<W, R>(back, (const R*)a.ws, a.batch * a.D, c.at, gridDim.y - 1, behind, -1, A[0], B[0]);
+    if (behind > 0) back = begin_segment<W, STARTS, R>(back, (const R*)a.ws, a.batch * a.D, c.at, gridDim.y - 1, behind, -1, A[0], B[0]);
     int turn = 0;
-    for (int64_t top = k1; top > k0; top -= W, turn ^= 1) {
-        const int64_t k = max(top - 1 - wave, k0), left = top - 1 - wave >= k0 ? a.steps - k * L : 0;
+    for (int top = k1; top > k0; top -= W, turn ^= 1) {
+        const int k = max(top - 1 - wave, k0), left = top - 1 - wave >= k0 ? steps - k * L : 0;
         T vx[L], vz[L], vg[L];
-        load_block(vx, x, a.x.step, k, a.steps);
-        load_block(vz, z, a.gate.step, k, a.steps);
-        load_block(vg, g, a.grad.step, k, a.steps);
-        R h = ((const R*)a.states)[(c.batch * blocks + k) * a.D + c.d];
-        const uint32_t starts = left > 0 ? starts_of<STARTS>(a, c, k) : 0;
+        load_block(vx, x, k, steps);
+        load_block(vz, z, k, steps);
+        load_block(vg, g, k, steps);
+        R h = kept.load(kept.row(k), kept.here());
+        const uint32_t starts = left > 0 ? starts_of<STARTS>(a, c, k, steps) : 0;
         // f = a, r = 1 - a, q = dz / G, b = g
         R f[L], r[L], q[L], b[L];
+        // one after the other, which keeps to the registers of four wavefronts a SIMD
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int j = 0; j < L; j++) gates(up(vz[j]), f[j], r[j]);
+        __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
         for (int j = 0; j < L; j++) {
-            gates(up(vz[j]), f[j], r[j]);
             const R v = up(vx[j]), before = STARTS && ((starts >> j) & 1) ? 0 : h;
             q[j] = (before - v) * (f[j] * r[j]);
             h = f[j] * before + r[j] * v;
             b[j] = up(vg[j]);
-            if (j >= left) f[j] = 1, b[j] = 0;
         }
-        const Map<R> m = backward_map<STARTS, R>(f, b, starts);
+        leave_out(left, f, b);
+        const Map<R, STARTS> m = backward_map<STARTS, R>(f, b, starts);
         A[turn][wave][lane] = m.A, B[turn][wave][lane] = m.B;
         __syncthreads();
         R s = back;
 #pragma unroll
         for (int w = 0; w < W; w++) {
             if (w == wave) s = back;
-            back = Map<R>{A[turn][w][lane], B[turn][w][lane]}(back);
+            back = Map<R, STARTS>{A[turn][w][lane], B[turn][w][lane]}(back);
         }
         if (left <= 0 || !c.live) continue;
-        const int64_t at = (c.batch * a.steps + k * L) * a.D + c.d;
-        T *dx = (T*)a.grad_x + at, *dz = (T*)a.grad_gate + at;
+        auto apply = [&](auto whole) {
+            Row row_x = dx.row(k * L + L - 1), row_z = dz.row(k * L + L - 1);
+            const OFF o = dx.here();
 #pragma unroll
-        for (int j = L - 1; j >= 0; j--) {
-            const R G = b[j] + s;
-            s = STARTS && ((starts >> j) & 1) ? 0 : f[j] * G;
-            if (j < left) {
-                dx[j * a.D] = down<T>(r[j] * G);
-                dz[j * a.D] = down<T>(q[j] * G);
+            for (int j = L - 1; j >= 0; j--, row_x -= dx.step, row_z -= dz.step) {
+                const R G = b[j] + s;
+                s = STARTS && ((starts >> j) & 1) ? 0 : f[j] * G;
+                if (decltype(whole)::value || j < left) {
+                    dx.store(row_x, o, down<T>(r[j] * G));
+                    dz.store(row_z, o, down<T>(q[j] * G));
+                }
             }
-        }
+        };
+        if (left >= L) apply(std::true_type{});
+        else apply(std::false_type{});
     }
     if (a.grad_initial && k0 == 0 && wave == 0 && c.live) ((R*)a.grad_initial)[c.at] = back;
 }
@@ -316,23 +391,32 @@ Split split_of(const int64_t batch, int64_t steps, int64_t D) {
     return p;
 }
 
-template <typename T, int W, bool STARTS> hipError_t run(const ScanArgs& a, const Split& p, bool back, hipStream_t s) {
+template <typename T, typename OFF, int W, bool STARTS> hipError_t run(const ScanArgs& a, const Split& p, bool back, hipStream_t s) {
     const dim3 grid((unsigned)p.groups, (unsigned)p.segments);
     if (back) {
-        if (p.segments > 1) k_scan_maps<T, W, STARTS, true><<<grid, 64 * W, 0, s>>>(a, p.blocks, p.each);
-        k_scan_bwd<T, W, STARTS><<<grid, 64 * W, 0, s>>>(a, p.blocks, p.each);
+        if (p.segments > 1) k_scan_maps<T, OFF, W, STARTS, true><<<grid, 64 * W, 0, s>>>(a, (int)p.blocks, (int)p.each);
+        k_scan_bwd<T, OFF, W, STARTS><<<grid, 64 * W, 0, s>>>(a, (int)p.blocks, (int)p.each);
     } else {
-        if (p.segments > 1) k_scan_maps<T, W, STARTS, false><<<grid, 64 * W, 0, s>>>(a, p.blocks, p.each);
-        k_scan_fwd<T, W, STARTS><<<grid, 64 * W, 0, s>>>(a, p.blocks, p.each);
+        if (p.segments > 1) k_scan_maps<T, OFF, W, STARTS, false><<<grid, 64 * W, 0, s>>>(a, (int)p.blocks, (int)p.each);
+        k_scan_fwd<T, OFF, W, STARTS><<<grid, 64 * W, 0, s>>>(a, (int)p.blocks, (int)p.each);
     }
     return hipGetLastError();
 }
 
+// Whether the bytes from a workgroup's first sequence to any of its columns fit 32 bits.
+bool near_by(const ScanArgs& a, int size, int wide) {
+    const int64_t most = ((int64_t)1 << 32) - 1, sequences = std::min(a.batch - 1, 63 / a.D + 1);
+    auto fits = [&](int64_t batch, int bytes) { return batch <= (most / bytes - a.D) / std::max<int64_t>(sequences, 1); };
+    return fits(a.x.batch, size) && fits(a.gate.batch, size) && fits(a.grad.batch, size) && fits(a.steps * a.D, size) &&
+           fits((a.steps + L - 1) / L * a.D, wide);
+}
+
 template <typename T, bool STARTS> hipError_t run(const ScanArgs& a, const Split& p, bool back, hipStream_t s) {
+    if (!near_by(a, sizeof(T), sizeof(Acc<T>))) return run<T, uint64_t, 16, STARTS>(a, p, back, s);
     switch (p.waves) {
-        case 1: return run<T, 1, STARTS>(a, p, back, s);
-        case 4: return run<T, 4, STARTS>(a, p, back, s);
-        default: return run<T, 16, STARTS>(a, p, back, s);
+        case 1: return run<T, uint32_t, 1, STARTS>(a, p, back, s);
+        case 4: return run<T, uint32_t, 4, STARTS>(a, p, back, s);
+        default: return run<T, uint32_t, 16, STARTS>(a, p, back, s);
     }
 }
 

@@ -28,7 +28,7 @@ static_assert(QL_SCAN_BLOCK == SCAN_BLOCK, "the header's block is the kernels'")
 
 int check_scan(int type, int64_t batch, int64_t steps, int64_t features) {
     if (!known_type(type)) return fail(QL_EINVAL, "unknown type");
-    if (steps < 0 || steps > INT32_MAX) return fail(QL_EINVAL, "steps out of range [0, 2^31)");
+    if (steps < 0 || steps > 1 << 30) return fail(QL_EINVAL, "steps out of range [0, 2^30]");
     if (features < 1 || features > 1 << 22) return fail(QL_EINVAL, "features out of range [1, 2^22]");
     if (batch < 0 || batch > ((int64_t)1 << 27) / features) return fail(QL_EINVAL, "batch * features out of range [0, 2^27]");
     if (batch * features > MOST_ELEMENTS / std::max<int64_t>(steps, 1)) return fail(QL_EINVAL, "too many elements");

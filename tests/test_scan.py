@@ -47,7 +47,7 @@ BAD_SIZES = [dict(type_=4), dict(batch=-1), dict(n=0), dict(n=(1 << 22) + 1), di
 
 
 @pytest.mark.parametrize("kw,code", [(k, -1) for k in BAD_SIZES] + [
-    (dict(steps=-1), -1), (dict(steps=1 << 31), -1), (dict(batch=1 << 20, steps=1 << 30), -1), (dict(xs=-1), -1), (dict(zs=-1), -1),
+    (dict(steps=-1), -1), (dict(steps=(1 << 30) + 1), -1), (dict(batch=1 << 20, steps=1 << 30), -1), (dict(xs=-1), -1), (dict(zs=-1), -1),
     (dict(xs=1 << 46), -1), (dict(x=None), -1), (dict(z=None), -1), (dict(h=None), -1), (dict(x=ODD), -1), (dict(z=ODD), -1),
     (dict(h=ODD), -1), (dict(initial=ODD), -1), (dict(last=ODD), -1), (dict(states=ODD), -1), (dict(steps=5000), -1),
     (dict(steps=5000, ws=ctypes.c_void_p(0x1008), ws_bytes=1 << 20), -1), (dict(steps=5000, ws=FAKE, ws_bytes=8), -2),
@@ -93,7 +93,7 @@ def test_workspace_bytes(lib):
     for steps in (0, 1, 16, 256):
         assert lib.ql_gated_scan_workspace_bytes(F32, 3, steps, 100, ctypes.byref(out)) == 0 and out.value == 0
     assert lib.ql_gated_scan_workspace_bytes(F32, 1, 65536, 64, ctypes.byref(out)) == 0 and out.value > 0
-    assert lib.ql_gated_scan_workspace_bytes(F32, 1, (1 << 31) - 1, 64, ctypes.byref(out)) == 0 and out.value <= 4096 * 2 * 64 * 4
+    assert lib.ql_gated_scan_workspace_bytes(F32, 1, 1 << 30, 64, ctypes.byref(out)) == 0 and out.value <= 4096 * 2 * 64 * 4
     assert lib.ql_gated_scan_workspace_bytes(F32, 0, 65536, 64, ctypes.byref(out)) == 0 and out.value == 0
 
 
