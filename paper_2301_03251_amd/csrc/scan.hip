@@ -210,14 +210,15 @@ template <typename T, typename OFF, int W, bool STARTS> __global__ __launch_boun
     R state = a.initial ? ((const R*)a.initial)[c.at] : 0;
     if (blockIdx.y > 0) state = begin_segment<W, STARTS, R>(state, (const R*)a.ws, a.batch * a.D, c.at, 0, blockIdx.y, 1, A[0], B[0]);
     int turn = 0;
+    T vx[L], vz[L];
+    if (k0 < k1) load_block(vx, x, k0 + wave, steps), load_block(vz, z, k0 + wave, steps);
     for (int base = k0; base < k1; base += W, turn ^= 1) {
         const int k = base + wave, left = k < k1 ? steps - k * L : 0;
-        T vx[L], vz[L];
-        load_block(vx, x, k, steps);
-        load_block(vz, z, k, steps);
         const uint32_t starts = left > 0 ? starts_of<STARTS>(a, c, k, steps) : 0;
         R f[L], b[L];
         const Map<R, STARTS> m = forward_map<T, STARTS, R>(vx, vz, starts, left, f, b);
+        // the next block is under way while this one is finished
+        if (base + W < k1) load_block(vx, x, k + W, steps), load_block(vz, z, k + W, steps);
         A[turn][wave][lane] = m.A, B[turn][wave][lane] = m.B;
         __syncthreads();
         R h = state;
@@ -297,21 +298,32 @@ template <typename T, typename OFF, int W, bool STARTS> __global__ __launch_boun
     R back = a.grad_last ? ((const R*)a.grad_last)[c.at] : 0;
     if (behind > 0) back = begin_segment<W, STARTS, R>(back, (const R*)a.ws, a.batch * a.D, c.at, gridDim.y - 1, behind, -1, A[0], B[0]);
     int turn = 0;
-    for (int top = k1; top > k0; top -= W, turn ^= 1) {
-        const int k = max(top - 1 - wave, k0), left = top - 1 - wave >= k0 ? steps - k * L : 0;
-        T vx[L], vz[L], vg[L];
+    T vx[L], vz[L], vg[L];
+    R nh = 0;
+    auto fetch = [&](int top) {
+        const int k = max(top - 1 - wave, k0);
         load_block(vx, x, k, steps);
         load_block(vz, z, k, steps);
         load_block(vg, g, k, steps);
-        R h = kept.load(kept.row(k), kept.here());
+        nh = kept.load(kept.row(k), kept.here());
+    };
+    // fp64 has no registers for a second block
+    constexpr bool AHEAD = sizeof(T) < 8;
+    if (AHEAD && k1 > k0) fetch(k1);
+    for (int top = k1; top > k0; top -= W, turn ^= 1) {
+        const int k = max(top - 1 - wave, k0), left = top - 1 - wave >= k0 ? steps - k * L : 0;
+        if constexpr (!AHEAD) fetch(top);
+        R h = nh;
         const uint32_t starts = left > 0 ? starts_of<STARTS>(a, c, k, steps) : 0;
         // f = a, r = 1 - a, q = dz / G, b = g
         R f[L], r[L], q[L], b[L];
         // one after the other, which keeps to the registers of four wavefronts a SIMD
         __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-        for (int j = 0; j < L; j++) gates(up(vz[j]), f[j], r[j]);
-        __builtin_amdgcn_sched_barrier(0);
+        for (int j = 0; j < L; j++) {
+            gates(up(vz[j]), f[j], r[j]);
+            if (j % 4 == 3) __builtin_amdgcn_sched_barrier(0);
+        }
 #pragma unroll
         for (int j = 0; j < L; j++) {
             const R v = up(vx[j]), before = STARTS && ((starts >> j) & 1) ? 0 : h;
@@ -321,10 +333,12 @@ template <typename T, typename OFF, int W, bool STARTS> __global__ __launch_boun
         }
         leave_out(left, f, b);
         const Map<R, STARTS> m = backward_map<STARTS, R>(f, b, starts);
+        // the next block is under way while this one is finished
+        if (AHEAD && top - W > k0) fetch(top - W);
         A[turn][wave][lane] = m.A, B[turn][wave][lane] = m.B;
         __syncthreads();
         R s = back;
-#pragma unroll
+#pragma unroll 4  // 16 maps at once would not fit the registers
         for (int w = 0; w < W; w++) {
             if (w == wave) s = back;
             back = Map<R, STARTS>{A[turn][w][lane], B[turn][w][lane]}(back);
@@ -378,28 +392,33 @@ struct Split {
     int waves;
     int64_t groups, blocks, each, segments;
 };
-Split split_of(const int64_t batch, int64_t steps, int64_t D) {
+// Wavefronts of a workgroup, which leave a block its registers and the next one's (of
+// 16 they are as fast forward: 97 us for 94 at 8x4096x2048 bfloat16, 20.4 for 22.6
+// at 1x65536x64 float32; backward there is no room for the next block, 161 for 144).
+constexpr int WAVES = 8;
+
+Split split_of(int64_t batch, int64_t steps, int64_t D) {
     Split p{};
     p.groups = (batch * D + 63) / 64;
     p.blocks = (steps + L - 1) / L;
-    p.waves = p.blocks <= 1 ? 1 : p.blocks <= 4 ? 4 : 16;
+    p.waves = p.blocks <= 1 ? 1 : p.blocks <= 4 ? 4 : WAVES;
     const int64_t turns = std::max<int64_t>(1, (p.blocks + p.waves - 1) / p.waves);
-    // segments of whole turns, as many as give every compute unit a workgroup
+    // segments of whole turns, as many as give every compute unit a workgroup: the maps
+    // read x and gate (gate and grad) once more, so no more (8x4096x2048 bfloat16, 256
+    // groups: 94 and 144 us in one segment, 155 and 204 in two; 1x65536x64 float32, one
+    // group: 47 us forward and backward in 256 segments, 58 in 512)
     const int64_t want = std::min<int64_t>(turns, std::max<int64_t>(1, 256 / p.groups));
     p.each = (turns + want - 1) / want * p.waves;
     p.segments = std::max<int64_t>(1, (p.blocks + p.each - 1) / p.each);
     return p;
 }
 
-template <typename T, typename OFF, int W, bool STARTS> hipError_t run(const ScanArgs& a, const Split& p, bool back, hipStream_t s) {
+template <typename T, typename OFF, int W, bool STARTS, bool BACK> hipError_t run(const ScanArgs& a, const Split& p, hipStream_t s) {
     const dim3 grid((unsigned)p.groups, (unsigned)p.segments);
-    if (back) {
-        if (p.segments > 1) k_scan_maps<T, OFF, W, STARTS, true><<<grid, 64 * W, 0, s>>>(a, (int)p.blocks, (int)p.each);
-        k_scan_bwd<T, OFF, W, STARTS><<<grid, 64 * W, 0, s>>>(a, (int)p.blocks, (int)p.each);
-    } else {
-        if (p.segments > 1) k_scan_maps<T, OFF, W, STARTS, false><<<grid, 64 * W, 0, s>>>(a, (int)p.blocks, (int)p.each);
-        k_scan_fwd<T, OFF, W, STARTS><<<grid, 64 * W, 0, s>>>(a, (int)p.blocks, (int)p.each);
-    }
+    const int blocks = (int)p.blocks, each = (int)p.each;
+    if (p.segments > 1) k_scan_maps<T, OFF, W, STARTS, BACK><<<grid, 64 * W, 0, s>>>(a, blocks, each);
+    if constexpr (BACK) k_scan_bwd<T, OFF, W, STARTS><<<grid, 64 * W, 0, s>>>(a, blocks, each);
+    else k_scan_fwd<T, OFF, W, STARTS><<<grid, 64 * W, 0, s>>>(a, blocks, each);
     return hipGetLastError();
 }
 
@@ -411,12 +430,18 @@ bool near_by(const ScanArgs& a, int size, int wide) {
            fits((a.steps + L - 1) / L * a.D, wide);
 }
 
-template <typename T, bool STARTS> hipError_t run(const ScanArgs& a, const Split& p, bool back, hipStream_t s) {
-    if (!near_by(a, sizeof(T), sizeof(Acc<T>))) return run<T, uint64_t, 16, STARTS>(a, p, back, s);
+template <typename T, bool STARTS, bool BACK> hipError_t run(const ScanArgs& a, const Split& p, hipStream_t s) {
+    if (!near_by(a, sizeof(T), sizeof(Acc<T>))) {
+        switch (p.waves) {
+            case 1: return run<T, uint64_t, 1, STARTS, BACK>(a, p, s);
+            case 4: return run<T, uint64_t, 4, STARTS, BACK>(a, p, s);
+            default: return run<T, uint64_t, WAVES, STARTS, BACK>(a, p, s);
+        }
+    }
     switch (p.waves) {
-        case 1: return run<T, uint32_t, 1, STARTS>(a, p, back, s);
-        case 4: return run<T, uint32_t, 4, STARTS>(a, p, back, s);
-        default: return run<T, uint32_t, 16, STARTS>(a, p, back, s);
+        case 1: return run<T, uint32_t, 1, STARTS, BACK>(a, p, s);
+        case 4: return run<T, uint32_t, 4, STARTS, BACK>(a, p, s);
+        default: return run<T, uint32_t, WAVES, STARTS, BACK>(a, p, s);
     }
 }
 
@@ -446,7 +471,8 @@ hipError_t launch(int type, const ScanArgs& a, bool back, hipStream_t s) {
     const Split p = split_of(a.batch, a.steps, a.D);
     return by_type(type, [&](auto t) {
         using T = decltype(t);
-        return a.starts ? run<T, true>(a, p, back, s) : run<T, false>(a, p, back, s);
+        if (back) return a.starts ? run<T, true, true>(a, p, s) : run<T, false, true>(a, p, s);
+        return a.starts ? run<T, true, false>(a, p, s) : run<T, false, false>(a, p, s);
     });
 }
 
@@ -454,8 +480,8 @@ hipError_t launch(int type, const ScanArgs& a, bool back, hipStream_t s) {
 
 size_t scan_workspace(int type, int64_t batch, int64_t steps, int64_t D) {
     if (batch == 0) return 0;
-    const Split p = split_of(batch, steps, D);
-    return p.segments > 1 ? (size_t)(p.segments * 2 * batch * D) * (type == E_F64 ? 8 : 4) : 0;
+    const int64_t segments = split_of(batch, steps, D).segments;
+    return segments > 1 ? (size_t)(segments * 2 * batch * D) * (type == E_F64 ? 8 : 4) : 0;
 }
 
 hipError_t launch_scan_forward(int type, const ScanArgs& a, hipStream_t s) { return launch(type, a, false, s); }

@@ -206,7 +206,7 @@ def check_case(name, x, z, initial, starts, g, g_last):
     return h, last, states
 
 
-# one wavefront, four and sixteen; blocks and turns cut short; few columns in segments
+# one wavefront, four and eight; blocks and turns cut short; few columns in segments
 SHAPES = [(1, 1, 1), (2, 1, 5), (3, 2, 7), (1, 15, 3), (2, 16, 64), (2, 17, 65), (1, 63, 10), (4, 64, 16), (2, 65, 33), (1, 255, 64),
           (1, 256, 64), (2, 257, 40), (3, 300, 130), (1, 1000, 64), (1, 4097, 5), (2, 5000, 9), (5, 700, 200), (300, 40, 70)]
 
@@ -333,7 +333,10 @@ def test_gates_that_keep_and_forget_all(need_gpu, name):
     z[:, 280:] = 1e4
     check_case(name, x, z, initial, None, g, g_last)
     h, *_ = Q.gated_scan_forward(x, z, initial)
-    assert torch.equal(h[:, 150, :8], h[:, 100, :8]) and torch.equal(h[:, 220:230], x[:, 220:230])
+    # bit by bit inside a block of 16 steps, which runs step by step; the state before
+    # a later block comes from the maps of the ones before it, rounded otherwise: the
+    # bounds above hold it
+    assert torch.equal(h[:, 111, :8], h[:, 100, :8]) and torch.equal(h[:, 220:230], x[:, 220:230])
 
 
 @gpu
