@@ -7,8 +7,8 @@
 //
 // The gradient's sums run in the order of the tokens' places, whatever the
 // grid: places are sorted by token (a stable radix sort), and a wavefront sums the
-// rows of a chunk of sorted places, token by token. A token whose rows lie in one
-// chunk is done there; of one that goes on in the next chunk the parts are joined
+// rows of a chunk of sorted places, token by token. A token whose rows end in the
+// chunk or the next is done there; of one that goes on further the parts are joined
 // in a second launch. Rows without tokens are zeros, written beside the sort. HBM
 // bounds large calls (N rows of g read, the table written), launches the others.
 #include <algorithm>
@@ -57,15 +57,16 @@ __device__ __forceinline__ uint32_t key_at(const EmbedArgs& a, int64_t i) {
     return t < 0 || t >= a.rows || (a.padded && t == a.padding) ? (uint32_t)a.rows : (uint32_t)t;
 }
 
-// Zeros for the whole table: the share of workgroup `part` of `parts`.
+// Zeros for the whole table: share `part` of `parts`.
 template <typename T> __device__ void clear_table(const EmbedArgs& a, int64_t part, int64_t parts) {
     constexpr int V = VEC<T>;
-    const int64_t n = a.rows * a.D, vectors = n / V;
+    const int64_t n = a.rows * a.D, vectors = n / V, each = (vectors + parts - 1) / parts;
+    const int64_t end = min(vectors, (part + 1) * each);
     T* out = (T*)a.grad_weight;
     Vec<T, V> zero;
 #pragma unroll
     for (int e = 0; e < V; e++) zero.v[e] = down<T>((Acc<T>)0);
-    for (int64_t i = part * blockDim.x + threadIdx.x; i < vectors; i += parts * blockDim.x) store_vec<T, V>(out + i * V, zero);
+    for (int64_t i = part * each + threadIdx.x; i < end; i += blockDim.x) store_vec<T, V>(out + i * V, zero);
     if (part == 0 && threadIdx.x < n % V) out[vectors * V + threadIdx.x] = zero.v[0];
 }
 
@@ -139,17 +140,15 @@ template <typename T> __global__ __launch_bounds__(1024) void k_embed_sort_small
             rank[j] = rank_of((k[j] >> shift) & ((1u << width) - 1), width, i < n, counts[wave]);
         }
         __syncthreads();
-        // thread d: digit d's elements before each wavefront's, then before the digit
-        uint32_t total = 0;
+        // thread d: digit d's elements before each wavefront's
+        uint32_t c[16] = {}, total = 0;
         if (threadIdx.x < 256)
-            for (int w = 0; w < 16; w++) {
-                const uint32_t c = counts[w][threadIdx.x];
-                counts[w][threadIdx.x] = total;
-                total += c;
-            }
-        const uint32_t base = sum_before<1024>(total, sums);
+#pragma unroll
+            for (int w = 0; w < 16; w++) c[w] = counts[w][threadIdx.x], total += c[w];
+        uint32_t to = sum_before<1024>(total, sums);
         if (threadIdx.x < 256)
-            for (int w = 0; w < 16; w++) counts[w][threadIdx.x] += base;
+#pragma unroll
+            for (int w = 0; w < 16; w++) counts[w][threadIdx.x] = to, to += c[w];
         __syncthreads();
 #pragma unroll
         for (int j = 0; j < ITEMS; j++) {
@@ -165,10 +164,11 @@ template <typename T> __global__ __launch_bounds__(1024) void k_embed_sort_small
     for (int i = threadIdx.x; i < n; i += 1024) keys[i] = key[i], places[i] = place[i];
 }
 
-// More: digits of up to 10 bits, each in three launches over tiles of 2048
+// More: digits of up to 10 bits, each in three launches over tiles of 1024
 // places: the tiles' counts of the digit's values, their sums over the tiles before,
-// and the move. Pass 0 reads the tokens.
-constexpr int TILE = 2048, MOST_VALUES = 1024;
+// and the move. Pass 0 reads the tokens. The launches are too short to fill the chip:
+// further workgroups of theirs clear the table, a share in each launch.
+constexpr int TILE = 1024, MOST_VALUES = 1024;
 
 struct SortPass {
     const uint32_t *keys, *places;  // null: the tokens
@@ -177,11 +177,12 @@ struct SortPass {
     uint32_t* totals;  // [values]
     int shift, width;
     int64_t tiles;
+    int64_t clear_first, clear_parts;  // shares of the table that this launch begins with, of all
 };
 
-template <typename T> __global__ __launch_bounds__(256) void k_embed_count(EmbedArgs a, SortPass p, int64_t clearing) {
+template <typename T> __global__ __launch_bounds__(256) void k_embed_count(EmbedArgs a, SortPass p) {
     if (blockIdx.x >= p.tiles) {
-        clear_table<T>(a, blockIdx.x - p.tiles, clearing);
+        clear_table<T>(a, p.clear_first + blockIdx.x - p.tiles, p.clear_parts);
         return;
     }
     __shared__ uint32_t counts[MOST_VALUES];
@@ -221,13 +222,26 @@ __global__ __launch_bounds__(1024) void k_embed_sum_tiles(SortPass p) {
     }
 }
 
-__global__ __launch_bounds__(256) void k_embed_move(EmbedArgs a, SortPass p) {
+template <typename T> __global__ __launch_bounds__(256) void k_embed_move(EmbedArgs a, SortPass p) {
+    if (blockIdx.x >= p.tiles) {
+        clear_table<T>(a, p.clear_first + blockIdx.x - p.tiles, p.clear_parts);
+        return;
+    }
     constexpr int ITEMS = TILE / 256, EACH = MOST_VALUES / 256;
     __shared__ uint32_t counts[4][MOST_VALUES];
     __shared__ uint32_t base[MOST_VALUES];
     __shared__ uint32_t sums[4];
     const int values = 1 << p.width, wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-    for (int i = threadIdx.x; i < 4 * MOST_VALUES; i += 256) counts[i / MOST_VALUES][i % MOST_VALUES] = 0;
+    const int64_t first = (int64_t)blockIdx.x * TILE + wave * (TILE / 4);
+    uint32_t key[ITEMS], place[ITEMS], rank[ITEMS];
+#pragma unroll
+    for (int j = 0; j < ITEMS; j++) {
+        const int64_t i = first + j * 64 + lane;
+        key[j] = i < a.n ? p.keys ? p.keys[i] : key_at(a, i) : 0;
+        place[j] = i < a.n && p.places ? p.places[i] : (uint32_t)i;
+    }
+    for (int w = 0; w < 4; w++)
+        for (int v = threadIdx.x; v < values; v += 256) counts[w][v] = 0;
     // thread t: values EACH t ... EACH t + EACH - 1
     uint32_t total[EACH], sum = 0;
 #pragma unroll
@@ -244,14 +258,6 @@ __global__ __launch_bounds__(256) void k_embed_move(EmbedArgs a, SortPass p) {
         before += total[e];
     }
     __syncthreads();
-    const int64_t first = (int64_t)blockIdx.x * TILE + wave * (TILE / 4);
-    uint32_t key[ITEMS], place[ITEMS], rank[ITEMS];
-#pragma unroll
-    for (int j = 0; j < ITEMS; j++) {
-        const int64_t i = first + j * 64 + lane;
-        key[j] = i < a.n ? p.keys ? p.keys[i] : key_at(a, i) : 0;
-        place[j] = i < a.n && p.places ? p.places[i] : (uint32_t)i;
-    }
 #pragma unroll
     for (int j = 0; j < ITEMS; j++)
         rank[j] = rank_of((key[j] >> p.shift) & (values - 1), p.width, first + j * 64 + lane < a.n, counts[wave]);
@@ -277,38 +283,73 @@ __global__ __launch_bounds__(256) void k_embed_move(EmbedArgs a, SortPass p) {
 // ---------------------------------------------------------------------------
 // The sums.
 
-// Places of a chunk, whose rows one group of lanes sums.
-constexpr int CHUNK = 64;
+// Places of a chunk, whose rows one group of lanes sums: 64 where that is enough of
+// them, down to 8 for the few tokens of a small call (4096 of 1000x64 float32: 14 us of
+// sums in 64 chunks, 7 in 512). It goes by the number of tokens alone, and so
+// do the bits of a sum.
+constexpr int CHUNK = 64, AHEAD = 8;
+int chunk_of(int64_t n) { return (int)std::max<int64_t>(AHEAD, std::min<int64_t>(CHUNK, n / 2048 / AHEAD * AHEAD)); }
 
 struct Sums {
     const uint32_t *keys, *places;
     void* parts;  // [chunks][2][D]: of the token that goes on from the chunk before, and on to the next
     int64_t chunks;
+    int chunk;
 };
 
-// A group of G lanes takes a chunk's rows in a tile of G V columns.
+// Whether the token at place i has the whole chunk of places from `first` on.
+__device__ __forceinline__ bool fills(const Sums& q, int64_t n, uint32_t key, int64_t first) {
+    return first + q.chunk <= n && q.keys[first] == key && q.keys[first + q.chunk - 1] == key;
+}
+
+// A group of G lanes takes the tokens that begin in a chunk, in a tile of G V columns. One
+// that goes on past the chunk is finished here too, unless it fills the next chunk:
+// then every chunk that it reaches leaves its part for k_embed_join. Eight
+// rows are under way while eight are summed, and the lanes hold the keys and places of
+// a chunk between them. 131072 rows of 1024 bfloat16 for 50000 tokens take 97 us: 345 MB
+// of rows in any order at 3.6 TB/s, whether a wavefront has 4, 8 or 16 KB under way.
 template <typename T, int V, int G> __global__ __launch_bounds__(256) void k_embed_sums(EmbedArgs a, Sums q) {
     using R = Acc<T>;
-    constexpr int GROUPS = 256 / G, AHEAD = 8;
+    constexpr int GROUPS = 256 / G, HELD = CHUNK / G;
     const int lane = threadIdx.x % G, D = (int)a.D;
-    const int c = (blockIdx.y * G + lane) * V;
-    if (c >= D) return;
-    const int at = min(c, D - V);
-    const T* g = (const T*)a.grad + at;
     const R scale = (R)a.scale;
     const uint32_t none = (uint32_t)a.rows;
-    for (int64_t chunk = (int64_t)blockIdx.x * GROUPS + threadIdx.x / G; chunk < q.chunks; chunk += (int64_t)gridDim.x * GROUPS) {
-        const int64_t lo = chunk * CHUNK, hi = min(lo + CHUNK, a.n);
+    const int tiles = (D + G * V - 1) / (G * V);
+    const int group = G == 64 ? __builtin_amdgcn_readfirstlane(threadIdx.x / 64) : threadIdx.x / G;
+    for (int64_t w = (int64_t)blockIdx.x * GROUPS + group; w < q.chunks * tiles; w += (int64_t)gridDim.x * GROUPS) {
+        // a chunk's tiles side by side: they read the same rows
+        const int64_t chunk = w / tiles, lo = chunk * q.chunk, hi = min(lo + q.chunk, a.n);
+        const int c = ((int)(w % tiles) * G + lane) * V, at = max(0, min(c, D - V));
+        const T* g = (const T*)a.grad + at;
+        uint32_t keys[HELD], places[HELD];
+        auto hold = [&](int64_t first, int count) {
+#pragma unroll
+            for (int h = 0; h < HELD; h++) {
+                const int64_t k = first + min(h * G + lane, count - 1);
+                keys[h] = q.keys[k], places[h] = q.places[k];
+            }
+        };
+        auto held = [&](const uint32_t (&v)[HELD], int i) {  // place i's, in all lanes of the group
+            if constexpr (G == 64) {
+                return (uint32_t)__builtin_amdgcn_readlane(v[0], i);
+            } else {
+                uint32_t r = v[0];
+#pragma unroll
+                for (int h = 1; h < HELD; h++) r = i / G == h ? v[h] : r;
+                return (uint32_t)__shfl((int)r, i % G, G);
+            }
+        };
         R sum[V] = {};
-        uint32_t current = q.keys[lo];
-        bool from_before = lo > 0 && q.keys[lo - 1] == current;
-        auto finish = [&](bool goes_on) {
-            if (current == none) return;
-            if (from_before || goes_on) {
+        uint32_t current = none;
+        // where the sum of the current token goes: 0 the table, 1 or 2 the chunk's first or second part, 3 nowhere
+        int to = 3;
+        auto finish = [&] {
+            if (current == none || to == 3 || c >= D) return;
+            if (to) {
                 Vec<R, V> r;
 #pragma unroll
                 for (int e = 0; e < V; e++) r.v[e] = sum[e];
-                store_vec<R, V>((R*)q.parts + (2 * chunk + (from_before ? 0 : 1)) * a.D + at, r);
+                store_vec<R, V>((R*)q.parts + (2 * chunk + to - 1) * a.D + at, r);
             } else {
                 Vec<T, V> r;
 #pragma unroll
@@ -316,47 +357,83 @@ template <typename T, int V, int G> __global__ __launch_bounds__(256) void k_emb
                 store_vec<T, V>((T*)a.grad_weight + (int64_t)current * a.D + at, r);
             }
         };
-        for (int64_t i = lo; i < hi; i += AHEAD) {
-            uint32_t key[AHEAD];
-            Vec<T, V> row[AHEAD];
+        // adds the rows of places [skip, count) that are held, up to the first key that `stops`
+        auto add = [&](int skip, int count, auto stops) {
+            Vec<T, V> next[AHEAD];
+            auto fetch = [&](int i) {
 #pragma unroll
-            for (int j = 0; j < AHEAD; j++) key[j] = q.keys[min(i + j, hi - 1)];
-            if (key[0] == none) break;  // and so are all that follow
+                for (int j = 0; j < AHEAD; j++)
+                    next[j] = load_vec<T, V>(g + (int64_t)held(places, min(i + j, count - 1)) * a.grad_stride);
+            };
+            fetch(skip);
+            for (int i = skip; i < count && !stops(held(keys, i)); i += AHEAD) {
+                Vec<T, V> row[AHEAD];
 #pragma unroll
-            for (int j = 0; j < AHEAD; j++)
-                row[j] = load_vec<T, V>(g + (int64_t)q.places[min(i + j, hi - 1)] * a.grad_stride);
+                for (int j = 0; j < AHEAD; j++) row[j] = next[j];
+                if (i + AHEAD < count) fetch(i + AHEAD);
 #pragma unroll
-            for (int j = 0; j < AHEAD; j++) {
-                if (i + j >= hi) break;
-                if (key[j] != current) {
-                    finish(false);
-                    current = key[j], from_before = false;
+                for (int j = 0; j < AHEAD; j++) {
+                    const uint32_t key = held(keys, min(i + j, count - 1));
+                    if (i + j >= count || stops(key)) break;
+                    if (key != current) {
+                        finish();
+                        current = key, to = 0;
 #pragma unroll
-                    for (int e = 0; e < V; e++) sum[e] = 0;
+                        for (int e = 0; e < V; e++) sum[e] = 0;
+                    }
+#pragma unroll
+                    for (int e = 0; e < V; e++) sum[e] += up(row[j].v[e]);
                 }
+            }
+        };
+        const int count = (int)(hi - lo);
+        hold(lo, count);
+        const uint32_t first = held(keys, 0), last = held(keys, count - 1);
+        if (first == none) continue;
+        int skip = 0;
+        if (lo > 0 && q.keys[lo - 1] == first) {
+            // one that began before: it leaves a part if it fills this chunk, or filled
+            // the chunk before and began before that; else the chunk where it began adds it
+            const bool part = fills(q, a.n, first, lo) || (lo > q.chunk && q.keys[lo - q.chunk - 1] == first);
+            current = first, to = part ? 1 : 3;
+            if (!part) {
 #pragma unroll
-                for (int e = 0; e < V; e++) sum[e] += up(row[j].v[e]);
+                for (int h = 0; h < HELD; h++) {
+                    const uint64_t same = __ballot(keys[h] == first && h * G + lane < count);
+                    skip += __popcll(G == 64 ? same : (same >> (threadIdx.x % 64 / G * G)) & ((1ull << (G % 64)) - 1));
+                }
+            }
+            if (skip == count) continue;
+        }
+        add(skip, count, [&](uint32_t key) { return key == none; });
+        if (hi < a.n && last != none && current == last && to == 0 && q.keys[hi] == last) {
+            if (fills(q, a.n, last, hi)) {
+                to = 2;
+            } else {
+                const int more = (int)min((int64_t)q.chunk, a.n - hi);
+                hold(hi, more);
+                add(0, more, [&](uint32_t key) { return key != last; });
             }
         }
-        finish(hi < a.n && q.keys[hi] == current);
+        finish();
     }
 }
 
-// The parts of a token that begins in a chunk and goes on past it, in fp64: the
-// workgroup's wavefronts take every eighth and meet in LDS.
-template <typename T, int V> __global__ __launch_bounds__(512) void k_embed_join(EmbedArgs a, Sums q) {
+// The parts of a token that begins in a chunk and fills the next, in fp64: the
+// workgroup's wavefronts take every fourth and meet in LDS.
+template <typename T, int V> __global__ __launch_bounds__(256) void k_embed_join(EmbedArgs a, Sums q) {
     using R = Acc<T>;
-    __shared__ double lds[8][64 * V];
+    __shared__ double lds[4][64 * V];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, D = (int)a.D;
     for (int64_t chunk = blockIdx.x; chunk < q.chunks - 1; chunk += gridDim.x) {
-        const int64_t lo = chunk * CHUNK, hi = lo + CHUNK;
+        const int64_t lo = chunk * q.chunk, hi = lo + q.chunk;
         const uint32_t key = q.keys[hi - 1];
-        if (key == (uint32_t)a.rows || q.keys[hi] != key || (lo > 0 && q.keys[lo] == key && q.keys[lo - 1] == key)) continue;
+        if (key == (uint32_t)a.rows || !fills(q, a.n, key, hi) || (lo > 0 && q.keys[lo] == key && q.keys[lo - 1] == key)) continue;
         // the last chunk that begins with the token
         int64_t last = chunk + 1;
         for (;;) {
             const int64_t j = last + 1 + lane;
-            const uint64_t other = ~__ballot(j < q.chunks && q.keys[min(j, q.chunks - 1) * CHUNK] == key);
+            const uint64_t other = ~__ballot(j < q.chunks && q.keys[min(j, q.chunks - 1) * q.chunk] == key);
             const int alike = other ? __ffsll((unsigned long long)other) - 1 : 64;
             last += alike;
             if (alike < 64) break;
@@ -364,11 +441,18 @@ template <typename T, int V> __global__ __launch_bounds__(512) void k_embed_join
         const int c = (blockIdx.y * 64 + lane) * V, at = max(0, min(c, D - V));
         double sum[V] = {};
         const R* parts = (const R*)q.parts + at;
-#pragma unroll 4
-        for (int64_t j = chunk + wave; j <= last; j += 8) {
-            const Vec<R, V> r = load_vec<R, V>(parts + (2 * j + (j == chunk ? 1 : 0)) * a.D);
+        for (int64_t j0 = chunk + wave; j0 <= last; j0 += 4 * AHEAD) {
+            Vec<R, V> r[AHEAD];
 #pragma unroll
-            for (int e = 0; e < V; e++) sum[e] += (double)r.v[e];
+            for (int i = 0; i < AHEAD; i++) {
+                const int64_t j = min(j0 + 4 * i, last);
+                r[i] = load_vec<R, V>(parts + (2 * j + (j == chunk ? 1 : 0)) * a.D);
+            }
+#pragma unroll
+            for (int i = 0; i < AHEAD; i++)
+                if (j0 + 4 * i <= last)
+#pragma unroll
+                    for (int e = 0; e < V; e++) sum[e] += (double)r[i].v[e];
         }
 #pragma unroll
         for (int e = 0; e < V; e++) lds[wave][lane * V + e] = sum[e];
@@ -379,7 +463,7 @@ template <typename T, int V> __global__ __launch_bounds__(512) void k_embed_join
             for (int e = 0; e < V; e++) {
                 double t = 0;
 #pragma unroll
-                for (int w = 0; w < 8; w++) t += lds[w][lane * V + e];
+                for (int w = 0; w < 4; w++) t += lds[w][lane * V + e];
                 out.v[e] = down<T>((R)(t * a.scale));
             }
             store_vec<T, V>((T*)a.grad_weight + (int64_t)key * a.D + at, out);
@@ -395,7 +479,7 @@ int bits_of(int64_t rows) { return 64 - __builtin_clzll((unsigned long long)rows
 struct Layout {
     size_t keys[2], places[2], counts, totals, parts, bytes;
     int64_t tiles, chunks;
-    int bits, passes, width;
+    int bits, passes, width, chunk;
 };
 Layout layout_of(int type, int64_t n, int64_t rows, int64_t D) {
     Layout l{};
@@ -405,7 +489,7 @@ Layout layout_of(int type, int64_t n, int64_t rows, int64_t D) {
         return at;
     };
     l.bits = bits_of(rows);
-    l.chunks = (n + CHUNK - 1) / CHUNK;
+    l.chunk = chunk_of(n), l.chunks = (n + l.chunk - 1) / l.chunk;
     const bool small = n <= SMALL;
     for (int k = 0; k < (small ? 1 : 2); k++) l.keys[k] = take((size_t)n * 4), l.places[k] = take((size_t)n * 4);
     if (!small) {
@@ -419,13 +503,13 @@ Layout layout_of(int type, int64_t n, int64_t rows, int64_t D) {
     return l;
 }
 
-// Workgroups of 512 threads: 2^22 of them stay below a launch's 2^32 threads.
+// Workgroups of 256 threads: 2^22 of them stay below a launch's 2^32 threads.
 unsigned grid_x(int64_t groups, int64_t y) { return (unsigned)std::max<int64_t>(1, std::min<int64_t>(groups, ((int64_t)1 << 22) / y)); }
 
 template <typename T, int V, int G> void sums(const EmbedArgs& a, const Sums& q, hipStream_t s) {
     const int64_t tiles = (a.D + G * V - 1) / (G * V), wide = (a.D + 64 * V - 1) / (64 * V);
-    k_embed_sums<T, V, G><<<dim3(grid_x((q.chunks * G + 255) / 256, tiles), (unsigned)tiles), 256, 0, s>>>(a, q);
-    if (q.chunks > 1) k_embed_join<T, V><<<dim3(grid_x(q.chunks - 1, wide), (unsigned)wide), 512, 0, s>>>(a, q);
+    k_embed_sums<T, V, G><<<grid_x((q.chunks * tiles * G + 255) / 256, 1), 256, 0, s>>>(a, q);
+    if (q.chunks > 1) k_embed_join<T, V><<<dim3(grid_x(q.chunks - 1, wide), (unsigned)wide), 256, 0, s>>>(a, q);
 }
 
 template <typename T> hipError_t backward(int type, const EmbedArgs& a, void* ws, hipStream_t s) {
@@ -446,14 +530,16 @@ template <typename T> hipError_t backward(int type, const EmbedArgs& a, void* ws
             p.to_keys = keys[at], p.to_places = places[at];
             p.counts = (uint32_t*)(base + l.counts), p.totals = (uint32_t*)(base + l.totals);
             p.shift = k * l.width, p.width = std::min(l.width, l.bits - p.shift), p.tiles = l.tiles;
-            const int64_t more = k == 0 ? clearing : 0;
-            k_embed_count<T><<<(unsigned)(l.tiles + more), 256, 0, s>>>(a, p, more);
+            const int64_t share = (clearing + 2 * l.passes - 1) / (2 * l.passes);
+            p.clear_parts = share * 2 * l.passes, p.clear_first = share * 2 * k;
+            k_embed_count<T><<<(unsigned)(l.tiles + share), 256, 0, s>>>(a, p);
             k_embed_sum_tiles<<<((1 << p.width) + 15) / 16, 1024, 0, s>>>(p);
-            k_embed_move<<<(unsigned)l.tiles, 256, 0, s>>>(a, p);
+            p.clear_first += share;
+            k_embed_move<T><<<(unsigned)(l.tiles + share), 256, 0, s>>>(a, p);
         }
         at ^= 1;
     }
-    const Sums q{keys[at], places[at], base + l.parts, l.chunks};
+    const Sums q{keys[at], places[at], base + l.parts, l.chunks, l.chunk};
     if (a.D < VEC<T>) sums<T, 1, 16>(a, q, s);
     else if (a.D <= 16 * VEC<T>) sums<T, VEC<T>, 16>(a, q, s);
     else sums<T, VEC<T>, 64>(a, q, s);

@@ -2,8 +2,8 @@
 (needs an MI355X).
 
 A row is one product and one rounding: off by u and half a step. A gradient sums
-at most 64 rows in the arithmetic's unit roundoff u (24 bits: 2^-24), then the sums of such
-chunks in fp64: off by (64 + 3) u of the sum of magnitudes, and half a step.
+at most two chunks of 64 rows in the arithmetic's unit roundoff u (24 bits: 2^-24), or the
+sums of chunks in fp64: off by (128 + 3) u of the sum of magnitudes, and half a step.
 """
 
 from __future__ import annotations
@@ -70,7 +70,8 @@ def test_workspace_bytes(lib):
     for n in (0, 1, 64, 65, 4096, 4097, 1 << 20, (1 << 31) - 1):
         for rows in (1, 255, 1 << 20, (1 << 31) - 1):
             assert lib.ql_embedding_workspace_bytes(BF16, n, rows, 16, ctypes.byref(out)) == 0
-            assert 8 * n <= out.value <= 16 * n + (n // 64 + 1) * 2 * 16 * 4 + (n // 2048 + 2) * 4096 + 4096
+            chunk = max(8, min(64, n // 2048 // 8 * 8))
+            assert 8 * n <= out.value <= 16 * n + (n // chunk + 1) * 2 * 16 * 4 + (n // 1024 + 2) * 4096 + 4096
 
 
 def test_no_tokens(lib):
@@ -124,7 +125,7 @@ def check(t, w, grad, name, scale=1.0, padding=None):
     at, kept = t.long()[keep].cpu(), grad.double()[keep].cpu()
     total = torch.zeros(rows, d, dtype=torch.float64).index_add_(0, at, kept).cuda()
     size = torch.zeros(rows, d, dtype=torch.float64).index_add_(0, at, kept.abs()).cuda()
-    bound = (size * 67 * u + total.abs() * out) * abs(scale) + tiny
+    bound = (size * 131 * u + total.abs() * out) * abs(scale) + tiny
     if name == "f64":  # the order of the reference's own sums counts too
         bound += size * abs(scale) * 2.0 ** -53 * (8 + torch.bincount(t.long()[keep], minlength=rows).max().item())
     assert got.dtype == grad.dtype and got.shape == (rows, d)
@@ -173,7 +174,7 @@ def test_tokens_outside_the_table(need_gpu, n):
     got = Q.embedding_backward(g, t, 40)
     # the same sums but for zeros among them, whose chunks may end elsewhere
     size = torch.zeros_like(total).index_add_(0, t[inside], g[inside].abs())
-    assert ((got - total).abs() <= size * 140 * 2.0 ** -24).all()
+    assert ((got - total).abs() <= size * 262 * 2.0 ** -24).all()
     y = Q.embedding_forward(t, w, padding=-1)
     assert not y[at[0]].any() and torch.isnan(y[at[1:]]).all()
     assert torch.equal(Q.embedding_backward(g, t, 40, padding=-1), got)
