@@ -25,27 +25,42 @@ __device__ __forceinline__ int64_t token_at(const EmbedArgs& a, int64_t i) {
     return a.wide ? ((const int64_t*)a.tokens)[i] : (int64_t)((const int32_t*)a.tokens)[i];
 }
 
-// A group of G lanes copies token after token's row.
-template <typename T, int V, int G> __global__ __launch_bounds__(256) void k_embed_fwd(EmbedArgs a) {
+// A group of G lanes copies K vectors a lane of token after token's row (a tile of
+// it where it is longer): the next row's loads and the token behind it are under way
+// while a row is written.
+template <typename T, int V, int G, int K> __global__ __launch_bounds__(256) void k_embed_fwd(EmbedArgs a) {
     using R = Acc<T>;
-    constexpr int ROWS = 256 / G;
-    const int lane = threadIdx.x % G, D = (int)a.D;
+    constexpr int GROUPS = 256 / G;
+    const int lane = threadIdx.x % G, D = (int)a.D, tiles = (D + G * V * K - 1) / (G * V * K);
     const R scale = (R)a.scale;
-    for (int64_t i = (int64_t)blockIdx.x * ROWS + threadIdx.x / G; i < a.n; i += (int64_t)gridDim.x * ROWS) {
-        const int64_t t = token_at(a, i);
+    const int64_t stride = (int64_t)gridDim.x * GROUPS, count = a.n * tiles;
+    int64_t w = (int64_t)blockIdx.x * GROUPS + threadIdx.x / G;
+    if (w >= count) return;
+    auto token = [&](int64_t w) { return token_at(a, min(w, count - 1) / tiles); };
+    auto column = [&](int64_t w, int k) { return min(((int)(w % tiles) * G * K + k * G + lane) * V, D - V); };
+    Vec<T, V> next[K];
+    auto fetch = [&](int64_t w, int64_t t) {
+        const T* src = (const T*)a.weight + (t >= 0 && t < a.rows ? t : 0) * a.weight_stride;
+#pragma unroll
+        for (int k = 0; k < K; k++) next[k] = load_vec<T, V>(src + column(w, k));
+    };
+    int64_t t = token(w), ahead = token(w + stride);
+    fetch(w, t);
+    for (; w < count; w += stride) {
+        Vec<T, V> v[K];
+#pragma unroll
+        for (int k = 0; k < K; k++) v[k] = next[k];
+        if (w + stride < count) fetch(w + stride, ahead);
         const bool pad = a.padded && t == a.padding, in = t >= 0 && t < a.rows;
-        const T* src = (const T*)a.weight + (in ? t : 0) * a.weight_stride;
-        T* dst = (T*)a.y + i * a.D;
-#pragma unroll 2
-        for (int c = lane * V; c < D; c += G * V) {
-            const int at = min(c, D - V);
-            Vec<T, V> v;
-            if (in && !pad) v = load_vec<T, V>(src + at);
+        T* dst = (T*)a.y + w / tiles * a.D;
+#pragma unroll
+        for (int k = 0; k < K; k++) {
 #pragma unroll
             for (int e = 0; e < V; e++)
-                v.v[e] = down<T>(pad ? (R)0 : in ? up(v.v[e]) * scale : (R)__builtin_nanf(""));
-            store_vec<T, V>(dst + at, v);
+                v[k].v[e] = down<T>(pad ? (R)0 : in ? up(v[k].v[e]) * scale : (R)__builtin_nanf(""));
+            store_vec<T, V>(dst + column(w, k), v[k]);
         }
+        t = ahead, ahead = token(w + 2 * stride);
     }
 }
 
@@ -546,18 +561,19 @@ template <typename T> hipError_t backward(int type, const EmbedArgs& a, void* ws
     return hipGetLastError();
 }
 
-template <typename T, int V, int G> hipError_t rows_of(const EmbedArgs& a, hipStream_t s) {
-    constexpr int ROWS = 256 / G;
-    k_embed_fwd<T, V, G><<<(unsigned)std::min<int64_t>((a.n + ROWS - 1) / ROWS, 1 << 20), 256, 0, s>>>(a);
+template <typename T, int V, int G, int K> hipError_t rows_of(const EmbedArgs& a, hipStream_t s) {
+    constexpr int GROUPS = 256 / G;
+    const int64_t count = a.n * ((a.D + G * V * K - 1) / (G * V * K));
+    k_embed_fwd<T, V, G, K><<<(unsigned)std::min<int64_t>((count + GROUPS - 1) / GROUPS, 4096), 256, 0, s>>>(a);
     return hipGetLastError();
 }
 
 template <typename T> hipError_t forward(const EmbedArgs& a, hipStream_t s) {
     constexpr int V = VEC<T>;
-    if (a.D < V) return rows_of<T, 1, 16>(a, s);
-    if (a.D <= 16 * V) return rows_of<T, V, 16>(a, s);
-    if (a.D <= 128 * V) return rows_of<T, V, 64>(a, s);
-    return rows_of<T, V, 256>(a, s);
+    if (a.D < V) return rows_of<T, 1, 16, 1>(a, s);
+    if (a.D <= 16 * V) return rows_of<T, V, 16, 1>(a, s);
+    if (a.D <= 64 * V) return rows_of<T, V, 64, 1>(a, s);
+    return rows_of<T, V, 64, 2>(a, s);
 }
 
 template <typename F> hipError_t by_type(int type, F f) {

@@ -90,7 +90,7 @@ def test_workspace_bytes(lib):
     out = ctypes.c_size_t()
     assert lib.ql_gated_scan_workspace_bytes(F32, 1, 8, 1, None) == -1
     assert lib.ql_gated_scan_workspace_bytes(F32, 1, -8, 1, ctypes.byref(out)) == -1
-    for steps in (0, 1, 16, 256):
+    for steps in (0, 1, 16, 128):
         assert lib.ql_gated_scan_workspace_bytes(F32, 3, steps, 100, ctypes.byref(out)) == 0 and out.value == 0
     assert lib.ql_gated_scan_workspace_bytes(F32, 1, 65536, 64, ctypes.byref(out)) == 0 and out.value > 0
     assert lib.ql_gated_scan_workspace_bytes(F32, 1, 1 << 30, 64, ctypes.byref(out)) == 0 and out.value <= 4096 * 2 * 64 * 4
@@ -521,3 +521,19 @@ def test_offsets_past_32_bits(need_gpu):
     near(last[..., at], ref.last, ref.dlast, "last")
     near(gx[..., at], ref.gx, ref.dgx, "grad_x")
     near(gz[..., at], ref.gz, ref.dgz, "grad_gate")
+
+
+@gpu
+@pytest.mark.parametrize("steps", [10, 60, 400])
+def test_sequences_gigabytes_apart(need_gpu, steps):
+    """Their columns lie further from a workgroup's first than 32 bits of bytes: the same bits."""
+    x, z, initial, starts, g, g_last = make(2, steps, 10, torch.bfloat16, seed=3)
+    far = torch.empty((1 << 32) + 20 * steps, dtype=torch.bfloat16, device="cuda")
+    both = far.as_strided((2, steps, 20), (1 << 32, 20, 1))
+    both[..., :10], both[..., 10:] = x, z
+
+    def run(x, z):
+        h, last, states = Q.gated_scan_forward(x, z, initial, starts)
+        return (h, last, *Q.gated_scan_backward(g, x, z, states, starts, g_last))
+
+    assert all(torch.equal(p, q) for p, q in zip(run(both[..., :10], both[..., 10:]), run(x, z)))
