@@ -124,59 +124,45 @@ template <int T> __device__ __forceinline__ uint32_t sum_before(uint32_t v, uint
     return base + s - v;
 }
 
-// Up to 4096 places: sorted in the LDS of workgroup 0, in digits of 8 bits,
-// while the others clear the table.
-constexpr int SMALL = 4096;
+// Up to 8192 places: one launch, in which every place counts what comes before it (16
+// lanes a place, all keys in each workgroup's LDS), while further workgroups clear the
+// table. 4096 places take 9.1 us (10.5 by digits in one workgroup's LDS); the work
+// goes with the square of their number, and at 16384 would take what the launches below do.
+constexpr int SMALL = 8192;
 
-template <typename T> __global__ __launch_bounds__(1024) void k_embed_sort_small(EmbedArgs a, int bits, uint32_t* keys, uint32_t* places) {
-    if (blockIdx.x > 0) {
-        clear_table<T>(a, blockIdx.x - 1, gridDim.x - 1);
+template <typename T>
+__global__ __launch_bounds__(256) void k_embed_rank(EmbedArgs a, int ranking, uint32_t* keys, uint32_t* places) {
+    if ((int)blockIdx.x >= ranking) {
+        clear_table<T>(a, blockIdx.x - ranking, gridDim.x - ranking);
         return;
     }
-    constexpr int ITEMS = SMALL / 1024;
-    __shared__ uint32_t key[SMALL];
-    __shared__ uint16_t place[SMALL];
-    __shared__ uint32_t counts[16][256];
-    __shared__ uint32_t sums[16];
-    const int n = (int)a.n, wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-    const int items = (n + 1023) / 1024;
-    for (int i = threadIdx.x; i < n; i += 1024) key[i] = key_at(a, i), place[i] = (uint16_t)i;
-    for (int shift = 0; shift < bits; shift += 8) {
-        const int width = min(8, bits - shift);
-        for (int i = threadIdx.x; i < 16 * 256; i += 1024) counts[i / 256][i % 256] = 0;
-        __syncthreads();
-        uint32_t k[ITEMS], rank[ITEMS];
-        uint16_t from[ITEMS];
+    __shared__ uint4 key4[SMALL / 4];
+    uint32_t* key = (uint32_t*)key4;
+    const int n = (int)a.n, padded = (n + 63) / 64 * 64;
+    for (int i0 = threadIdx.x; i0 < padded; i0 += 256 * 8) {
+        uint32_t k[8];
 #pragma unroll
-        for (int j = 0; j < ITEMS; j++) {
-            const int i = (wave * items + j) * 64 + lane;
-            if (j >= items) break;
-            k[j] = i < n ? key[i] : 0, from[j] = i < n ? place[i] : 0;
-            rank[j] = rank_of((k[j] >> shift) & ((1u << width) - 1), width, i < n, counts[wave]);
-        }
-        __syncthreads();
-        // thread d: digit d's elements before each wavefront's
-        uint32_t c[16] = {}, total = 0;
-        if (threadIdx.x < 256)
+        for (int e = 0; e < 8; e++) k[e] = key_at(a, min(i0 + 256 * e, n - 1));
 #pragma unroll
-            for (int w = 0; w < 16; w++) c[w] = counts[w][threadIdx.x], total += c[w];
-        uint32_t to = sum_before<1024>(total, sums);
-        if (threadIdx.x < 256)
-#pragma unroll
-            for (int w = 0; w < 16; w++) counts[w][threadIdx.x] = to, to += c[w];
-        __syncthreads();
-#pragma unroll
-        for (int j = 0; j < ITEMS; j++) {
-            const int i = (wave * items + j) * 64 + lane;
-            if (j >= items) break;
-            if (i < n) {
-                const uint32_t to = counts[wave][(k[j] >> shift) & ((1u << width) - 1)] + rank[j];
-                key[to] = k[j], place[to] = from[j];
-            }
-        }
-        __syncthreads();
+        for (int e = 0; e < 8; e++)
+            if (i0 + 256 * e < padded) key[i0 + 256 * e] = i0 + 256 * e < n ? k[e] : ~0u;  // after every key
     }
-    for (int i = threadIdx.x; i < n; i += 1024) keys[i] = key[i], places[i] = place[i];
+    __syncthreads();
+    const int i = blockIdx.x * 16 + threadIdx.x / 16, lane = threadIdx.x % 16;
+    const uint32_t own = key[min(i, n - 1)];
+    uint32_t before = 0;
+#pragma unroll 4
+    for (int j = lane * 4; j < padded; j += 64) {
+        const uint4 k = key4[j / 4];
+        // equal keys come in the order of their places
+        before += k.x < own + (j < i);
+        before += k.y < own + (j + 1 < i);
+        before += k.z < own + (j + 2 < i);
+        before += k.w < own + (j + 3 < i);
+    }
+#pragma unroll
+    for (int d = 1; d < 16; d *= 2) before += __shfl_xor((int)before, d, 16);
+    if (lane == 0 && i < n) keys[before] = own, places[before] = i;
 }
 
 // More: digits of up to 10 bits, each in three launches over tiles of 1024
@@ -536,7 +522,8 @@ template <typename T> hipError_t backward(int type, const EmbedArgs& a, void* ws
     const int64_t clearing = std::max<int64_t>(1, std::min<int64_t>(2048, a.rows * a.D * (int64_t)sizeof(T) >> 14));
     int at = 0;
     if (a.n <= SMALL) {
-        k_embed_sort_small<T><<<(unsigned)(1 + clearing), 1024, 0, s>>>(a, l.bits, keys[0], places[0]);
+        const int ranking = (int)(a.n + 15) / 16;
+        k_embed_rank<T><<<(unsigned)(ranking + clearing), 256, 0, s>>>(a, ranking, keys[0], places[0]);
         if (a.n == 0) return hipGetLastError();
     } else {
         for (int k = 0; k < l.passes; k++, at ^= 1) {

@@ -67,7 +67,7 @@ def test_workspace_bytes(lib):
     out = ctypes.c_size_t()
     assert lib.ql_embedding_workspace_bytes(F32, 4, 8, 1, None) == -1
     assert lib.ql_embedding_workspace_bytes(F32, -4, 8, 1, ctypes.byref(out)) == -1
-    for n in (0, 1, 64, 65, 4096, 4097, 1 << 20, (1 << 31) - 1):
+    for n in (0, 1, 64, 65, 8192, 8193, 1 << 20, (1 << 31) - 1):
         for rows in (1, 255, 1 << 20, (1 << 31) - 1):
             assert lib.ql_embedding_workspace_bytes(BF16, n, rows, 16, ctypes.byref(out)) == 0
             chunk = max(8, min(64, n // 2048 // 8 * 8))
@@ -146,7 +146,7 @@ def test_values(need_gpu, n, rows, d, name):
 @gpu
 @pytest.mark.parametrize("kind", ["even", "one", "few", "frequent"])
 @pytest.mark.parametrize("n,rows,d,name", [(4096, 50, 20, "f32"), (4097, 3, 12, "f32"), (5000, 200, 7, "f16"), (20001, 1500, 66, "bf16"),
-                                           (70000, 300000, 16, "f32"), (9000, 1 << 21, 4, "f64"), (140000, 1023, 130, "bf16"),
+                                           (70000, 300000, 16, "f32"), (8191, 40, 9, "f64"), (8192, 3000, 24, "bf16"), (8193, 700, 17, "f32"), (9000, 1 << 21, 4, "f64"), (140000, 1023, 130, "bf16"),
                                            (300000, 1024, 5, "f32")])
 def test_sorts_and_runs(need_gpu, n, rows, d, name, kind):
     """Both sorts, one to three digits, tokens of one place and of nearly all."""
@@ -155,7 +155,7 @@ def test_sorts_and_runs(need_gpu, n, rows, d, name, kind):
 
 
 @gpu
-@pytest.mark.parametrize("n", [60, 4096, 10000])
+@pytest.mark.parametrize("n", [60, 4096, 8192, 10000])
 def test_tokens_outside_the_table(need_gpu, n):
     """They have rows of NaN and no gradient; the padding may be one of them."""
     t, w, g = make(n, 40, 24, torch.float32, seed=n)
