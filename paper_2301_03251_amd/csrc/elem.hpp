@@ -79,6 +79,19 @@ template <typename T, int V> __device__ __forceinline__ void store_vec(T* p, con
     }
 }
 
+// As load_vec, for what is read once: its lines are the first to leave the caches.
+template <typename T, int V> __device__ __forceinline__ Vec<T, V> load_once(const T* p) {
+    if constexpr (sizeof(T) * V != 16) {
+        return load_vec<T, V>(p);
+    } else {
+        using R = typename Raw16<alignof(T)>::type;
+        const R r = __builtin_nontemporal_load((const R*)p);
+        struct Q {
+            uint32_t w[4];
+        } q{{r.x, r.y, r.z, r.w}};
+        return __builtin_bit_cast(Vec<T, V>, q);
+    }
+}
 // The same bits, which the compiler takes for new ones: keeps it from holding
 // what it has unpacked from them in registers until the next use.
 template <typename T, int V> __device__ __forceinline__ void renew(Vec<T, V>& v) {

@@ -307,8 +307,9 @@ __device__ __forceinline__ bool fills(const Sums& q, int64_t n, uint32_t key, in
 // that goes on past the chunk is finished here too, unless it fills the next chunk:
 // then every chunk that it reaches leaves its part for k_embed_join. Eight
 // rows are under way while eight are summed, and the lanes hold the keys and places of
-// a chunk between them. 131072 rows of 1024 bfloat16 for 50000 tokens take 97 us: 345 MB
-// of rows in any order at 3.6 TB/s, whether a wavefront has 4, 8 or 16 KB under way.
+// a chunk between them. Rows are loaded past the caches' usual order, as none is met
+// again: 131072 of 1024 bfloat16 for 50000 tokens take 69 us (345 MB at 5.0 TB/s), 97
+// by plain loads, however many are under way; 16384 rows take the same either way.
 template <typename T, int V, int G> __global__ __launch_bounds__(256) void k_embed_sums(EmbedArgs a, Sums q) {
     using R = Acc<T>;
     constexpr int GROUPS = 256 / G, HELD = CHUNK / G;
@@ -364,7 +365,7 @@ template <typename T, int V, int G> __global__ __launch_bounds__(256) void k_emb
             auto fetch = [&](int i) {
 #pragma unroll
                 for (int j = 0; j < AHEAD; j++)
-                    next[j] = load_vec<T, V>(g + (int64_t)held(places, min(i + j, count - 1)) * a.grad_stride);
+                    next[j] = load_once<T, V>(g + (int64_t)held(places, min(i + j, count - 1)) * a.grad_stride);
             };
             fetch(skip);
             for (int i = skip; i < count && !stops(held(keys, i)); i += AHEAD) {
