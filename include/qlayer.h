@@ -541,8 +541,8 @@ int ql_dropout(ql_type type, int64_t rows, int64_t features, const void* x, int6
  * begins: the state before that step is taken as 0, whatever it holds. A state that is not finite
  * makes its sequence's later ones infinite or NaN, and no others.
  *
- * The backward call: with G_t = grad_h_t + a_{t+1} G_{t+1} (grad_last, which may be NULL, behind the last
- * step; nothing comes back past a start),
+ * The backward call: with G_t = grad_h_t + a_{t+1} G_{t+1} (behind the last step
+ * grad_last, which may be NULL; nothing comes back past a start),
  *   grad_x = (1 - a) G,  grad_gate = G (h_{t-1} - x) a (1 - a),  grad_initial = a_0 G_0
  * (may be NULL). grad_x and grad_gate are contiguous.
  *
