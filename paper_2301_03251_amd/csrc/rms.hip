@@ -14,6 +14,7 @@
 // bits the row's largest |s w| comes from the same step as its sum of squares,
 // and r drops out of y / scale = s w 448 / max |s w|.
 #include <algorithm>
+#include <type_traits>
 
 #include "elem.hpp"
 #include "rms.hpp"
@@ -28,18 +29,37 @@ __device__ __forceinline__ double inv_sqrt(double v) { return 1.0 / sqrt(v); }
 
 constexpr float MOST_E4M3 = 448;
 
-// What takes |s w| <= most to [0, 448]: a power of two first where 448 / most
-// alone would overflow.
-struct Steps {
-    float first, second;
-    __device__ __forceinline__ explicit Steps(float most) {
-        first = most < 1e-30f ? 0x1p100f : 1.0f;
-        second = most > 0 ? MOST_E4M3 / (most * first) : 0;
+// A row's values in [-448, 448]: p 448 / most of p = s w, most = max |p|. A product by 448 /
+// most in fp32 is off by 2^-23 and takes one in seven of the quotients that lie
+// half-way between two e4m3 values (4e-4 of bfloat16's) to the wrong one. So the factor
+// is the next fp32 number up, and the last two bits of the product go. The factor is 0 to
+// 3 2^-24 of itself too large; a quotient of five bits (a half) then comes out less than
+// four steps up, which the two bits take back, and goes to the even value. For bfloat16
+// rows and weights, whose p and most have 16 bits, any other quotient is at least 2^-20.95
+// of itself away from a half and stays on its side. (16384x8192 bfloat16 without a
+// residual: 76 us, 74 without this, 80 with the remainder of a division, 94 in fp64.)
+// Rows whose p may have lost bits, and those with infinities, are done in fp64.
+struct Quotient {
+    double wide = 0;
+    float factor;
+    bool narrow;
+    __device__ __forceinline__ explicit Quotient(float most)
+        : factor(__builtin_bit_cast(float, __builtin_bit_cast(uint32_t, MOST_E4M3 / most) + 1)),
+          narrow(most >= 0x1p-100f && most <= 0x1p127f) {
+        if (!narrow && most > 0) wide = (double)MOST_E4M3 / most;
+    }
+    template <bool NARROW> __device__ __forceinline__ float of(float v, float w) const {
+        if constexpr (NARROW) {
+            return __builtin_bit_cast(float, __builtin_bit_cast(uint32_t, v * w * factor) & ~3u);
+        } else {
+            // converted here: not held in fp64 from row to row
+            asm volatile("" : "+v"(v), "+v"(w));
+            return (float)((double)v * w * wide);
+        }
     }
 };
 
-// Four values in e4m3, rounded to nearest even. Rounding in `second` may leave a
-// value one step past 448, which rounds back to it; NaN stays NaN.
+// Four values in e4m3, rounded to nearest even; NaN stays NaN.
 __device__ __forceinline__ uint32_t e4m3x4(float a, float b, float c, float d) {
     int v = __builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false);
     return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(c, d, v, true);
@@ -120,21 +140,30 @@ __global__ __launch_bounds__(G > 256 ? G : 256) void k_rms_fwd(RmsArgs a) {
             if (a.rstd) ((R*)a.rstd)[row] = rstd;
             if constexpr (Q) a.scale[row] = (float)rstd * ((float)most / MOST_E4M3);
         }
-        const Steps steps((float)most);
+        if constexpr (Q) {
+            const Quotient quotient(most);
+            auto quantize = [&](auto narrow) {
 #pragma unroll
-        for (int k = 0; k < K; k++) {
-            const Span<V> sp((k * G + lane) * V, D);
-            if (!sp.any()) continue;
-            renew(s[k]);
-            if constexpr (Q) {
-                float q[V];
+                for (int k = 0; k < K; k++) {
+                    const Span<V> sp((k * G + lane) * V, D);
+                    if (!sp.any()) continue;
+                    renew(s[k]);
+                    if constexpr (K > 1) renew(w[k]);  // unpacked, 4 vectors of them do not fit: 54 us for 120 at 1000x32768
+                    float q[V];
 #pragma unroll
-                for (int e = 0; e < V; e++) {
-                    const float v = up(s[k].v[e]) * steps.first;
-                    q[e] = (a.weight ? v * (float)up(w[k].v[e]) : v) * steps.second;
+                    for (int e = 0; e < V; e++)
+                        q[e] = quotient.template of<narrow.value>(up(s[k].v[e]), a.weight ? (float)up(w[k].v[e]) : 1);
+                    store_e4m3<V>((uint8_t*)a.y + row * a.D + sp.at, q);
                 }
-                store_e4m3<V>((uint8_t*)a.y + row * a.D + sp.at, q);
-            } else {
+            };
+            if (quotient.narrow) quantize(std::true_type{});
+            else quantize(std::false_type{});
+        } else {
+#pragma unroll
+            for (int k = 0; k < K; k++) {
+                const Span<V> sp((k * G + lane) * V, D);
+                if (!sp.any()) continue;
+                renew(s[k]);
                 Vec<T, V> q;
 #pragma unroll
                 for (int e = 0; e < V; e++) {
@@ -214,14 +243,16 @@ template <typename T, typename W, bool Q> __global__ __launch_bounds__(256) void
         if (a.weight) w = load_vec<W, V>((const W*)a.weight + sp.at);
         const R rstd = ((const R*)a.joined)[2 * row];
         if constexpr (Q) {
-            const Steps steps((float)((const R*)a.joined)[2 * row + 1]);
-            float q[V];
+            const Quotient quotient(((const R*)a.joined)[2 * row + 1]);
+            auto quantize = [&](auto narrow) {
+                float q[V];
 #pragma unroll
-            for (int e = 0; e < V; e++) {
-                const float v = up(s.v[e]) * steps.first;
-                q[e] = (a.weight ? v * (float)up(w.v[e]) : v) * steps.second;
-            }
-            store_e4m3<V>((uint8_t*)a.y + row * a.D + sp.at, q);
+                for (int e = 0; e < V; e++)
+                    q[e] = quotient.template of<narrow.value>(up(s.v[e]), a.weight ? (float)up(w.v[e]) : 1);
+                store_e4m3<V>((uint8_t*)a.y + row * a.D + sp.at, q);
+            };
+            if (quotient.narrow) quantize(std::true_type{});
+            else quantize(std::false_type{});
         } else {
             Vec<T, V> q;
 #pragma unroll
