@@ -178,8 +178,20 @@ template <int N, typename R> __device__ __forceinline__ R lanes_max(R v) {
     return v;
 }
 
+// The largest value over the N lanes of a row's group, as group_sum.
+template <int N, typename R> __device__ __forceinline__ R group_max(R v, R* lds) {
+    v = lanes_max<N <= 64 ? N : 64>(v);
+    if constexpr (N > 64) {
+        if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = v;
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < N / 64; i++) v = larger(v, lds[i]);
+    }
+    return v;
+}
+
 // The sum of s and the largest m >= 0 over a row's group, as group_sum, behind one barrier.
-template <int N, typename R> __device__ __forceinline__ void group_sum_max(R& s, R& m, R* lds_s, R* lds_m) {
+template <int N, typename S, typename M> __device__ __forceinline__ void group_sum_max(S& s, M& m, S* lds_s, M* lds_m) {
     s = lanes_sum<N <= 64 ? N : 64>(s);
     m = lanes_max<N <= 64 ? N : 64>(m);
     if constexpr (N > 64) {

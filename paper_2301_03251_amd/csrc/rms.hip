@@ -14,7 +14,6 @@
 // bits the row's largest |s w| comes from the same step as its sum of squares,
 // and r drops out of y / scale = s w 448 / max |s w|.
 #include <algorithm>
-#include <type_traits>
 
 #include "elem.hpp"
 #include "rms.hpp"
@@ -37,27 +36,27 @@ constexpr float MOST_E4M3 = 448;
 // four steps up, which the two bits take back, and goes to the even value. For bfloat16
 // rows and weights, whose p and most have 16 bits, any other quotient is at least 2^-20.95
 // of itself away from a half and stays on its side. (16384x8192 bfloat16 without a
-// residual: 76 us, 74 without this, 80 with the remainder of a division, 94 in fp64.)
-// Rows whose p may have lost bits, and those with infinities, are done in fp64.
-struct Quotient {
-    double wide = 0;
+// residual: 77 us, 74 without this, 80 with the remainder of a division, 94 in fp64.)
+// Rows whose p may have lost bits, or is past fp32, and those with infinities are done in
+// fp64, behind the others (16384x8192, half of the rows at 1e-35: 176 us).
+__device__ __forceinline__ bool in_fp32(float most) { return most >= 0x1p-100f && most <= 0x1p127f; }
+
+struct Narrow {
     float factor;
-    bool narrow;
-    __device__ __forceinline__ explicit Quotient(float most)
-        : factor(__builtin_bit_cast(float, __builtin_bit_cast(uint32_t, MOST_E4M3 / most) + 1)),
-          narrow(most >= 0x1p-100f && most <= 0x1p127f) {
-        if (!narrow && most > 0) wide = (double)MOST_E4M3 / most;
-    }
-    template <bool NARROW> __device__ __forceinline__ float of(float v, float w) const {
-        if constexpr (NARROW) {
-            return __builtin_bit_cast(float, __builtin_bit_cast(uint32_t, v * w * factor) & ~3u);
-        } else {
-            // converted here: not held in fp64 from row to row
-            asm volatile("" : "+v"(v), "+v"(w));
-            return (float)((double)v * w * wide);
-        }
+    __device__ __forceinline__ explicit Narrow(float most)
+        : factor(most > 0 ? __builtin_bit_cast(float, __builtin_bit_cast(uint32_t, MOST_E4M3 / most) + 1) : 0) {}
+    __device__ __forceinline__ float operator()(float p) const {
+        return __builtin_bit_cast(float, __builtin_bit_cast(uint32_t, p * factor) & ~3u);
     }
 };
+struct Wide {
+    double factor;
+    __device__ __forceinline__ explicit Wide(double most) : factor(most > 0 ? MOST_E4M3 / most : 0) {}
+    __device__ __forceinline__ float operator()(double p) const { return (float)(p * factor); }
+};
+// The scales beside them.
+__device__ __forceinline__ float scale_of(float rstd, float most) { return rstd * (most / MOST_E4M3); }
+__device__ __forceinline__ float scale_of(float rstd, double most) { return (float)((double)rstd * most / MOST_E4M3); }
 
 // Four values in e4m3, rounded to nearest even; NaN stays NaN.
 __device__ __forceinline__ uint32_t e4m3x4(float a, float b, float c, float d) {
@@ -80,15 +79,51 @@ template <int V> __device__ __forceinline__ void store_e4m3(uint8_t* p, const fl
     }
 }
 
+// A row of k_rms_fwd in fp64. The lanes read their elements again.
+template <typename T, typename W, int V, int G, int K>
+__device__ __forceinline__ void wide_row(const RmsArgs& a, int64_t row, int lane, float rstd, double* lds) {
+    const T* s = a.residual ? (const T*)a.summed + row * a.D : (const T*)a.x + row * a.x_stride;
+    auto each = [&](auto f) {
+#pragma unroll 1
+        for (int k = 0; k < K; k++) {
+            const Span<V> sp((k * G + lane) * V, (int)a.D);
+            if (!sp.any()) break;
+            const Vec<T, V> v = load_vec<T, V>(s + sp.at);
+            Vec<W, V> w;
+            if (a.weight) w = load_vec<W, V>((const W*)a.weight + sp.at);
+            f(sp.at, v, w);
+        }
+    };
+    auto product = [&](const Vec<T, V>& v, const Vec<W, V>& w, int e) {
+        return (double)up(v.v[e]) * (a.weight ? (double)up(w.v[e]) : 1);
+    };
+    double most = 0;
+    each([&](int, auto& v, auto& w) {
+#pragma unroll
+        for (int e = 0; e < V; e++) most = larger(most, fabs(product(v, w, e)));
+    });
+    most = group_max<G>(most, lds);
+    if (lane == 0) a.scale[row] = scale_of(rstd, most);
+    const Wide quotient(most);
+    each([&](int at, auto& v, auto& w) {
+        float q[V];
+#pragma unroll
+        for (int e = 0; e < V; e++) q[e] = quotient(product(v, w, e));
+        store_e4m3<V>((uint8_t*)a.y + row * a.D + at, q);
+    });
+}
+
 // Rows in registers: a group of G lanes holds a row as K vectors of V elements
 // per lane (vector k of lane l starts at element (k G + l) V), and takes row,
 // row + stride, ...: the weight is read once, and the next row's loads are under
-// way while a row is worked on.
+// way while a row is worked on. In 8 bits with K = 2 the registers are held to six
+// wavefronts a SIMD: 16384x8192 bfloat16 with float32 weights 80 us, 87 with five.
 template <typename T, typename W, int V, int G, int K, bool Q>
-__global__ __launch_bounds__(G > 256 ? G : 256) void k_rms_fwd(RmsArgs a) {
+__global__ __launch_bounds__(G > 256 ? G : 256, Q && K == 2 ? 6 : 1) void k_rms_fwd(RmsArgs a) {
     using R = Acc<T>;
     constexpr int ROWS = (G > 256 ? G : 256) / G;
     __shared__ R lds[2][2][G > 64 ? G / 64 : 1];
+    __shared__ double lds_wide[Q && G > 64 ? G / 64 : 1];
     const int lane = threadIdx.x % G, D = (int)a.D;
     const R d = (R)a.D;
     const int64_t stride = (int64_t)gridDim.x * ROWS;
@@ -108,6 +143,7 @@ __global__ __launch_bounds__(G > 256 ? G : 256) void k_rms_fwd(RmsArgs a) {
     for (int k = 0; k < K; k++) {
         if (a.weight) w[k] = load_vec<W, V>((const W*)a.weight + Span<V>((k * G + lane) * V, D).at);
     }
+    bool waiting = false;  // the same for all of a row's lanes
     for (int turn = 0; row < a.rows; row += stride, turn ^= 1) {
         Vec<T, V> s[K];
 #pragma unroll
@@ -136,28 +172,28 @@ __global__ __launch_bounds__(G > 256 ? G : 256) void k_rms_fwd(RmsArgs a) {
         if constexpr (Q) group_sum_max<G>(sum, most, lds[turn][0], lds[turn][1]);
         else sum = group_sum<G>(sum, lds[turn][0]);
         const R rstd = inv_sqrt(sum / d + (R)a.eps);
+        // Rows for fp64 wait until the others are done, their scale -rstd so far. Those of
+        // zeros need not: no product is above 2^-150, and where 1 / rms is at most 2^10 the
+        // scale is below 2^-148, two of fp32's least steps.
+        const bool narrow = in_fp32(most) || (most == 0 && sum >= d * (R)(0x1p-20 - a.eps));
         if (lane == 0) {
             if (a.rstd) ((R*)a.rstd)[row] = rstd;
-            if constexpr (Q) a.scale[row] = (float)rstd * ((float)most / MOST_E4M3);
+            if constexpr (Q) a.scale[row] = narrow ? scale_of(rstd, most) : -rstd;
         }
         if constexpr (Q) {
-            const Quotient quotient(most);
-            auto quantize = [&](auto narrow) {
+            waiting |= !narrow;
+            const Narrow quotient(most);
 #pragma unroll
-                for (int k = 0; k < K; k++) {
-                    const Span<V> sp((k * G + lane) * V, D);
-                    if (!sp.any()) continue;
-                    renew(s[k]);
-                    if constexpr (K > 1) renew(w[k]);  // unpacked, 4 vectors of them do not fit: 54 us for 120 at 1000x32768
-                    float q[V];
+            for (int k = 0; k < K; k++) {
+                const Span<V> sp((k * G + lane) * V, D);
+                if (!sp.any()) continue;
+                renew(s[k]);
+                if constexpr (K > 1) renew(w[k]);  // unpacked, 4 vectors of them do not fit: 54 us for 120 at 1000x32768
+                float q[V];
 #pragma unroll
-                    for (int e = 0; e < V; e++)
-                        q[e] = quotient.template of<narrow.value>(up(s[k].v[e]), a.weight ? (float)up(w[k].v[e]) : 1);
-                    store_e4m3<V>((uint8_t*)a.y + row * a.D + sp.at, q);
-                }
-            };
-            if (quotient.narrow) quantize(std::true_type{});
-            else quantize(std::false_type{});
+                for (int e = 0; e < V; e++) q[e] = quotient(a.weight ? up(s[k].v[e]) * (float)up(w[k].v[e]) : up(s[k].v[e]));
+                store_e4m3<V>((uint8_t*)a.y + row * a.D + sp.at, q);
+            }
         } else {
 #pragma unroll
             for (int k = 0; k < K; k++) {
@@ -175,6 +211,17 @@ __global__ __launch_bounds__(G > 256 ? G : 256) void k_rms_fwd(RmsArgs a) {
             }
         }
     }
+    if constexpr (Q) {
+        if (!waiting) return;
+        if constexpr (G > 64) __syncthreads();
+        else __threadfence_block();
+        for (row = (int64_t)blockIdx.x * ROWS + threadIdx.x / G; row < a.rows; row += stride) {
+            const float mark = a.scale[row];
+            if (!(__builtin_bit_cast(uint32_t, mark) >> 31)) continue;
+            if constexpr (G > 64) __syncthreads();  // the row before has been read from lds_wide
+            wide_row<T, W, V, G, K>(a, row, lane, -mark, lds_wide);
+        }
+    }
 }
 
 // Long rows go through the chip in segments of 256 vectors, one workgroup each,
@@ -183,10 +230,16 @@ __global__ __launch_bounds__(G > 256 ? G : 256) void k_rms_fwd(RmsArgs a) {
 // workgroups as there are segments: no workgroup's registers hold such a row.
 template <typename T> constexpr int SEGMENT = 256 * VEC<T>;
 
+// A segment's sum of squares and largest |s w|; a row's 1 / rms and largest.
+struct Part {
+    double sum, most;
+};
+
 template <typename T, typename W, bool Q> __global__ __launch_bounds__(256) void k_rms_fwd_sums(RmsArgs a, int segments) {
     using R = Acc<T>;
     constexpr int V = VEC<T>;
     __shared__ R lds[2][2][4];
+    __shared__ double lds_wide[4];
     int turn = 0;
     for (int64_t i = blockIdx.x; i < a.rows * segments; i += gridDim.x, turn ^= 1) {
         const int64_t row = i / segments;
@@ -208,24 +261,36 @@ template <typename T, typename W, bool Q> __global__ __launch_bounds__(256) void
             if constexpr (Q) most = larger(most, fabsf(a.weight ? v * (R)up(w.v[e]) : v));
         }
         group_sum_max<256>(sum, most, lds[turn][0], lds[turn][1]);
-        if (threadIdx.x == 0) ((R*)a.sums)[2 * i] = sum, ((R*)a.sums)[2 * i + 1] = most;
+        double wide = most;
+        if constexpr (Q) {
+            if (!in_fp32(most)) {
+                wide = 0;
+#pragma unroll
+                for (int e = 0; e < V; e++)
+                    wide = larger(wide, fabs((double)up(s.v[e]) * (a.weight ? (double)up(w.v[e]) : 1)));
+                wide = group_max<256>(wide, lds_wide);
+            }
+        }
+        if (threadIdx.x == 0) ((Part*)a.sums)[i] = {sum, wide};
     }
 }
 
 template <typename T, bool Q> __global__ __launch_bounds__(256) void k_rms_fwd_join(RmsArgs a, int segments) {
     using R = Acc<T>;
-    __shared__ R lds[2][2][4];
+    __shared__ R lds[2][4];
+    __shared__ double lds_most[2][4];
     int turn = 0;
     for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x, turn ^= 1) {
-        const R* s = (const R*)a.sums + 2 * row * segments;
-        R sum = 0, most = 0;
-        for (int j = threadIdx.x; j < segments; j += 256) sum += s[2 * j], most = larger(most, s[2 * j + 1]);
-        group_sum_max<256>(sum, most, lds[turn][0], lds[turn][1]);
+        const Part* s = (const Part*)a.sums + row * segments;
+        R sum = 0;
+        double most = 0;
+        for (int j = threadIdx.x; j < segments; j += 256) sum += (R)s[j].sum, most = larger(most, s[j].most);
+        group_sum_max<256>(sum, most, lds[turn], lds_most[turn]);
         const R rstd = inv_sqrt(sum / (R)a.D + (R)a.eps);
         if (threadIdx.x == 0) {
-            ((R*)a.joined)[2 * row] = rstd, ((R*)a.joined)[2 * row + 1] = most;
+            ((Part*)a.joined)[row] = {rstd, most};
             if (a.rstd) ((R*)a.rstd)[row] = rstd;
-            if constexpr (Q) a.scale[row] = (float)rstd * ((float)most / MOST_E4M3);
+            if constexpr (Q) a.scale[row] = in_fp32((float)most) ? scale_of(rstd, (float)most) : scale_of(rstd, most);
         }
     }
 }
@@ -241,19 +306,21 @@ template <typename T, typename W, bool Q> __global__ __launch_bounds__(256) void
                                        : load_vec<T, V>((const T*)a.x + row * a.x_stride + sp.at);
         Vec<W, V> w;
         if (a.weight) w = load_vec<W, V>((const W*)a.weight + sp.at);
-        const R rstd = ((const R*)a.joined)[2 * row];
+        const Part part = ((const Part*)a.joined)[row];
         if constexpr (Q) {
-            const Quotient quotient(((const R*)a.joined)[2 * row + 1]);
-            auto quantize = [&](auto narrow) {
-                float q[V];
+            float q[V];
+            if (in_fp32((float)part.most)) {
+                const Narrow quotient((float)part.most);
 #pragma unroll
-                for (int e = 0; e < V; e++)
-                    q[e] = quotient.template of<narrow.value>(up(s.v[e]), a.weight ? (float)up(w.v[e]) : 1);
-                store_e4m3<V>((uint8_t*)a.y + row * a.D + sp.at, q);
-            };
-            if (quotient.narrow) quantize(std::true_type{});
-            else quantize(std::false_type{});
+                for (int e = 0; e < V; e++) q[e] = quotient(a.weight ? up(s.v[e]) * (float)up(w.v[e]) : up(s.v[e]));
+            } else {
+                const Wide quotient(part.most);
+#pragma unroll
+                for (int e = 0; e < V; e++) q[e] = quotient((double)up(s.v[e]) * (a.weight ? (double)up(w.v[e]) : 1));
+            }
+            store_e4m3<V>((uint8_t*)a.y + row * a.D + sp.at, q);
         } else {
+            const R rstd = (R)part.sum;
             Vec<T, V> q;
 #pragma unroll
             for (int e = 0; e < V; e++) {
@@ -501,10 +568,9 @@ Split split_of(int type, int64_t rows, int64_t D) {
 size_t acc_size(int type) { return type == E_F64 ? 8 : 4; }
 size_t rounded(size_t bytes) { return (bytes + 255) & ~(size_t)255; }
 size_t part_bytes(const Split& p, int type, int64_t D) { return rounded((size_t)p.parts * (size_t)D * acc_size(type)); }
-// Two sums a segment forward, one backward; as many for a row behind them.
-size_t sums_bytes(int type, int64_t rows, int segments, int each) {
-    return rounded((size_t)(rows * segments) * each * acc_size(type));
-}
+// The segments' sums (Part forward), and as many of rows behind them.
+size_t part_sums_bytes(int64_t rows, int segments) { return rounded((size_t)(rows * segments) * sizeof(Part)); }
+size_t sums_bytes(int type, int64_t rows, int segments) { return rounded((size_t)(rows * segments) * acc_size(type)); }
 
 int grid_of(int64_t groups) { return (int)std::min<int64_t>(groups, 4096); }
 
@@ -517,7 +583,7 @@ template <typename T, typename W, bool Q, int G, int K, int V = VEC<T>> hipError
 template <typename T, typename W, bool Q> hipError_t forward(int type, RmsArgs a, void* ws, hipStream_t s) {
     constexpr int V = VEC<T>;
     if (const int segments = forward_segments(type, a.rows, a.D)) {
-        a.sums = ws, a.joined = (char*)ws + sums_bytes(type, a.rows, segments, 2);
+        a.sums = ws, a.joined = (char*)ws + part_sums_bytes(a.rows, segments);
         k_rms_fwd_sums<T, W, Q><<<grid_of(a.rows * segments), 256, 0, s>>>(a, segments);
         k_rms_fwd_join<T, Q><<<grid_of(a.rows), 256, 0, s>>>(a, segments);
         k_rms_fwd_segment<T, W, Q><<<grid_of(a.rows * segments), 256, 0, s>>>(a, segments);
@@ -557,7 +623,7 @@ template <typename T, typename W> hipError_t backward(int type, RmsArgs a, void*
         case 1024 * 8 + 2: e = backward_rows<T, W, 1024, 2>(a, p, s); break;
         default:
             if (a.grad_x && a.rows > 0) {
-                a.joined = (char*)a.sums + sums_bytes(type, a.rows, p.segments, 1);
+                a.joined = (char*)a.sums + sums_bytes(type, a.rows, p.segments);
                 k_rms_bwd_sums<T, W><<<grid_of(a.rows * p.segments), 256, 0, s>>>(a, p.segments);
                 k_rms_bwd_join<T><<<grid_of(a.rows), 256, 0, s>>>(a, p.segments);
             }
@@ -585,10 +651,10 @@ size_t rms_workspace(int type, int64_t rows, int64_t D, bool backward) {
     if (backward) {
         const Split p = split_of(type, rows, D);
         return part_bytes(p, type, D) +
-               (p.segments ? sums_bytes(type, rows, p.segments, 1) + sums_bytes(type, rows, 1, 1) : 0);
+               (p.segments ? sums_bytes(type, rows, p.segments) + sums_bytes(type, rows, 1) : 0);
     }
     const int segments = forward_segments(type, rows, D);
-    return segments ? sums_bytes(type, rows, segments, 2) + sums_bytes(type, rows, 1, 2) : 0;
+    return segments ? part_sums_bytes(rows, segments) + part_sums_bytes(rows, 1) : 0;
 }
 
 hipError_t launch_rms_forward(int type, int wtype, const RmsArgs& a, void* ws, hipStream_t s) {

@@ -25,7 +25,7 @@ struct RmsArgs {
     void* grad_x;          // [rows][D] or null (backward)
     void* grad_weight;     // [D] or null (backward)
     void* part;            // workspace: the column sums of each workgroup (backward),
-    void* sums;            // of long rows the sums of each segment,
+    void* sums;            // of long rows the sums (forward also the largest) of each segment,
     void* joined;          // and of each row
     int64_t rows, D, x_stride, residual_stride, grad_stride, grad_sum_stride;
     double eps;

@@ -123,3 +123,26 @@ def test_large_rows_under_small_weights(n, name):
     x[:, n // 3], w[n // 3] = 1e18, 0
     q, scale, s = Q.rms_norm_quantized(x, w)
     check(s, w, q, scale)
+
+
+@pytest.mark.parametrize("name", ["f32", "bf16"])
+@pytest.mark.parametrize("n", SIZES)
+def test_products_far_from_one(n, name):
+    """Products s w that float32 does not hold, or not in all bits, where y and its scale are ordinary."""
+    g = torch.Generator().manual_seed(n)
+    base = torch.randn(6, n, generator=g, dtype=torch.float64)
+    for size, weight in ((1e10, 1e-40), (1e10, 1e30), (1e-30, 1e-10), (1e-20, 1e-20), (1e-20, 1e25)):
+        x = (base * size).to(TYPES[name]).cuda()
+        w = (weight * (1 + 0.2 * torch.randn(n, generator=g, dtype=torch.float64))).to(TYPES[name]).cuda()
+        q, scale, s = Q.rms_norm_quantized(x, w)
+        assert torch.isfinite(q.float()).all() and torch.isfinite(scale).all(), (size, weight)
+        check(s, w, q, scale)
+
+
+@pytest.mark.parametrize("n", SIZES)
+def test_scales_below_the_normal_range(n):
+    """Rows of 1e-39 and 1e-41 keep what bits their scale has."""
+    x = torch.randn(4, n, generator=torch.Generator().manual_seed(n), dtype=torch.float64)
+    x = (x * torch.tensor([[1e-37], [1e-39], [1e-41], [1e-30]])).float().cuda()
+    q, scale, s = Q.rms_norm_quantized(x)
+    check(s, None, q, scale)
