@@ -54,9 +54,13 @@ struct Wide {
     __device__ __forceinline__ explicit Wide(double most) : factor(most > 0 ? MOST_E4M3 / most : 0) {}
     __device__ __forceinline__ float operator()(double p) const { return (float)(p * factor); }
 };
-// The scales beside them.
-__device__ __forceinline__ float scale_of(float rstd, float most) { return rstd * (most / MOST_E4M3); }
-__device__ __forceinline__ float scale_of(float rstd, double most) { return (float)((double)rstd * most / MOST_E4M3); }
+// The scales beside them. A row of zeros has 0 also where eps is 0 and rstd infinite; NaN stays.
+__device__ __forceinline__ float scale_of(float rstd, float most) {
+    return most > 0 ? rstd * (most / MOST_E4M3) : 0;
+}
+__device__ __forceinline__ float scale_of(float rstd, double most) {
+    return most > 0 || rstd != rstd ? (float)((double)rstd * most / MOST_E4M3) : 0;
+}
 
 // Four values in e4m3, rounded to nearest even; NaN stays NaN.
 __device__ __forceinline__ uint32_t e4m3x4(float a, float b, float c, float d) {

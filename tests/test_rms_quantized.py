@@ -146,3 +146,15 @@ def test_scales_below_the_normal_range(n):
     x = (x * torch.tensor([[1e-37], [1e-39], [1e-41], [1e-30]])).float().cuda()
     q, scale, s = Q.rms_norm_quantized(x)
     check(s, None, q, scale)
+
+
+@pytest.mark.parametrize("n", SIZES)
+def test_rows_of_zeros_without_eps(n):
+    """1 / 0 does not reach the scale, and the rows beside them are as ever."""
+    x = torch.randn(5, n, generator=torch.Generator().manual_seed(n)).cuda()
+    x[1] = x[4] = 0
+    for w in (None, torch.ones(n, device="cuda")):
+        q, scale, s = Q.rms_norm_quantized(x, w, eps=0.0)
+        assert not scale[[1, 4]].any() and not q[[1, 4]].float().any()
+        rest = [0, 2, 3]
+        check(s[rest], w, q[rest], scale[rest], 0.0)
