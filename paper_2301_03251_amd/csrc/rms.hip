@@ -38,7 +38,7 @@ constexpr float MOST_E4M3 = 448;
 // of itself away from a half and stays on its side. (16384x8192 bfloat16 without a
 // residual: 77 us, 74 without this, 80 with the remainder of a division, 94 in fp64.)
 // Rows whose p may have lost bits, or is past fp32, and those with infinities are done in
-// fp64, behind the others (16384x8192, half of the rows at 1e-35: 176 us).
+// fp64, behind the others (16384x8192, half of the rows at 1e-35: 187 us).
 __device__ __forceinline__ bool in_fp32(float most) { return most >= 0x1p-100f && most <= 0x1p127f; }
 
 struct Narrow {
@@ -83,6 +83,14 @@ template <int V> __device__ __forceinline__ void store_e4m3(uint8_t* p, const fl
     }
 }
 
+// Infinity if one of the elements is, else m.
+template <typename T, int V, typename R> __device__ __forceinline__ R infinity_or(const Vec<T, V>& s, R m) {
+    bool any = false;
+#pragma unroll
+    for (int e = 0; e < V; e++) any |= fabsf(up(s.v[e])) == INFINITY;
+    return any ? (R)INFINITY : m;
+}
+
 // A row of k_rms_fwd in fp64. The lanes read their elements again.
 template <typename T, typename W, int V, int G, int K>
 __device__ __forceinline__ void wide_row(const RmsArgs& a, int64_t row, int lane, float rstd, double* lds) {
@@ -105,6 +113,7 @@ __device__ __forceinline__ void wide_row(const RmsArgs& a, int64_t row, int lane
     each([&](int, auto& v, auto& w) {
 #pragma unroll
         for (int e = 0; e < V; e++) most = larger(most, fabs(product(v, w, e)));
+        most = infinity_or(v, most);
     });
     most = group_max<G>(most, lds);
     if (lane == 0) a.scale[row] = scale_of(rstd, most);
@@ -176,10 +185,11 @@ __global__ __launch_bounds__(G > 256 ? G : 256, Q && K == 2 ? 6 : 1) void k_rms_
         if constexpr (Q) group_sum_max<G>(sum, most, lds[turn][0], lds[turn][1]);
         else sum = group_sum<G>(sum, lds[turn][0]);
         const R rstd = inv_sqrt(sum / d + (R)a.eps);
-        // Rows for fp64 wait until the others are done, their scale -rstd so far. Those of
-        // zeros need not: no product is above 2^-150, and where 1 / rms is at most 2^10 the
+        // Rows for fp64 wait until the others are done, their scale -rstd so far, and those that
+        // may hold an infinity (under a weight of 0 no product tells). Rows of zeros
+        // need not: no product is above 2^-150, and where 1 / rms is at most 2^10 the
         // scale is below 2^-148, two of fp32's least steps.
-        const bool narrow = in_fp32(most) || (most == 0 && sum >= d * (R)(0x1p-20 - a.eps));
+        const bool narrow = sum < (R)INFINITY && (in_fp32(most) || (most == 0 && sum >= d * (R)(0x1p-20 - a.eps)));
         if (lane == 0) {
             if (a.rstd) ((R*)a.rstd)[row] = rstd;
             if constexpr (Q) a.scale[row] = narrow ? scale_of(rstd, most) : -rstd;
@@ -264,6 +274,8 @@ template <typename T, typename W, bool Q> __global__ __launch_bounds__(256) void
             sum += sp.own(e) ? v * v : 0;
             if constexpr (Q) most = larger(most, fabsf(a.weight ? v * (R)up(w.v[e]) : v));
         }
+        if constexpr (Q)
+            if (sum == (R)INFINITY) most = infinity_or(s, most);
         group_sum_max<256>(sum, most, lds[turn][0], lds[turn][1]);
         double wide = most;
         if constexpr (Q) {
@@ -272,7 +284,7 @@ template <typename T, typename W, bool Q> __global__ __launch_bounds__(256) void
 #pragma unroll
                 for (int e = 0; e < V; e++)
                     wide = larger(wide, fabs((double)up(s.v[e]) * (a.weight ? (double)up(w.v[e]) : 1)));
-                wide = group_max<256>(wide, lds_wide);
+                wide = group_max<256>(infinity_or(s, wide), lds_wide);
             }
         }
         if (threadIdx.x == 0) ((Part*)a.sums)[i] = {sum, wide};

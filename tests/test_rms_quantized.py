@@ -158,3 +158,19 @@ def test_rows_of_zeros_without_eps(n):
         assert not scale[[1, 4]].any() and not q[[1, 4]].float().any()
         rest = [0, 2, 3]
         check(s[rest], w, q[rest], scale[rest], 0.0)
+
+
+@pytest.mark.parametrize("n", SIZES)
+def test_infinities_under_a_weight_of_zero(n):
+    """The scale of a row that holds an infinity is NaN, whatever weight stands at it."""
+    g = torch.Generator().manual_seed(n)
+    x, w = torch.randn(4, n, generator=g).cuda(), torch.ones(n, device="cuda")
+    want = Q.rms_norm_quantized(x, w)[1]
+    w[n // 2] = 0
+    clean = Q.rms_norm_quantized(x, w)
+    x[2, n // 2] = float("inf")
+    q, scale, _ = Q.rms_norm_quantized(x, w)
+    assert torch.isnan(scale[2]) and torch.isfinite(want).all()
+    keep = [0, 1, 3]
+    assert torch.equal(scale[keep], clean[1][keep]) and torch.equal(q[keep].float(), clean[0][keep].float())
+    assert torch.isnan(Q.rms_norm_quantized(x, torch.zeros_like(w))[1][2])
