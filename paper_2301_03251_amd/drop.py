@@ -96,11 +96,21 @@ def _module_class():
             # the seed, and the number of calls so far
             self.register_buffer("key", torch.tensor([int(seed), 0], dtype=torch.int64, device=device))
 
-        def forward(self, x):
-            if not self.training or self.p == 0:
-                return x
+        def draw(self):
+            """The next call's key, which is counted."""
             key = self.key.clone()
             self.key[1].add_(1)
+            return key
+
+        def forward(self, x, key=None):
+            if not self.training or self.p == 0:
+                return x
+            if key is None:
+                # a call from inside a backward pass is a recomputation, which must not draw another mask
+                if torch._C._current_graph_task_id() != -1:
+                    raise RuntimeError("Dropout in a backward pass (recomputation by a checkpoint) needs the first "
+                                       "call's key: draw it outside, key = layer.draw(), and call layer(x, key)")
+                key = self.draw()
             return dropout(x, self.p, key)
 
         def extra_repr(self):
@@ -114,5 +124,10 @@ def Dropout(p=0.1, seed=None, device="cuda"):
     ``key`` holds the seed (in [0, 2^63); None draws one from torch's generator)
     and the number of calls so far, which is the offset: every call has a mask of
     its own, in replays of a captured graph too, and a loaded state goes on where
-    the saved one was. Processes that train together give each its own seed."""
+    the saved one was. Processes that train together give each its own seed.
+
+    Recomputation (``torch.utils.checkpoint``) runs a layer again in the backward
+    pass, where it must draw the mask that it drew before: what is checkpointed takes
+    the key as an argument, ``key = layer.draw()`` outside and ``layer(x, key)``
+    inside. Without a key a call in a backward pass raises RuntimeError."""
     return _module_class()(p, seed, device)

@@ -1,0 +1,112 @@
+"""The Dropout module under recomputation (CPU, the kernel replaced by the generator on
+the host; and on the kernel, which needs an MI355X)."""
+
+from __future__ import annotations
+
+import numpy as np
+import pytest
+
+torch = pytest.importorskip("torch")
+from torch.utils.checkpoint import checkpoint  # noqa: E402
+
+import paper_2301_03251_amd as Q  # noqa: E402
+from paper_2301_03251_amd import drop  # noqa: E402
+from test_dropout import philox  # noqa: E402
+
+MODES = [False, True]  # checkpoint's use_reentrant
+
+
+def on_host(x, p, key):
+    """``dropout_forward`` of CPU tensors."""
+    seed, offset = (int(k) % (1 << 64) for k in key)
+    n = x.numel()
+    words = philox(np.arange((n + 3) // 4, dtype=np.uint64), offset, seed).reshape(-1)[:n]
+    keep = torch.from_numpy(words.astype(np.int64) >= round(p * 2.0 ** 32)).view(x.shape)
+    return torch.where(keep, x / (1 - p), torch.zeros_like(x))
+
+
+@pytest.fixture
+def host(monkeypatch):
+    monkeypatch.setattr(drop, "dropout_forward", on_host)
+
+
+class Net(torch.nn.Module):
+    """Two dropouts, the first one also called twice; what is around them needs its inputs again."""
+
+    def __init__(self, device="cpu"):
+        super().__init__()
+        torch.manual_seed(1)
+        self.a, self.b = torch.nn.Linear(12, 16, device=device), torch.nn.Linear(16, 5, device=device)
+        self.first, self.second = Q.Dropout(0.4, seed=3, device=device), Q.Dropout(0.2, seed=4, device=device)
+
+    def forward(self, x, keys=(None, None, None)):
+        y = self.first(torch.tanh(self.a(x)), keys[0])
+        return self.second(torch.tanh(self.b(torch.sin(self.first(y * y, keys[1])))), keys[2])
+
+    def draw(self):
+        return self.first.draw(), self.first.draw(), self.second.draw()
+
+
+def gradients(net, loss):
+    return torch.autograd.grad(loss, list(net.parameters()))
+
+
+def recomputed(device):
+    x = torch.randn(9, 12, device=device)
+    for reentrant in MODES:
+        x = x.detach().requires_grad_(reentrant)
+        plain, net = Net(device), Net(device)
+        for _ in range(2):  # the second step goes on from the first one's counters
+            want = gradients(plain, plain(x).square().sum())
+            keys = net.draw()
+            y = checkpoint(lambda x, *k: net(x, k), x, *keys, use_reentrant=reentrant)
+            if reentrant:  # takes gradients by .backward() alone
+                net.zero_grad()
+                y.square().sum().backward()
+                got = [p.grad for p in net.parameters()]
+            else:
+                got = gradients(net, y.square().sum())
+            assert all(torch.equal(p, q) for p, q in zip(got, want))
+        assert torch.equal(net.first.key, plain.first.key) and net.first.key.tolist() == [3, 4]
+
+
+def refused(device):
+    """Each mode, whichever layers are inside; neither counts a call that was refused."""
+    x = torch.randn(9, 12, device=device, requires_grad=True)
+    for reentrant in MODES:
+        net = Net(device)
+        y = checkpoint(net, x, use_reentrant=reentrant)
+        assert net.first.key.tolist() == [3, 2] and net.second.key.tolist() == [4, 1]
+        with pytest.raises(RuntimeError, match="backward pass"):
+            y.sum().backward()
+        assert net.first.key.tolist() == [3, 2] and net.second.key.tolist() == [4, 1]
+        # what drops nothing may be run again
+        net.eval()
+        checkpoint(net, x, use_reentrant=reentrant).sum().backward()
+
+
+def test_recomputation(host):
+    """Keys drawn outside give the gradients of the network without recomputation."""
+    recomputed("cpu")
+
+
+def test_recomputation_without_keys_is_refused(host):
+    """A mask of its own in the second forward pass would give another function's gradients."""
+    refused("cpu")
+
+
+def test_draw(host):
+    layer, x = Q.Dropout(0.5, seed=8, device="cpu"), torch.randn(30, 7)
+    keys = [layer.draw() for _ in range(3)]
+    assert [k.tolist() for k in keys] == [[8, 0], [8, 1], [8, 2]] and layer.key.tolist() == [8, 3]
+    assert torch.equal(layer(x, keys[1]), on_host(x, 0.5, (8, 1))) and layer.key.tolist() == [8, 3]
+    assert torch.equal(layer(x, (8, 1)), on_host(x, 0.5, (8, 1)))
+    assert torch.equal(layer(x), on_host(x, 0.5, (8, 3))) and layer.key.tolist() == [8, 4]
+
+
+@pytest.mark.gpu
+def test_recomputation_on_the_kernel():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    recomputed("cuda")
+    refused("cuda")
