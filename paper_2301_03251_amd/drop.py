@@ -93,8 +93,33 @@ def _module_class():
                 raise ValueError("p must be in [0, 1]")
             if seed is None:
                 seed = int(torch.randint((1 << 63) - 1, ()))
-            # the seed, and the number of calls so far
-            self.register_buffer("key", torch.tensor([int(seed), 0], dtype=torch.int64, device=device))
+            # the seed, and the number of calls so far. No buffer: DistributedDataParallel makes the
+            # ranks' buffers alike, and with them their masks
+            self.key = torch.tensor([int(seed), 0], dtype=torch.int64, device=device)
+
+        def _apply(self, fn, recurse=True):
+            super()._apply(fn, recurse)
+            self.key = fn(self.key)
+            return self
+
+        def _save_to_state_dict(self, destination, prefix, keep_vars):
+            super()._save_to_state_dict(destination, prefix, keep_vars)
+            destination[prefix + "key"] = self.key if keep_vars else self.key.detach()
+
+        def _load_from_state_dict(self, state, prefix, metadata, strict, missing, unexpected, errors):
+            name = prefix + "key"
+            key = state.get(name)
+            super()._load_from_state_dict({k: v for k, v in state.items() if k != name}, prefix, metadata, strict, missing,
+                                          unexpected, errors)
+            if key is None:
+                if strict:
+                    missing.append(name)
+            elif key.shape != self.key.shape:
+                errors.append(f"size mismatch for {name}: {tuple(key.shape)} in the state, {tuple(self.key.shape)} here")
+            elif metadata.get("assign_to_params_buffers"):
+                self.key = key
+            else:
+                self.key.copy_(key)  # in place: a captured graph reads it where it is
 
         def draw(self):
             """The next call's key, which is counted."""
@@ -120,11 +145,13 @@ def _module_class():
 
 
 def Dropout(p=0.1, seed=None, device="cuda"):
-    """``dropout`` as a ``torch.nn.Module``; the identity in evaluation. Its buffer
+    """``dropout`` as a ``torch.nn.Module``; the identity in evaluation. Its tensor
     ``key`` holds the seed (in [0, 2^63); None draws one from torch's generator)
     and the number of calls so far, which is the offset: every call has a mask of
     its own, in replays of a captured graph too, and a loaded state goes on where
-    the saved one was. Processes that train together give each its own seed.
+    the saved one was. Layers of a network and processes that train together have each
+    its own seed, which ``DistributedDataParallel`` leaves alone; processes that load
+    one state set ``key[0]`` anew.
 
     Recomputation (``torch.utils.checkpoint``) runs a layer again in the backward
     pass, where it must draw the mask that it drew before: what is checkpointed takes

@@ -1,12 +1,18 @@
-"""The Dropout module under recomputation (CPU, the kernel replaced by the generator on
-the host; and on the kernel, which needs an MI355X)."""
+"""The Dropout module under recomputation and in processes that train together (CPU, the
+kernel replaced by the generator on the host; recomputation also on the kernel, which
+needs an MI355X)."""
 
 from __future__ import annotations
+
+import os
+import socket
 
 import numpy as np
 import pytest
 
 torch = pytest.importorskip("torch")
+import torch.distributed as dist  # noqa: E402
+import torch.multiprocessing as mp  # noqa: E402
 from torch.utils.checkpoint import checkpoint  # noqa: E402
 
 import paper_2301_03251_amd as Q  # noqa: E402
@@ -102,6 +108,56 @@ def test_draw(host):
     assert torch.equal(layer(x, keys[1]), on_host(x, 0.5, (8, 1))) and layer.key.tolist() == [8, 3]
     assert torch.equal(layer(x, (8, 1)), on_host(x, 0.5, (8, 1)))
     assert torch.equal(layer(x), on_host(x, 0.5, (8, 3))) and layer.key.tolist() == [8, 4]
+
+
+def _rank(rank, port, path):
+    os.environ.update(MASTER_ADDR="127.0.0.1", MASTER_PORT=str(port), RANK=str(rank), WORLD_SIZE="2")
+    dist.init_process_group("gloo")
+    drop.dropout_forward = on_host
+    torch.manual_seed(0)
+    net = torch.nn.Sequential(torch.nn.Linear(6, 40), Q.Dropout(0.5, seed=100 + rank, device="cpu"))
+    both = torch.nn.parallel.DistributedDataParallel(net)
+    masks = []
+    for _ in range(3):
+        y = both(torch.ones(8, 6))
+        masks.append(y.detach() != 0)
+        y.sum().backward()
+    torch.save((net[1].key.clone(), torch.stack(masks)), f"{path}/{rank}")
+    dist.destroy_process_group()
+
+
+def test_processes_keep_their_seeds(tmp_path):
+    """DistributedDataParallel makes the ranks' parameters and buffers alike, but not their masks."""
+    with socket.socket() as s:
+        s.bind(("127.0.0.1", 0))
+        port = s.getsockname()[1]
+    mp.spawn(_rank, (port, str(tmp_path)), nprocs=2)
+    (a, m), (b, n) = (torch.load(tmp_path / str(r), weights_only=True) for r in range(2))
+    assert a.tolist() == [100, 3] and b.tolist() == [101, 3]
+    assert all((m[i] != n[i]).any() for i in range(3))
+
+
+def test_state(host):
+    """The key is part of the state under its name, follows the module, and a loaded one keeps its address."""
+    net = torch.nn.Sequential(Q.Dropout(0.5, seed=9, device="cpu"))
+    net[0].draw()
+    state = net.state_dict()
+    assert list(state) == ["0.key"] and state["0.key"].tolist() == [9, 1]
+    other = torch.nn.Sequential(Q.Dropout(0.5, device="cpu"))
+    held = other[0].key
+    assert str(other.load_state_dict(state)) == "<All keys matched successfully>"
+    assert other[0].key is held and held.tolist() == [9, 1]
+    state["0.key"].zero_()
+    assert held.tolist() == [9, 1]
+    assert other.load_state_dict({}, strict=False).missing_keys == ["0.key"]
+    with pytest.raises(RuntimeError, match="Missing key"):
+        other.load_state_dict({})
+    with pytest.raises(RuntimeError, match="size mismatch"):
+        other.load_state_dict({"0.key": torch.zeros(3, dtype=torch.int64)})
+    assert other.half().double()[0].key.dtype == torch.int64
+    assert other.to("meta")[0].key.device.type == "meta"
+    other.load_state_dict({"0.key": torch.tensor([2, 6])}, assign=True)
+    assert other[0].key.tolist() == [2, 6]
 
 
 @pytest.mark.gpu
