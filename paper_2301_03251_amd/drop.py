@@ -5,6 +5,7 @@ is stored, and a captured graph draws a new one at every replay.
 
 from __future__ import annotations
 
+import copy
 import functools
 
 from .norm import _check_rows, _rows, has_tangent, on_device
@@ -85,6 +86,9 @@ def dropout(x, p, key):
 def _module_class():
     torch = _torch()
 
+    def new_seed():
+        return int(torch.randint((1 << 63) - 1, ()))
+
     class DropoutModule(torch.nn.Module):
         def __init__(self, p, seed, device):
             super().__init__()
@@ -92,10 +96,17 @@ def _module_class():
             if not 0 <= self.p <= 1:
                 raise ValueError("p must be in [0, 1]")
             if seed is None:
-                seed = int(torch.randint((1 << 63) - 1, ()))
+                seed = new_seed()
             # the seed, and the number of calls so far. No buffer: DistributedDataParallel makes the
             # ranks' buffers alike, and with them their masks
             self.key = torch.tensor([int(seed), 0], dtype=torch.int64, device=device)
+
+        def __deepcopy__(self, memo):
+            twin = self.__class__.__new__(self.__class__)
+            memo[id(self)] = twin
+            twin.__setstate__(copy.deepcopy(self.__dict__, memo))
+            twin.key.copy_(torch.tensor([new_seed(), 0], dtype=torch.int64))
+            return twin
 
         def _apply(self, fn, recurse=True):
             super()._apply(fn, recurse)
@@ -151,7 +162,8 @@ def Dropout(p=0.1, seed=None, device="cuda"):
     its own, in replays of a captured graph too, and a loaded state goes on where
     the saved one was. Layers of a network and processes that train together have each
     its own seed, which ``DistributedDataParallel`` leaves alone; processes that load
-    one state set ``key[0]`` anew.
+    one state set ``key[0]`` anew. A copy (``copy.deepcopy``) draws a seed of its own, as
+    None does, and starts at 0: blocks that are copies of one drop other places.
 
     Recomputation (``torch.utils.checkpoint``) runs a layer again in the backward
     pass, where it must draw the mask that it drew before: what is checkpointed takes

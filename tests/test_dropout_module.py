@@ -1,9 +1,10 @@
-"""The Dropout module under recomputation and in processes that train together (CPU, the
-kernel replaced by the generator on the host; recomputation also on the kernel, which
-needs an MI355X)."""
+"""The Dropout module under recomputation, in processes that train together and in
+copies of a network (CPU, the kernel replaced by the generator on the host), and
+recomputation on the kernel (needs an MI355X)."""
 
 from __future__ import annotations
 
+import copy
 import os
 import socket
 
@@ -135,6 +136,27 @@ def test_processes_keep_their_seeds(tmp_path):
     (a, m), (b, n) = (torch.load(tmp_path / str(r), weights_only=True) for r in range(2))
     assert a.tolist() == [100, 3] and b.tolist() == [101, 3]
     assert all((m[i] != n[i]).any() for i in range(3))
+
+
+def test_copies_have_masks_of_their_own(host):
+    """Blocks of a network that are copies of one, as layers with seeds of their own."""
+    block = torch.nn.Sequential(torch.nn.Linear(6, 40), Q.Dropout(0.5, seed=9, device="cpu"))
+    block[1].draw()
+    torch.manual_seed(5)
+    first, second = copy.deepcopy(block), copy.deepcopy(block)
+    assert block[1].key.tolist() == [9, 1]
+    keys = [m[1].key.tolist() for m in (block, first, second)]
+    assert len({k[0] for k in keys}) == 3 and keys[1][1] == keys[2][1] == 0
+    x = torch.ones(8, 6)
+    masks = [m(x) != 0 for m in (block, first, second)]
+    assert (masks[0] != masks[1]).any() and (masks[0] != masks[2]).any() and (masks[1] != masks[2]).any()
+    assert torch.equal(first[0].weight, block[0].weight) and first[1].p == 0.5 and first[1].training
+    torch.manual_seed(5)
+    assert copy.deepcopy(block)[1].key.tolist() == keys[1]
+    # one layer in two places is one layer in the copy too
+    shared = torch.nn.ModuleList([block[1], block[1]])
+    twin = copy.deepcopy(shared)
+    assert twin[0] is twin[1] and twin[0] is not block[1]
 
 
 def test_state(host):
