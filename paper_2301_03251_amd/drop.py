@@ -62,7 +62,7 @@ def _function():
                 ctx.key = None
                 ctx.save_for_backward(key)
             else:
-                ctx.key = key
+                ctx.key = key = tuple(key)  # the caller's list may change before the backward pass
             return dropout_forward(x, p, key)
 
         @staticmethod

@@ -182,6 +182,15 @@ def test_state(host):
     assert other[0].key.tolist() == [2, 6]
 
 
+def test_a_key_of_numbers_is_kept_as_it_was(host):
+    """The gradient's mask is the forward's, whatever becomes of the caller's list."""
+    key, x = [3, 4], torch.randn(40, 5, requires_grad=True)
+    y = Q.dropout(x, 0.5, key)
+    key[1] = 5
+    y.sum().backward()
+    assert torch.equal(x.grad, on_host(torch.ones_like(x), 0.5, (3, 4)))
+
+
 @pytest.mark.gpu
 def test_recomputation_on_the_kernel():
     if not torch.cuda.is_available():
