@@ -502,7 +502,8 @@ int ql_rms_norm_backward(ql_type type, ql_type weight_type, int64_t rows, int64_
  * [rows][features] contiguous, in the order of i: the same bits every time. Tokens that
  * are the padding or outside the table have no gradient, rows without tokens get zeros.
  *
- * count in [0, 2^31), rows in [1, 2^31), features in [1, 2^22], scale finite.
+ * count in [0, 2^31), rows in [1, 2^31), features in [1, 2^22], scale finite (as
+ * QL_F32 where the rows are not QL_F64).
  * ql_embedding_workspace_bytes gives the backward call's device workspace. */
 int ql_embedding_forward(ql_type type, int tokens_64, int64_t count, int64_t rows, int64_t features,
                          const void* tokens, const void* weight, int64_t weight_stride,

@@ -24,6 +24,11 @@ int check_embedding(int type, int64_t count, int64_t rows, int64_t features) {
     return QL_OK;
 }
 
+// A factor that the arithmetic (fp64 for QL_F64, else fp32) holds.
+bool scale_ok(int type, double scale) {
+    return std::isfinite(scale) && (type == QL_F64 || std::isfinite((float)scale));
+}
+
 static_assert(QL_SCAN_BLOCK == SCAN_BLOCK, "the header's block is the kernels'");
 
 int check_scan(int type, int64_t batch, int64_t steps, int64_t features) {
@@ -100,7 +105,7 @@ int ql_embedding_forward(ql_type type, int tokens_64, int64_t count, int64_t row
                          const void* weight, int64_t weight_stride, double scale, int has_padding, int64_t padding,
                          void* y, hipStream_t stream) {
     if (int rc = check_embedding(type, count, rows, features)) return rc;
-    if (!std::isfinite(scale)) return fail(QL_EINVAL, "scale must be finite");
+    if (!scale_ok(type, scale)) return fail(QL_EINVAL, "scale must be finite, beside other rows than QL_F64 in QL_F32");
     if (!stride_ok(rows, weight_stride)) return fail(QL_EINVAL, "weight_stride out of range");
     if (count > 0 && (!tokens || !weight || !y)) return fail(QL_EINVAL, "tokens, weight or y is NULL");
     if (!aligned(tokens, tokens_64 ? QL_F64 : QL_F32) || !aligned(weight, type) || !aligned(y, type))
@@ -123,7 +128,7 @@ int ql_embedding_backward(ql_type type, int tokens_64, int64_t count, int64_t ro
                           const void* tokens, const void* grad_y, int64_t grad_stride, double scale, int has_padding,
                           int64_t padding, void* grad_weight, void* ws, size_t ws_bytes, hipStream_t stream) {
     if (int rc = check_embedding(type, count, rows, features)) return rc;
-    if (!std::isfinite(scale)) return fail(QL_EINVAL, "scale must be finite");
+    if (!scale_ok(type, scale)) return fail(QL_EINVAL, "scale must be finite, beside other rows than QL_F64 in QL_F32");
     if (!stride_ok(count, grad_stride)) return fail(QL_EINVAL, "grad_stride out of range");
     if (!grad_weight || (count > 0 && (!tokens || !grad_y)))
         return fail(QL_EINVAL, "tokens, grad_y or grad_weight is NULL");
