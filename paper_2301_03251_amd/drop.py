@@ -36,7 +36,7 @@ def dropout_forward(x, p, key):
     torch = _torch()
     device, shape, xt = _check_rows(x)
     if isinstance(key, torch.Tensor) and (key.dtype != torch.int64 or key.shape != (2,) or key.get_device() != device
-                                          or not key.is_contiguous()):
+                                          or not key.is_contiguous() or key.is_neg()):
         raise ValueError("key must be (seed, offset) or a contiguous int64 tensor of the two on x's device")
     seed, offset, address = _numbers(key)
     there = on_device(device)

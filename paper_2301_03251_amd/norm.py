@@ -129,7 +129,7 @@ def layer_norm_backward(grad_y, x, mean, rstd, weight=None, want_x=True, want_we
         raise ValueError("grad_y must have x's shape, dtype and device")
     sd = x.dtype if xt < 2 else _torch().float32
     for s in (mean, rstd):
-        if s.shape != shape[:-1] or s.dtype != sd or s.get_device() != device or not s.is_contiguous():
+        if s.shape != shape[:-1] or s.dtype != sd or s.get_device() != device or not s.is_contiguous() or s.is_neg():
             raise ValueError(f"mean and rstd must be contiguous {sd} tensors {tuple(shape[:-1])} on x's device")
     there = on_device(device)
     if there is not None:

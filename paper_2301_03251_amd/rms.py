@@ -96,7 +96,8 @@ def rms_norm_backward(grad_y, summed, rstd, weight=None, grad_summed=None, want_
     if grad_summed is not None:
         _like_x(grad_summed, summed, "grad_summed")
     sd = summed.dtype if xt < 2 else _torch().float32
-    if rstd.shape != shape[:-1] or rstd.dtype != sd or rstd.get_device() != device or not rstd.is_contiguous():
+    if (rstd.shape != shape[:-1] or rstd.dtype != sd or rstd.get_device() != device or not rstd.is_contiguous()
+            or rstd.is_neg()):
         raise ValueError(f"rstd must be a contiguous {sd} tensor {tuple(shape[:-1])} on x's device")
     there = on_device(device)
     if there is not None:

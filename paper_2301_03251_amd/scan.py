@@ -110,7 +110,7 @@ def gated_scan_backward(grad_h, x, gate, states, starts=None, grad_last=None, wa
     batch, steps, features = x.shape
     wide, blocks = _wide(x), (steps + BLOCK - 1) // BLOCK
     if (tuple(states.shape) != (batch, blocks, features) or states.dtype != wide or states.get_device() != device
-            or not states.is_contiguous()):
+            or not states.is_contiguous() or states.is_neg()):
         raise ValueError(f"states must be a contiguous {wide} tensor {(batch, blocks, features)} on x's device")
     if starts is not None:
         _check_starts(starts, x)

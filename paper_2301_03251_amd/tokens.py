@@ -54,7 +54,7 @@ def embedding_forward(tokens, weight, scale=1.0, padding=None):
         weight, _, stride = _rows(weight, weight.shape)
     else:
         weight, stride = weight.resolve_neg(), features
-    tokens = tokens.contiguous()
+    tokens = tokens.contiguous().resolve_neg()
     y = weight.new_empty((*tokens.shape, features))
     _check(load().ql_embedding_forward(t, wide, tokens.numel(), rows, features, tokens.data_ptr(), weight.data_ptr(),
                                        stride, scale, *_padding(padding), y.data_ptr(), _stream(weight.device)))
@@ -77,7 +77,7 @@ def embedding_backward(grad, tokens, rows, scale=1.0, padding=None):
     rows, features, n = int(rows), grad.shape[-1], tokens.numel()
     ws_bytes = _workspace_bytes(t, n, rows, features)
     grad, _, stride = _rows(grad, grad.shape)
-    tokens = tokens.contiguous()
+    tokens = tokens.contiguous().resolve_neg()
     out = grad.new_empty((rows, features))
     ws = grad.new_empty(ws_bytes, dtype=torch.uint8)
     _check(load().ql_embedding_backward(t, wide, n, rows, features, tokens.data_ptr(), grad.data_ptr(), stride, scale,

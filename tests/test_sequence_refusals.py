@@ -33,3 +33,40 @@ def test_embedding_scales_past_the_arithmetic_are_refused():
         assert (fwd, bwd) == (0, -1) and "workspace" in message
     fwd, bwd, message = _scaled(lib, F64, 1e300)
     assert (fwd, bwd) == (0, -1) and "workspace" in message
+
+
+@pytest.fixture
+def need_gpu():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    Q.load()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [torch.int64, torch.int32])
+def test_negative_views_of_tokens(need_gpu, dtype):
+    t = torch.randint(1, 20, (50,), device="cuda", dtype=dtype)
+    w, g = torch.randn(20, 12, device="cuda"), torch.randn(50, 12, device="cuda")
+    view = torch._neg_view(-t)
+    assert torch.equal(view, t)
+    assert torch.equal(Q.embedding_forward(view, w), Q.embedding_forward(t, w))
+    assert torch.equal(Q.embedding_backward(g, view, 20), Q.embedding_backward(g, t, 20))
+
+
+@pytest.mark.gpu
+def test_negative_views_of_what_must_be_contiguous(need_gpu):
+    """A key, the norms' statistics and the recurrence's states are read as they lie: refused."""
+    x, g = torch.randn(6, 40, device="cuda"), torch.randn(6, 40, device="cuda")
+    with pytest.raises(ValueError, match="key"):
+        Q.dropout(x, 0.5, torch._neg_view(torch.tensor([5, 9], device="cuda")))
+    _, s, r = Q.rms_norm_forward(x)
+    with pytest.raises(ValueError, match="rstd"):
+        Q.rms_norm_backward(g, s, torch._neg_view(-r))
+    _, mean, rstd = Q.layer_norm_forward(x)
+    for a, b in ((torch._neg_view(-mean), rstd), (mean, torch._neg_view(-rstd))):
+        with pytest.raises(ValueError, match="rstd"):
+            Q.layer_norm_backward(g, x, a, b)
+    x, z, g = torch.randn(3, 2, 40, 8, device="cuda").unbind(0)
+    _, _, states = Q.gated_scan_forward(x, z)
+    with pytest.raises(ValueError, match="states"):
+        Q.gated_scan_backward(g, x, z, torch._neg_view(-states))
