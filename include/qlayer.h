@@ -470,7 +470,9 @@ int ql_muon_step(ql_type type, const ql_matrix* matrices, int32_t count,
  * scale not NULL: y is bytes in e4m3 (OCP FP8, largest value 448) instead, and
  * scale[rows] (QL_F32) = max |s * rstd * weight| / 448 is what they are multiples of; a
  * row of zeros has scale 0, and where the row holds an infinity or NaN the scale is
- * NaN. Not for QL_F64 (QL_EUNSUPPORTED).
+ * NaN. The bytes are s * weight * 448 / max |s * weight| to nearest, halves to even: as
+ * defined for QL_BF16 rows and weights, otherwise of a value that may be off by 2^-20 of
+ * itself. Not for QL_F64 (QL_EUNSUPPORTED).
  *
  * The backward call: with h = s * rstd,
  *   grad_x      = rstd * (g w - h * mean(g w h)) + grad_summed (NULL: 0),
@@ -499,8 +501,9 @@ int ql_rms_norm_backward(ql_type type, ql_type weight_type, int64_t rows, int64_
  * table or not) give zeros. Other tokens outside [0, rows) give NaN.
  *
  * The backward call: grad_weight[v] = scale * (sum over i with t_i = v of grad_y_i),
- * [rows][features] contiguous, in the order of i: the same bits every time. Tokens that
- * are the padding or outside the table have no gradient, rows without tokens get zeros.
+ * [rows][features] contiguous, added in an order that the call's tokens fix: the same
+ * bits every time (with other tokens beside it a row's sum may be rounded otherwise). Tokens
+ * that are the padding or outside the table have no gradient, rows without tokens get zeros.
  *
  * count in [0, 2^31), rows in [1, 2^31), features in [1, 2^22], scale finite (as
  * QL_F32 where the rows are not QL_F64).

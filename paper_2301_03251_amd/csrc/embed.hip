@@ -5,12 +5,15 @@
 // Tokens that are the padding have a row of zeros and no gradient. One outside the
 // table has a row of NaN, as nothing on the host sees it, and no gradient.
 //
-// The gradient's sums run in the order of the tokens' places, whatever the
+// How the gradient's sums are put together follows from the call's tokens, not from the
 // grid: places are sorted by token (a stable radix sort), and a wavefront sums the
-// rows of a chunk of sorted places, token by token. A token whose rows end in the
-// chunk or the next is done there; of one that goes on further the parts are joined
-// in a second launch. Rows without tokens are zeros, written beside the sort. HBM
-// bounds large calls (N rows of g read, the table written), launches the others.
+// rows of a chunk of sorted places, token by token, in the order of their places. A
+// token whose rows end in the chunk or the next is done there; of one that goes on
+// further the parts are joined in a second launch, every fourth by one wavefront and
+// then the four. Chunks are cut from the whole list: with other tokens in the call a
+// token's rows may be split elsewhere, and its sum rounded otherwise. Rows without
+// tokens are zeros, written beside the sort. HBM bounds large calls (N rows of g read,
+// the table written), launches the others.
 #include <algorithm>
 
 #include "elem.hpp"
@@ -286,8 +289,7 @@ template <typename T> __global__ __launch_bounds__(256) void k_embed_move(EmbedA
 
 // Places of a chunk, whose rows one group of lanes sums: 64 where that is enough of
 // them, down to 8 for the few tokens of a small call (4096 of 1000x64 float32: 14 us of
-// sums in 64 chunks, 7 in 512). It goes by the number of tokens alone, and so
-// do the bits of a sum.
+// sums in 64 chunks, 7 in 512). It goes by the number of tokens alone.
 constexpr int CHUNK = 64, AHEAD = 8;
 int chunk_of(int64_t n) { return (int)std::max<int64_t>(AHEAD, std::min<int64_t>(CHUNK, n / 2048 / AHEAD * AHEAD)); }
 

@@ -570,7 +570,8 @@ Split split_of(int type, int64_t rows, int64_t D) {
         }
     if (p.lanes) {
         // at least four rows for a group of lanes, whose column sums cost a write
-        // and a read of a row in fp32; no more workgroups than run at once
+        // and a read of a row in fp32 (fewer rows are not measured); no more
+        // workgroups than run at once
         const int64_t groups = std::max(1, 256 / p.lanes), most = p.lanes < 512 ? 512 : 256;
         p.parts = std::max<int64_t>(1, std::min(most, (rows + 4 * groups - 1) / (4 * groups)));
     } else {

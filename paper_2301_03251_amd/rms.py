@@ -68,8 +68,8 @@ def rms_norm_forward(x, weight=None, residual=None, eps=1e-6, stats=True):
 def rms_norm_quantized(x, weight=None, residual=None, eps=1e-6):
     """(q, scale, summed): ``rms_norm_forward`` with y in 8 bits, for rows of
     float32, bfloat16 or float16. q is float8_e4m3fn and scale float32 [...], the
-    row's largest |y| / 448: y = q * scale, rounded to nearest. A row of zeros has
-    scale 0. Not differentiable: refused where autograd would follow it."""
+    row's largest |y| / 448: y = q * scale, rounded to nearest, halves to even. A row
+    of zeros has scale 0, one that holds an infinity or NaN has NaN. Not differentiable: refused where autograd would follow it."""
     torch = _torch()
     ts = [t for t in (x, weight, residual) if t is not None]
     if (torch.is_grad_enabled() and any(t.requires_grad for t in ts)) or has_tangent(*ts):

@@ -63,7 +63,7 @@ def embedding_forward(tokens, weight, scale=1.0, padding=None):
 
 def embedding_backward(grad, tokens, rows, scale=1.0, padding=None):
     """The gradient [rows, features] of the table from grad [..., features] and the
-    forward's tokens [...]: sums in the order of the tokens' places, the same bits
+    forward's tokens [...]: sums in an order that the call's tokens fix, the same bits
     every time; zeros for rows without tokens. Autograd does not see the call."""
     torch = _torch()
     device, t = grad.get_device(), type_of(grad, "grad")
