@@ -174,3 +174,30 @@ def test_infinities_under_a_weight_of_zero(n):
     keep = [0, 1, 3]
     assert torch.equal(scale[keep], clean[1][keep]) and torch.equal(q[keep].float(), clean[0][keep].float())
     assert torch.isnan(Q.rms_norm_quantized(x, torch.zeros_like(w))[1][2])
+
+
+@pytest.mark.parametrize("name,rows,n", [("bf16", 200000, 24), ("f32", 70000, 100), ("bf16", 20000, 700), ("f16", 20000, 900), ("bf16", 9000, 3000),
+                                         ("f32", 9000, 3000), ("bf16", 9000, 6000), ("bf16", 4500, 12000), ("bf16", 600, 40000)])
+def test_ordinary_rows_among_others(name, rows, n):
+    """More rows than are in work at once: rows of zeros, tiny ones, such with an infinity or
+    NaN and ordinary ones, in any order, each as it is alone."""
+    g = torch.Generator(device="cuda").manual_seed(n)
+    x = torch.randn(rows, n, generator=g, device="cuda")
+    kind = torch.randint(6, (rows,), generator=g, device="cuda")
+    small = 6e-8 if name == "f16" else 1e-38
+    x = (x * torch.where(kind == 1, small, 1.0)[:, None] * (kind != 2)[:, None]).to(TYPES[name])
+    bad = torch.nonzero(kind >= 4)[:, 0]
+    at = torch.randint(n, (len(bad),), generator=g, device="cuda")
+    x[bad, at] = torch.where(kind[bad] == 4, float("inf"), float("nan")).to(x.dtype)
+    w = (1 + 0.2 * torch.randn(n, generator=g, device="cuda")).to(TYPES[name])
+    w[::7] = 0
+    eps = 1e-12
+    res = torch.zeros_like(x) if n % 200 == 100 or n == 6000 else None
+    q, scale, s = Q.rms_norm_quantized(x, w, res, eps)
+    assert torch.isnan(scale[bad]).all()
+    good = torch.nonzero(kind < 4)[:, 0]
+    for part in good.split(2000):
+        check(s[part], w, q[part], scale[part], eps)
+    assert not scale[kind == 2].any() and not q[kind == 2].float().any()
+    again = Q.rms_norm_quantized(x, w, res, eps)
+    assert torch.equal(again[0].view(torch.uint8), q.view(torch.uint8)) and torch.equal(again[1][good], scale[good])
